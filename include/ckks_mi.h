@@ -152,7 +152,10 @@ typedef enum {
     CKKS_OP_LINEAR_PROJECT = 11, /* shape = {limbs of the inputs, tokens, d_in, d_out, n1} */
     CKKS_OP_LINEAR_PROJECT_TM = 12, /* the same shape */
     CKKS_OP_ATTN_SCORES = 13,   /* shape = {limbs of the inputs, tokens, head_dim} */
-    CKKS_OP_ATTN_APPLY = 14     /* shape = {limbs of the scores, limbs of the values, tokens, head_dim} */
+    CKKS_OP_ATTN_APPLY = 14,    /* shape = {limbs of the scores, limbs of the values, tokens, head_dim} */
+    CKKS_OP_ROPE_TABLES = 15,   /* rope_tables and cache_tables; shape unused */
+    CKKS_OP_ROPE = 16,          /* shape = {limbs of the inputs, ciphertexts of one call} */
+    CKKS_OP_CACHE_APPEND = 17   /* shape = {limbs of the inputs, heads of one call} */
 } ckks_op;
 size_t ckks_workspace_bytes(const ckks_ctx *ctx, int op, const uint32_t *shape);
 ckks_status ckks_set_workspace(ckks_ctx *ctx, void *dev, size_t bytes);
@@ -392,6 +395,106 @@ ckks_status ckks_attention_apply(ckks_ctx *ctx, const ckks_buf *p, uint32_t n_p,
                                  const uint32_t *v_of_p, const ckks_attn_shape *shape, const uint64_t *dev_rlk,
                                  const int32_t *key_steps, const uint64_t *const *dev_keys, uint32_t n_keys,
                                  ckks_buf *out);
+
+/* ---- rotary positions and the key/value cache ------------------------------ */
+
+/* Rotary positions (RoPE) on ciphertexts, and appending encrypted keys and
+ * values to pages that the attention calls above read.  Both weight a few
+ * rotations of a ciphertext by plaintext tables before one division by P q_level:
+ *   out = Rescale(ModDown( sum_j pt_j t_j )),
+ *   t_j = P (sigma_g(c0), 0) + sum_d sigma_g(D_d) key_j,d  over Q_level u P,
+ * D the ModUp digits of c1 and g the Galois element of term j (t_j = P (c0, c1)
+ * where the rotation is by nothing), exactly: the stages are ckks_modup's,
+ * ckks_moddown's and ckks_rescale's.  Needs special primes; any primes the
+ * context takes.
+ *
+ * Shape.  `tokens` tokens a ciphertext (T, a power of two up to N/2; D = N/2/T
+ * features), heads of `head_dim` features (any size up to D; features after the
+ * last whole head are left as they are), of which the first `rot_dim` (even) are
+ * rotated and the others left as they are.  CKKS_TOKEN_MAJOR: slot t*D + f holds
+ * feature f of token t (the attention calls' layout); CKKS_FEATURE_MAJOR: slot
+ * f*T + t.  CKKS_ROPE_HALF: feature d < rot_dim/2 of a head turns with feature
+ * d + rot_dim/2; CKKS_ROPE_INTERLEAVED: feature 2i with feature 2i + 1.  A pair
+ * (x, y) of pair index i becomes (x cos - y sin, y cos + x sin). */
+enum { CKKS_TOKEN_MAJOR = 0, CKKS_FEATURE_MAJOR = 1 };
+enum { CKKS_ROPE_HALF = 0, CKKS_ROPE_INTERLEAVED = 1 };
+typedef struct {
+    uint32_t tokens, head_dim, rot_dim, layout, pairing;
+} ckks_rope_shape;
+
+/* dev_cos, dev_sin[i][k] = factor cos, sin(dev_positions[i] * dev_inv_freq[k]),
+ * i < count, k < half (rot_dim/2): fp64, the product's rounding error carried, so
+ * far positions (up to 2^53) are as exact as near ones.  Frequencies scaled for
+ * long contexts are the caller's; any other source of cosines and sines does as
+ * well.  Nothing is done for count or half 0. */
+ckks_status ckks_rope_cos_sin(ckks_ctx *ctx, const int64_t *dev_positions, uint32_t count, const double *dev_inv_freq,
+                              uint32_t half, double factor, double *dev_cos, double *dev_sin);
+
+/* The tables of ckks_rope, dev_tables [3][n_limbs + n_p][N]: plaintexts over q_0 ..
+ * q_(n_limbs-1) and the special primes, NTT domain, encoded as by ckks_encode at
+ * scale q_(n_limbs-1), for inputs of n_limbs limbs.  Token first + i (i < count)
+ * turns by row i of dev_cos and dev_sin ([count][rot_dim/2]); the slots of every
+ * other token become zero.  Table 0 holds cos (1 on features left alone), 1 the
+ * -sin of each pair's lower feature, 2 the sin of its upper one.  With -sin for
+ * sin the rotation turns back (the transposed rotation, of gradients).  |cos|
+ * and |sin| up to 2^62 / q keep the coefficients inside ckks_encode's bound.
+ * Scratch: CKKS_OP_ROPE_TABLES. */
+ckks_status ckks_rope_tables(ckks_ctx *ctx, const ckks_rope_shape *shape, uint32_t first, uint32_t count,
+                             const double *dev_cos, const double *dev_sin, uint32_t n_limbs, uint64_t *dev_tables);
+
+/* Rotate `count` ciphertexts (queries or keys), equal n_limbs = level + 1 >= 2,
+ * by the tables of that many limbs; out[r]: n_limbs = level, scale set to
+ * in[r]'s (the tables' scale cancels in the rescale).  Keys (Galois,
+ * key_steps[r] -> dev_keys[r], steps taken modulo N/2): the left rotations by
+ * h and -h, h = rot_dim/2 (half pairs) or 1 (interleaved), times T feature-major.
+ * Outputs may overlap neither inputs nor each other (CKKS_EINVAL).  Scratch:
+ * CKKS_OP_ROPE.  Other errors: CKKS_EINVAL (shape, descriptors), CKKS_ELEVEL,
+ * CKKS_ENOKEY, CKKS_EUNSUPPORTED (no special primes); all before any launch. */
+ckks_status ckks_rope(ckks_ctx *ctx, const ckks_buf *in, uint32_t count, const ckks_rope_shape *shape,
+                      const uint64_t *dev_tables, const int32_t *key_steps, const uint64_t *const *dev_keys,
+                      uint32_t n_keys, ckks_buf *out);
+
+/* A paged cache.  A page holds T tokens of one head, repeated in every head
+ * position, as a ciphertext with one limb fewer than the new tokens' (the
+ * attention calls' key or value ciphertext).  k_pages, v_pages: n_pages
+ * descriptors each; table (host, [n_heads][n_blocks]): the page of tokens
+ * b T .. b T + T - 1 of head h, the same in both pools. */
+typedef struct {
+    ckks_buf *k_pages, *v_pages;
+    uint32_t n_pages;
+    const uint32_t *table;
+    uint32_t n_blocks;
+} ckks_cache;
+
+/* The tables of ckks_cache_append for `count` (at most T) tokens after `length`
+ * in the cache: for each page touched (one, or two over a page border)
+ * [4][n_limbs + n_p][N], ckks_rope_tables' three for that page's tokens and one of
+ * ones in their slots; with rot_dim 0 (keys that are not rotated) the last alone.
+ * dev_cos, dev_sin: [count][rot_dim/2].  A step's tables serve every layer.
+ * Token-major only.  Scratch: CKKS_OP_ROPE_TABLES. */
+ckks_status ckks_cache_tables(ckks_ctx *ctx, const ckks_rope_shape *shape, uint32_t length, uint32_t count,
+                              const double *dev_cos, const double *dev_sin, uint32_t n_limbs, uint64_t *dev_tables);
+
+/* Append `count` tokens of n_heads heads to a cache of `length` tokens: token
+ * src + i of k[h] (rotated by the tables) and of v[h] becomes token length + i of
+ * head h.  k, v: one head a ciphertext, repeated in every head position; n_limbs =
+ * level + 1 >= 2, equal; equal scales within each.  The slots of their other
+ * tokens are not read into the cache.  The pages' slots before the new tokens stay, slots after them become
+ * zero where a page is begun (length a multiple of T, or the second page) and
+ * stay (zero, as it was begun) otherwise; no other page is touched.  A begun page's old
+ * contents do not matter; a started one must have the new tokens' scale.
+ * fork (host, [n_heads], or NULL): the page that head h's started page continues,
+ * if not itself - its contents are taken over, and it stays as it is (sequences that share
+ * a prefix).  The pages written must be distinct, and none may be an input or
+ * another head's forked page (CKKS_EINVAL).  Keys: the left rotations by -m and, with rot_dim > 0, h - m and
+ * -h - m (as ckks_rope's h), m = D ((length - src) mod T); a token placed in its
+ * own slot by the encryptor (src = length mod T) needs +-h alone, and its values
+ * no key.  Scratch: CKKS_OP_CACHE_APPEND.  Errors as ckks_rope's, CKKS_EINVAL also
+ * for a page index out of range or a table too short, CKKS_ESCALE. */
+ckks_status ckks_cache_append(ckks_ctx *ctx, const ckks_buf *k, const ckks_buf *v, uint32_t n_heads,
+                              const ckks_rope_shape *shape, uint32_t src, uint32_t length, uint32_t count,
+                              const uint64_t *dev_tables, const int32_t *key_steps, const uint64_t *const *dev_keys,
+                              uint32_t n_keys, const ckks_cache *cache, const uint32_t *fork);
 
 /* ---- measurement helpers ------------------------------------------------- */
 

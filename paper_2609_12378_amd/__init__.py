@@ -9,6 +9,7 @@ current torch stream at context creation.  The library must be built first
 without the built library raises instead of falling back to anything else.
 """
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 from typing import Dict, List, Optional, Sequence
@@ -18,7 +19,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libckks_mi.so")
 
-__all__ = ["Context", "Buf", "CkksError", "load_library", "LIB_PATH"]
+__all__ = ["Context", "Buf", "CkksError", "load_library", "rope_inv_freq", "LIB_PATH"]
 
 
 class CkksError(RuntimeError):
@@ -43,6 +44,15 @@ class _ProjShape(ctypes.Structure):
 
 class _AttnShape(ctypes.Structure):
     _fields_ = [("tokens", ctypes.c_uint32), ("head_dim", ctypes.c_uint32)]
+
+
+class _RopeShape(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_uint32) for f in ("tokens", "head_dim", "rot_dim", "layout", "pairing")]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.POINTER(_Buf)), ("v_pages", ctypes.POINTER(_Buf)), ("n_pages", ctypes.c_uint32),
+                ("table", ctypes.POINTER(ctypes.c_uint32)), ("n_blocks", ctypes.c_uint32)]
 
 
 _LIB = None
@@ -90,6 +100,12 @@ _SIGS = {
                                              _VP, _U32, _BP]),
     "ckks_attention_apply": (ctypes.c_int, [_VP, _BP, _U32, _BP, _U32, _VP, ctypes.POINTER(_AttnShape), _VP, _VP,
                                             _VP, _U32, _BP]),
+    "ckks_rope_cos_sin": (ctypes.c_int, [_VP, _VP, _U32, _VP, _U32, _DBL, _VP, _VP]),
+    "ckks_rope_tables": (ctypes.c_int, [_VP, ctypes.POINTER(_RopeShape), _U32, _U32, _VP, _VP, _U32, _VP]),
+    "ckks_rope": (ctypes.c_int, [_VP, _BP, _U32, ctypes.POINTER(_RopeShape), _VP, _VP, _VP, _U32, _BP]),
+    "ckks_cache_tables": (ctypes.c_int, [_VP, ctypes.POINTER(_RopeShape), _U32, _U32, _VP, _VP, _U32, _VP]),
+    "ckks_cache_append": (ctypes.c_int, [_VP, _BP, _BP, _U32, ctypes.POINTER(_RopeShape), _U32, _U32, _U32, _VP, _VP,
+                                         _VP, _U32, ctypes.POINTER(_Cache), _VP]),
     "ckks_profile_enable": (ctypes.c_int, [_VP, ctypes.c_int]),
     "ckks_profile_read": (ctypes.c_int, [_VP, ctypes.c_char_p, ctypes.POINTER(_DBL), ctypes.POINTER(_U64),
                                          ctypes.POINTER(_DBL), ctypes.POINTER(_DBL)]),
@@ -160,6 +176,30 @@ def _arg(t, what: str, dtype: torch.dtype, shape=None, numel: Optional[int] = No
         raise CkksError("%s: %s" % (what, e)) from None
 
 
+def rope_inv_freq(rot_dim: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                  original: int = 8192, low: float = 1.0, high: float = 4.0) -> torch.Tensor:
+    """Rotary frequencies base^(-2 k / rot_dim), k < rot_dim / 2 (float64, host), scaled for contexts `factor` times the
+    `original` length: "linear" divides each by the factor; "ntk" raises the base so that the slowest is divided by it
+    and the fastest stays; "bands" divides those with under `low` turns in the original context, keeps those with over
+    `high` and blends between."""
+    if rot_dim < 2 or rot_dim % 2:
+        raise CkksError("rope_inv_freq: a rotated part of %d features is odd or empty" % rot_dim)
+    if not (base > 0 and factor > 0 and original > 0 and 0 < low < high):
+        raise CkksError("rope_inv_freq: base, factor, original, low < high must be positive")
+    if scaling not in (None, "linear", "ntk", "bands"):
+        raise CkksError("rope_inv_freq: unknown scaling %r" % (scaling,))
+    if scaling == "ntk" and rot_dim > 2:
+        base *= factor ** (rot_dim / (rot_dim - 2))
+    f = torch.tensor(float(base), dtype=torch.float64) ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64) / rot_dim)
+    if scaling == "linear":
+        return f / factor
+    if scaling == "bands":
+        turns = original * f / (2 * math.pi)
+        keep = ((turns - low) / (high - low)).clamp(0, 1)
+        return f * (keep + (1 - keep) / factor)
+    return f
+
+
 @dataclass
 class Buf:
     """A plaintext ([1][limbs][N]) or ciphertext ([2][limbs][N]) tensor with its scale."""
@@ -203,6 +243,7 @@ class Context:
         if stream is None:
             stream = torch.cuda.current_stream()
         self._stream = stream
+        self.device = torch.cuda.current_device()
         h = ctypes.c_void_p()
         _check(L.ckks_ctx_create(ctypes.byref(prm), ctypes.c_void_p(stream.cuda_stream), ctypes.byref(h)),
                "ckks_ctx_create")
@@ -243,7 +284,8 @@ class Context:
 
     # workspace op codes (ckks_op)
     OP_ENCODE, OP_DECODE, OP_ENCRYPT, OP_DECRYPT, OP_KEYGEN, OP_RESCALE, OP_ROTATE, OP_MUL_RELIN, OP_MODUP, \
-        OP_MODDOWN, OP_LINEAR_PROJECT, OP_LINEAR_PROJECT_TM, OP_ATTN_SCORES, OP_ATTN_APPLY = range(1, 15)
+        OP_MODDOWN, OP_LINEAR_PROJECT, OP_LINEAR_PROJECT_TM, OP_ATTN_SCORES, OP_ATTN_APPLY, OP_ROPE_TABLES, OP_ROPE, \
+        OP_CACHE_APPEND = range(1, 18)
 
     def workspace_bytes(self, op: int, shape=()) -> int:
         """Device bytes one call of `op` takes from the arena or workspace, for the given shape."""
@@ -562,6 +604,183 @@ class Context:
         st = set(-d for d in range(1, tokens)) | set(d * (D - 1) for d in range(1, tokens)) | set(range(1, head_dim))
         st |= set(d * D for d in range(1, tokens)) | set(j for j in range(-head_dim + 1, tokens) if j)
         return sorted(st)
+
+    # ---------------- rotary positions and the key/value cache ----------------
+    _LAYOUTS, _PAIRINGS = {"tm": 0, "fm": 1}, {"half": 0, "interleaved": 1}
+
+    def _rope_shape(self, tokens: int, head_dim: int, rot_dim: int, layout: str, pairing: str) -> _RopeShape:
+        if layout not in self._LAYOUTS:
+            raise CkksError("layout must be 'fm' or 'tm'")
+        if pairing not in self._PAIRINGS:
+            raise CkksError("pairing must be 'half' or 'interleaved'")
+        for name, v in (("tokens", tokens), ("head_dim", head_dim), ("rot_dim", rot_dim)):
+            if not isinstance(v, int) or not 0 <= v <= self.n:
+                raise CkksError("%s: %r is not a count of at most %d" % (name, v, self.n))
+        return _RopeShape(tokens, head_dim, rot_dim, self._LAYOUTS[layout], self._PAIRINGS[pairing])
+
+    def _used(self, *tensors):
+        """Tensors handed to a call on the context's stream: of the context's device, and known to the caching allocator
+        as in use there where that is not the current stream (or their memory could be given away too early)."""
+        for t in tensors:
+            if t is not None and t.is_cuda and t.device.index != self.device:
+                raise CkksError("a tensor of device %s, the context is on device %d" % (t.device, self.device))
+        stream = self._stream
+        if stream is not None and stream != torch.cuda.current_stream(self.device):
+            for t in tensors:
+                if t is not None and t.is_cuda:
+                    t.record_stream(stream)
+
+    def _keys_of(self, keys: Dict[int, torch.Tensor]):
+        steps = sorted(keys)
+        for st in steps:
+            if not -(1 << 31) <= st < 1 << 31:
+                raise CkksError("key step %d is not a 32-bit integer" % st)
+        ks = (ctypes.c_int32 * max(1, len(steps)))(*steps)
+        kp = (ctypes.c_void_p * max(1, len(steps)))(*[self._key(keys[s], "key for step %d" % s).value for s in steps])
+        return ks, kp, len(steps)
+
+    def _cos_sin(self, cos, sin, count: int, half: int):
+        if not half or not count:
+            return None, None
+        return (_arg(cos, "cosines", torch.float64, shape=(count, half)),
+                _arg(sin, "sines", torch.float64, shape=(count, half)))
+
+    def rope_cos_sin(self, positions: torch.Tensor, inv_freq: torch.Tensor, factor: float = 1.0):
+        """(cos, sin) [count][half] of positions (int64 [count]) times inv_freq (float64 [half]), times factor."""
+        if not isinstance(positions, torch.Tensor) or positions.dim() != 1:
+            raise CkksError("positions: a 1-d tensor expected")
+        if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
+            raise CkksError("inv_freq: a 1-d tensor expected")
+        count, half = positions.numel(), inv_freq.numel()
+        pp, pf = _arg(positions, "positions", torch.int64), _arg(inv_freq, "inv_freq", torch.float64)
+        cos = torch.empty((count, half), dtype=torch.float64, device=positions.device)
+        sin = torch.empty_like(cos)
+        self._used(positions, inv_freq, cos, sin)
+        _check(self.lib.ckks_rope_cos_sin(self.h, pp, count, pf, half, float(factor), _ptr(cos), _ptr(sin)),
+               "ckks_rope_cos_sin")
+        return cos, sin
+
+    def rope_tables(self, cos: torch.Tensor, sin: torch.Tensor, tokens: int, head_dim: int, rot_dim: int, n_limbs: int,
+                    first: int = 0, layout: str = "tm", pairing: str = "half",
+                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Tables [3][n_limbs + n_p][N] of rope() for inputs of n_limbs limbs: token first + i turns by row i of cos and
+        sin ([count][rot_dim/2]), the other tokens become zero."""
+        shape = self._rope_shape(tokens, head_dim, rot_dim, layout, pairing)
+        if not isinstance(cos, torch.Tensor) or cos.dim() != 2:
+            raise CkksError("cosines: a 2-d tensor [tokens][rot_dim/2] expected")
+        count = cos.shape[0]
+        if not 0 <= first <= tokens or count > tokens - first or not 1 <= n_limbs <= self.n_q:
+            raise CkksError("rope_tables: tokens %d .. %d of %d, %d limbs of %d"
+                            % (first, first + count, tokens, n_limbs, self.n_q))
+        pc, ps = self._cos_sin(cos, sin, count, rot_dim // 2)
+        want = (3, n_limbs + self.n_p, self.n)
+        out = torch.empty(want, dtype=torch.uint64, device=cos.device) if out is None else out
+        po = _arg(out, "tables", torch.uint64, shape=want)
+        self._used(cos, sin, out)
+        _check(self.lib.ckks_rope_tables(self.h, ctypes.byref(shape), first, count, pc, ps, n_limbs, po),
+               "ckks_rope_tables")
+        return out
+
+    def rope(self, cts: Sequence[Buf], tables: torch.Tensor, tokens: int, head_dim: int, rot_dim: int,
+             keys: Dict[int, torch.Tensor], layout: str = "tm", pairing: str = "half",
+             outs: Optional[Sequence[Buf]] = None) -> List[Buf]:
+        """Rotary positions: every ciphertext turned by rope_tables()' tables, one limb fewer out."""
+        shape = self._rope_shape(tokens, head_dim, rot_dim, layout, pairing)
+        if not cts:
+            return []
+        limbs = cts[0].n_limbs
+        ib = (_Buf * len(cts))(*[c.c(self.n) for c in cts])
+        pt = _arg(tables, "tables", torch.uint64, shape=(3, limbs + self.n_p, self.n))
+        if outs is None:
+            outs = [Buf(self._empty(c.data, 2, max(1, limbs - 1)), c.scale) for c in cts]
+        if len(outs) < len(cts):
+            raise CkksError("rope: %d outputs for %d inputs" % (len(outs), len(cts)))
+        outs = list(outs[:len(cts)])
+        ob = (_Buf * len(cts))(*[o.c(self.n) for o in outs])
+        ks, kp, nk = self._keys_of(keys)
+        self._used(tables, *[c.data for c in cts], *[o.data for o in outs], *keys.values())
+        _check(self.lib.ckks_rope(self.h, ib, len(cts), ctypes.byref(shape), pt, ks, kp, nk, ob), "ckks_rope")
+        for o, b in zip(outs, ob):
+            o.scale = b.scale
+        return outs
+
+    def _cache_blocks(self, tokens: int, length: int, count: int) -> int:
+        """Pages that `count` tokens after `length` touch."""
+        if not 0 <= length < 1 << 32 or not 0 <= count <= tokens:
+            raise CkksError("cache: %d tokens after %d, at most %d at once" % (count, length, tokens))
+        return (length + count - 1) // tokens - length // tokens + 1 if count else 0
+
+    def cache_tables(self, cos: Optional[torch.Tensor], sin: Optional[torch.Tensor], tokens: int, head_dim: int,
+                     rot_dim: int, length: int, count: int, n_limbs: int, pairing: str = "half",
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Tables [pages][4][n_limbs + n_p][N] ([pages][1].. with rot_dim 0) of cache_append() for `count` tokens after
+        `length`; cos and sin [count][rot_dim/2] at the new tokens' positions."""
+        shape = self._rope_shape(tokens, head_dim, rot_dim, "tm", pairing)
+        blocks = self._cache_blocks(tokens, length, count)
+        if not 1 <= n_limbs <= self.n_q:
+            raise CkksError("cache_tables: %d limbs of %d" % (n_limbs, self.n_q))
+        pc, ps = self._cos_sin(cos, sin, count, rot_dim // 2)
+        want = (blocks, 4 if rot_dim else 1, n_limbs + self.n_p, self.n)
+        if out is None:
+            out = torch.empty(want, dtype=torch.uint64, device=torch.device("cuda", self.device))
+        po = _arg(out, "tables", torch.uint64, shape=want)
+        self._used(cos if rot_dim else None, sin if rot_dim else None, out)
+        _check(self.lib.ckks_cache_tables(self.h, ctypes.byref(shape), length, count, pc, ps, n_limbs, po),
+               "ckks_cache_tables")
+        return out
+
+    def cache_append(self, k_cts: Sequence[Buf], v_cts: Sequence[Buf], tables: torch.Tensor, tokens: int, head_dim: int,
+                     rot_dim: int, length: int, count: int, keys: Dict[int, torch.Tensor], k_pages: Sequence[Buf],
+                     v_pages: Sequence[Buf], block_table: Sequence[Sequence[int]], src: int = 0,
+                     pairing: str = "half", fork: Optional[Sequence[int]] = None) -> None:
+        """Append tokens src .. src + count - 1 of each head's key (rotated by the tables) and value ciphertext to a
+        paged cache of `length` tokens: block_table[h][b] is the page of head h's tokens b * tokens and on, in both
+        pools; fork[h] the page that head h's started page continues, if not itself."""
+        shape = self._rope_shape(tokens, head_dim, rot_dim, "tm", pairing)
+        heads = len(k_cts)
+        if len(v_cts) != heads or len(block_table) != heads or (fork is not None and len(fork) != heads):
+            raise CkksError("cache_append: %d keys, %d values, %d rows of the block table, %s forks"
+                            % (heads, len(v_cts), len(block_table), "no" if fork is None else len(fork)))
+        if len(k_pages) != len(v_pages):
+            raise CkksError("cache_append: %d key pages, %d value pages" % (len(k_pages), len(v_pages)))
+        blocks = self._cache_blocks(tokens, length, count)
+        if not 0 <= src <= tokens:
+            raise CkksError("cache_append: first token %d of %d" % (src, tokens))
+        if not heads or not count:
+            return
+        n_blocks = min(len(row) for row in block_table)
+        index = [int(p) for row in block_table for p in row[:n_blocks]]
+        if any(not 0 <= p < 1 << 32 for p in index + list(fork or ())):
+            raise CkksError("cache_append: a page index is not a 32-bit count")
+        pt = _arg(tables, "tables", torch.uint64,
+                  shape=(blocks, 4 if rot_dim else 1, k_cts[0].n_limbs + self.n_p, self.n))
+        kb, vb = ((_Buf * heads)(*[c.c(self.n) for c in x]) for x in (k_cts, v_cts))
+        n_pages = len(k_pages)
+        kp_, vp_ = ((_Buf * max(1, n_pages))(*[c.c(self.n) for c in x]) for x in (k_pages, v_pages))
+        tab = (_U32 * max(1, len(index)))(*index)
+        cache = _Cache(kp_, vp_, n_pages, tab, n_blocks)
+        fk = None if fork is None else (_U32 * heads)(*fork)
+        ks, kp, nk = self._keys_of(keys)
+        self._used(tables, *[c.data for x in (k_cts, v_cts, k_pages, v_pages) for c in x], *keys.values())
+        _check(self.lib.ckks_cache_append(self.h, kb, vb, heads, ctypes.byref(shape), src, length, count, pt, ks, kp,
+                                          nk, ctypes.byref(cache), fk), "ckks_cache_append")
+        for bufs, pages in ((kp_, k_pages), (vp_, v_pages)):
+            for b, p in zip(bufs, pages):
+                p.scale = b.scale
+
+    @staticmethod
+    def rope_steps(slots: int, tokens: int, rot_dim: int, layout: str = "tm", pairing: str = "half") -> List[int]:
+        """The rotation steps rope() needs keys for."""
+        h = (rot_dim // 2 if pairing == "half" else 1) * (tokens if layout == "fm" else 1)
+        return sorted({s for s in (h % slots, -h % slots) if s})
+
+    @staticmethod
+    def append_steps(slots: int, tokens: int, rot_dim: int, length: int, src: int = 0,
+                     pairing: str = "half") -> List[int]:
+        """The rotation steps cache_append() needs keys for."""
+        m = (length - src) % tokens * (slots // tokens)
+        h = 0 if not rot_dim else rot_dim // 2 if pairing == "half" else 1
+        return sorted({s for s in (-m % slots, (h - m) % slots, (-h - m) % slots) if s})
 
     # ---------------- measurement ----------------
     def profile(self, on: bool = True):

@@ -74,6 +74,13 @@ size_t op_workspace_bytes(const ckks_ctx *ctx, int op, const uint32_t *shape)
     case CKKS_OP_ATTN_APPLY:
         if (!shape) return SIZE_MAX;
         return attn_apply_workspace_bytes(ctx, shape[0], shape[1], shape[2], shape[3]);
+    case CKKS_OP_ROPE_TABLES: return rope_tables_workspace_bytes(ctx);
+    case CKKS_OP_ROPE:
+        if (!shape) return SIZE_MAX;
+        return rope_workspace_bytes(ctx, shape[0], shape[1]);
+    case CKKS_OP_CACHE_APPEND:
+        if (!shape) return SIZE_MAX;
+        return append_workspace_bytes(ctx, shape[0], shape[1]);
     default: return SIZE_MAX;
     }
 }

@@ -196,6 +196,11 @@ size_t proj_tm_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t tokens,
 size_t attn_scores_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t tokens, uint32_t head_dim);
 size_t attn_apply_workspace_bytes(const ckks_ctx *ctx, uint32_t Lp, uint32_t Lv, uint32_t tokens, uint32_t head_dim);
 
+// rotary positions and the cache (rope.hip)
+size_t rope_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t count);
+size_t append_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t heads);
+size_t rope_tables_workspace_bytes(const ckks_ctx *ctx);
+
 // projection helpers (project.hip): W's cyclic diagonals Wd[((jb * n_in + i) * D + k) * D + o] =
 // W[(i D + (k + o) mod D) * d_out + jb D + o]; canonical residues -> the same integers as doubles, in place
 ckks_status launch_diag_layout(ckks_ctx *ctx, double *Wd, const double *W, uint32_t D, uint32_t n_in,
