@@ -1,126 +1,21 @@
-// Rotary positions on ciphertexts and the encrypted key/value cache.
-//
-// Both are a sum of a few rotations of a ciphertext (c0, c1) at level l, each weighted by a plaintext, divided by P q_l:
-//
-//   t_j,k = sum_d sigma_gj(D_d) key_j,d,k + [k = 0] P sigma_gj(c0)     over Q_l u P (D the ModUp digits of c1)
-//   t_0,k = P c_k                                                       (a term that is not rotated)
-//   u_k   = sum_j pt_j t_j,k,            out = Rescale(ModDown(u))  (+ the page)
-//
-// The weights multiply before the division by P (they are encoded over Q_l u P), so a sum of rotations takes one ModUp
-// and one division where rotate, multiply and add take a ModDown per rotation: the double hoisting of Bossuat et al.
-// 2021.  ModDown(P x) = x exactly, so the unrotated term is what a plaintext product gives.
-//
-//   rope     cos at the slot itself, -sin and sin at the slots of its pair, half the rotated part away or next to it
+// Rotary positions on ciphertexts and the encrypted key/value cache: the tables, and the calls.  Both are weighted sums
+// of rotations (wsum.hip):
+//   rope     cos at the slot itself, -sin and sin at the slots of its pair, half the rotated part away or next to it;
 //   append   the same, every rotation lowered by the token slots that the new tokens move up, the weights zero
-//            outside the new tokens' slots of the page; values take one term with a 0/1 weight
+//            outside the new tokens' slots of the page; values take one term with a 0/1 weight.
 #include <algorithm>
 #include <cmath>
 #include <new>
 #include <vector>
 
 #include "ckks_internal.h"
-#include "ks_args.h"
+#include "ntt_core.h"
 #include "ops.h"
+#include "wsum.h"
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr uint32_t kTerms = 3;      // weighted terms of one output: the slot itself and its pair on either side
-constexpr uint32_t kCts = 16;       // ciphertexts a batch: at most two pages each, so kRotBatch outputs
-
-// One way of weighting: term j reads through the automorphism g[j] with key[j] (null: the unrotated term) and table
-// tab[j] ([ext][N]).
-struct Weights {
-    uint32_t n;
-    uint32_t g[kTerms];
-    const uint64_t *key[kTerms], *tab[kTerms];
-};
-constexpr uint32_t kWeights = 4;    // keys and values of two pages
-struct WsumArgs {
-    Weights w[kWeights];
-    const uint64_t *c[kRotBatch];    // ciphertext [2][level+1][N] of output r
-    const uint64_t *dig[kRotBatch];  // its ModUp digits [nd][ext][N]
-    uint64_t *out[kRotBatch];        // [2][level][N]
-    const uint64_t *prev[kRotBatch]; // [2][level][N] added to the output (null: nothing); may be out itself
-    uint8_t kind[kRotBatch];         // index into w
-};
-
-// u[r][k][row][n] = sum_j pt_j t_j,k on every row of Q_level u P, in exact 128-bit sums (a term sums nd + 1 products, an
-// output kTerms)
-__global__ __launch_bounds__(kThreads) void k_wsum(WsumArgs a, uint64_t *u, uint32_t nd, uint32_t ext, uint32_t L,
-                                                   uint32_t n_q, uint32_t key_rows,
-                                                   const ulonglong2 *__restrict__ pmodq,
-                                                   const ModQ *__restrict__ mods, uint32_t log_n)
-{
-    const uint32_t col = blockIdx.x * kThreads + threadIdx.x, row = blockIdx.y, r = blockIdx.z;
-    if (col >= (1u << log_n)) return;
-    const uint32_t prime = row < L ? row : n_q + (row - L);
-    const ModQ m = mods[prime];
-    const Weights &w = a.w[a.kind[r]];
-    const uint64_t pq = row < L ? pmodq[row].x : 0;
-    const uint64_t *c = a.c[r] + ((size_t)row << log_n), *dig = a.dig[r] + ((size_t)row << log_n);
-    acc128 u0{0, 0}, u1{0, 0};
-    for (uint32_t j = 0; j < w.n; j++) {
-        const uint64_t pt = w.tab[j][((size_t)row << log_n) + col];
-        acc128 t0{0, 0}, t1{0, 0};
-        if (w.key[j]) {
-            const uint32_t sc = auto_index(col, w.g[j], log_n);
-            const uint64_t *key = w.key[j] + ((size_t)prime << log_n) + col;
-            for (uint32_t d = 0; d < nd; d++) {
-                const uint64_t v = dig[((size_t)d * ext << log_n) + sc];
-                mac(t0, v, nttc::ld_stream(key + ((size_t)(2 * d) * key_rows << log_n)));
-                mac(t1, v, nttc::ld_stream(key + ((size_t)(2 * d + 1) * key_rows << log_n)));
-            }
-            if (row < L) mac(t0, c[sc], pq);
-        } else if (row < L) {
-            mac(t0, c[col], pq);
-            mac(t1, c[((size_t)L << log_n) + col], pq);
-        }
-        mac(u0, reduce128(t0, m), pt);
-        mac(u1, reduce128(t1, m), pt);
-    }
-    uint64_t *o = u + (((size_t)r * 2 * ext + row) << log_n) + col;
-    o[0] = reduce128(u0, m);
-    o[(size_t)ext << log_n] = reduce128(u1, m);
-}
-
-// v[r][k][row] = pt c_k: an output whose one term is not rotated
-__global__ __launch_bounds__(kThreads) void k_wmul(WsumArgs a, uint64_t *v, uint32_t L, const ModQ *__restrict__ mods,
-                                                   uint32_t log_n)
-{
-    const uint32_t col = blockIdx.x * kThreads + threadIdx.x, row = blockIdx.y, r = blockIdx.z;
-    if (col >= (1u << log_n)) return;
-    const ModQ m = mods[row];
-    const uint64_t pt = a.w[a.kind[r]].tab[0][((size_t)row << log_n) + col];
-    const uint64_t *c = a.c[r] + ((size_t)row << log_n) + col;
-    uint64_t *o = v + (((size_t)r * 2 * L + row) << log_n) + col;
-    o[0] = mulmod(c[0], pt, m);
-    o[(size_t)L << log_n] = mulmod(c[(size_t)L << log_n], pt, m);
-}
-
-// c1 of ciphertext i to out[i][L][N]
-struct CtList {
-    const uint64_t *c[kCts];
-};
-__global__ __launch_bounds__(kThreads) void k_gather_c1(uint64_t *out, CtList cts, uint32_t L, uint32_t log_n)
-{
-    const uint32_t col = blockIdx.x * kThreads + threadIdx.x, row = blockIdx.y, i = blockIdx.z;
-    if (col >= (1u << log_n)) return;
-    out[(((size_t)i * L + row) << log_n) + col] = cts.c[i][(((size_t)L + row) << log_n) + col];
-}
-
-// out_r = x[r] (+ prev_r), [2][l][N] each
-__global__ __launch_bounds__(kThreads) void k_emit(WsumArgs a, const uint64_t *x, uint32_t l,
-                                                   const ModQ *__restrict__ mods, uint32_t log_n)
-{
-    const uint32_t col = blockIdx.x * kThreads + threadIdx.x, row = blockIdx.y, r = blockIdx.z;
-    if (col >= (1u << log_n)) return;
-    const size_t at = ((size_t)row << log_n) + col;
-    uint64_t v = x[((size_t)r * 2 * l << log_n) + at];
-    if (a.prev[r]) v = addmod(v, a.prev[r][at], mods[row % l].q);
-    a.out[r][at] = v;
-}
-
 // cos and sin of positions[i] * inv_freq[k], times factor.  The product is taken with its rounding error e (an FMA) and
 // the angles added, so a far position's angle is as exact as a near one's.
 __global__ __launch_bounds__(kThreads) void k_cos_sin(const int64_t *positions, const double *inv_freq, uint32_t half,
@@ -184,115 +79,6 @@ LimbMap ext_map(const ckks_ctx *ctx, uint32_t L)
 
 dim3 grid_of(const ckks_ctx *ctx, uint32_t rows, uint32_t z) { return dim3((ctx->n + kThreads - 1) / kThreads, rows, z); }
 
-// words of a batch of `cts` ciphertexts and `outs` outputs at L limbs: the digits with their staging rows, then u, the
-// quotient by P, the conversion's rows (before them, the gathered c1), and the rescale's rows and result
-struct Scratch {
-    size_t dig, stage_rows, u, v, work, res, total;
-};
-Scratch scratch_of(const ckks_ctx *ctx, uint32_t L, uint32_t cts, uint32_t outs)
-{
-    const size_t N = ctx->n, ext = L + ctx->n_p, nd = n_digits(ctx, L - 1);
-    Scratch s{};
-    s.stage_rows = (size_t)cts * std::max<size_t>(ctx->alpha, L);
-    s.dig = cts * nd * ext * N + s.stage_rows * N;
-    s.u = (size_t)outs * 2 * ext * N;
-    s.v = (size_t)outs * 2 * L * N;
-    s.work = (size_t)outs * 2 * L * N;     // ModDown: 2 L rows an output; rescale: 2 (1 + (L - 1))
-    s.res = (size_t)outs * 2 * (L - 1) * N;
-    s.total = s.dig + s.u + s.v + s.work + s.res;
-    return s;
-}
-
-// One output: of ciphertext c, weighted as w[kind], to out, prev added.
-struct Job {
-    const uint64_t *c;
-    uint8_t kind;
-    uint64_t *out;
-    const uint64_t *prev;
-};
-
-bool rotated(const Weights &w)
-{
-    for (uint32_t j = 0; j < w.n; j++)
-        if (w.key[j]) return true;
-    return false;
-}
-
-// The outputs of at most kCts ciphertexts with consecutive jobs, all of rotated weights or all of unrotated ones.
-ckks_status run_batch(ckks_ctx *ctx, uint32_t L, const Weights *w, const Job *jobs, uint32_t n, bool rot, uint64_t *mem)
-{
-    const uint32_t level = L - 1, ext = L + ctx->n_p, nd = n_digits(ctx, level);
-    const size_t N = ctx->n;
-    WsumArgs a{};
-    for (uint32_t i = 0; i < kWeights; i++) a.w[i] = w[i];
-    std::vector<const uint64_t *> cts;
-    for (uint32_t r = 0; r < n; r++) {
-        if (cts.empty() || cts.back() != jobs[r].c) cts.push_back(jobs[r].c);
-        a.c[r] = jobs[r].c;
-        a.dig[r] = mem + (cts.size() - 1) * nd * ext * N;
-        a.out[r] = jobs[r].out;
-        a.prev[r] = jobs[r].prev;
-        a.kind[r] = jobs[r].kind;
-    }
-    const Scratch s = scratch_of(ctx, L, (uint32_t)cts.size(), n);
-    uint64_t *u = mem + s.dig, *v = u + s.u, *work = v + s.v, *res = work + s.work;
-    if (rot) {
-        // one batched ModUp: of ciphertexts that do not lie at one distance, the second components gathered first
-        const uint32_t n_ct = (uint32_t)cts.size();
-        size_t stride = 2 * (size_t)L * N;
-        const uint64_t *c1 = cts[0] + (size_t)L * N;
-        bool even = true;
-        for (size_t i = 1; i < cts.size(); i++) even = even && cts[i] == cts[0] + i * stride;
-        if (!even) {
-            CtList list{};
-            for (uint32_t i = 0; i < n_ct; i++) list.c[i] = cts[i];
-            prof_begin(ctx, K_ELEM, 16.0 * N * L * n_ct);
-            hipLaunchKernelGGL(k_gather_c1, grid_of(ctx, L, n_ct), dim3(kThreads), 0, ctx->stream, work, list, L, ctx->log_n);
-            prof_end(ctx, K_ELEM);
-            HIP_TRY(hipGetLastError());
-            c1 = work;
-            stride = (size_t)L * N;
-        }
-        CK_TRY(ks_modup_batch(ctx, c1, stride, n_ct, level, mem, s.stage_rows));
-        prof_begin(ctx, K_KEYIP, 8.0 * N * ext * n * (nd + 3.0));
-        hipLaunchKernelGGL(k_wsum, grid_of(ctx, ext, n), dim3(kThreads), 0, ctx->stream, a, u, nd, ext, L, ctx->n_q,
-                           ctx->n_primes(), ctx->d_pmodq, ctx->d_mod, ctx->log_n);
-        prof_end(ctx, K_KEYIP);
-        HIP_TRY(hipGetLastError());
-        CK_TRY(ks_moddown(ctx, u, 2 * n, level, nullptr, 1, nullptr, v, work));
-    } else {
-        prof_begin(ctx, K_ELEM, 8.0 * N * L * n * 5.0);
-        hipLaunchKernelGGL(k_wmul, grid_of(ctx, L, n), dim3(kThreads), 0, ctx->stream, a, v, L, ctx->d_mod, ctx->log_n);
-        prof_end(ctx, K_ELEM);
-        HIP_TRY(hipGetLastError());
-    }
-    CK_TRY(rescale_many(ctx, v, n, level, res, work));
-    prof_begin(ctx, K_ELEM, 8.0 * N * level * n * 6.0);
-    hipLaunchKernelGGL(k_emit, grid_of(ctx, 2 * level, n), dim3(kThreads), 0, ctx->stream, a, res, level, ctx->d_mod,
-                       ctx->log_n);
-    prof_end(ctx, K_ELEM);
-    HIP_TRY(hipGetLastError());
-    return CKKS_OK;
-}
-
-// every job (those of one ciphertext consecutive), in batches of kCts ciphertexts
-ckks_status run_jobs(ckks_ctx *ctx, uint32_t L, const Weights *w, const std::vector<Job> &jobs, uint64_t *mem)
-{
-    for (size_t r0 = 0; r0 < jobs.size();) {
-        const bool rot = rotated(w[jobs[r0].kind]);
-        size_t r = r0;
-        for (uint32_t cts = 0; r < jobs.size() && rotated(w[jobs[r].kind]) == rot; r++) {
-            if (r == r0 || jobs[r].c != jobs[r - 1].c) {
-                if (cts == kCts) break;
-                cts++;
-            }
-        }
-        CK_TRY(run_batch(ctx, L, w, &jobs[r0], (uint32_t)(r - r0), rot, mem));
-        r0 = r;
-    }
-    return CKKS_OK;
-}
-
 // ------------------------------------------------------------------------------------------- arguments --------------
 ckks_status check_shape(const ckks_ctx *ctx, const ckks_rope_shape *s, const char *what, bool rotary, Shape *out)
 {
@@ -317,7 +103,7 @@ ckks_status check_shape(const ckks_ctx *ctx, const ckks_rope_shape *s, const cha
 // left rotation of the pair above, in slots
 int64_t pair_step(const Shape &s) { return (int64_t)(s.interleaved ? 1 : s.rot_dim / 2) * (s.fm ? s.tokens : 1); }
 
-ckks_status check_cts(const ckks_ctx *ctx, const ckks_buf *b, uint32_t n, uint32_t L, const char *what, const char *name)
+ckks_status check_cts(const ckks_buf *b, uint32_t n, uint32_t L, const char *what, const char *name)
 {
     for (uint32_t i = 0; i < n; i++) {
         CK_REQUIRE(b[i].data && b[i].n_polys == 2, CKKS_EINVAL, "%s: %s %u is not a ciphertext", what, name, i);
@@ -353,7 +139,7 @@ ckks_status check_overlap(std::vector<Range> outs, const std::vector<Range> &ins
 }
 
 // the terms' automorphisms and keys: left rotations by base, base + h, base - h
-ckks_status find_keys(const ckks_ctx *ctx, Weights *w, uint32_t n, int64_t base, int64_t h, const int32_t *key_steps,
+ckks_status find_keys(const ckks_ctx *ctx, WsumKind *w, uint32_t n, int64_t base, int64_t h, const int32_t *key_steps,
                       const uint64_t *const *keys, uint32_t n_keys, const char *what)
 {
     const int64_t slots = ctx->n / 2;
@@ -363,6 +149,7 @@ ckks_status find_keys(const ckks_ctx *ctx, Weights *w, uint32_t n, int64_t base,
         w->g[j] = ckks_galois_elt(ctx, (int32_t)st);
         w->key[j] = nullptr;
         if (!st) continue;
+        w->rotated = 1;
         for (uint32_t r = 0; r < n_keys && !w->key[j]; r++)
             if ((((int64_t)key_steps[r] % slots) + slots) % slots == st) w->key[j] = keys[r];
         CK_REQUIRE(w->key[j], CKKS_ENOKEY, "%s: no key for step %lld (modulo %lld)", what, (long long)st, (long long)slots);
@@ -430,16 +217,14 @@ struct DeviceScope {
 size_t rope_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t count)
 {
     if (L < 2 || L > ctx->n_q || !ctx->n_p || !count) return SIZE_MAX;
-    const uint32_t c = std::min(count, kCts);
-    return scratch_of(ctx, L, c, c).total * 8;
+    return wsum_scratch_words(ctx, L, count, 1) * 8;
 }
 size_t append_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t heads)
 {
     if (L < 2 || L > ctx->n_q || !ctx->n_p || !heads) return SIZE_MAX;
-    const uint32_t c = (uint32_t)std::min<uint64_t>(2 * (uint64_t)heads, kCts);
-    return scratch_of(ctx, L, c, 2 * c).total * 8;
+    return wsum_scratch_words(ctx, L, (uint32_t)std::min<uint64_t>(2 * (uint64_t)heads, UINT32_MAX), kWsumPages) * 8;
 }
-size_t rope_tables_workspace_bytes(const ckks_ctx *ctx) { return tables_bytes(ctx, kTerms + 1); }
+size_t rope_tables_workspace_bytes(const ckks_ctx *ctx) { return tables_bytes(ctx, kWsumTerms + 1); }
 
 extern "C" {
 
@@ -478,7 +263,7 @@ ckks_status ckks_rope_tables(ckks_ctx *ctx, const ckks_rope_shape *shape, uint32
     CK_REQUIRE(!count || (cs && sn), CKKS_EINVAL, "rope_tables: null argument");
     void *w;
     CK_TRY(ctx_scratch(ctx, op_workspace_bytes(ctx, CKKS_OP_ROPE_TABLES, nullptr), &w));
-    return make_tables(ctx, s, first, count, kTerms, false, cs, sn, n_limbs, tables, w);
+    return make_tables(ctx, s, first, count, kWsumTerms, false, cs, sn, n_limbs, tables, w);
 }
 
 ckks_status ckks_cache_tables(ckks_ctx *ctx, const ckks_rope_shape *shape, uint32_t length, uint32_t count, const double *cs,
@@ -497,7 +282,7 @@ ckks_status ckks_cache_tables(ckks_ctx *ctx, const ckks_rope_shape *shape, uint3
     CK_REQUIRE(tables && (!s.rot_dim || (cs && sn)), CKKS_EINVAL, "cache_tables: null argument");
     void *w;
     CK_TRY(ctx_scratch(ctx, op_workspace_bytes(ctx, CKKS_OP_ROPE_TABLES, nullptr), &w));
-    const uint32_t off = length % s.tokens, n0 = std::min(count, s.tokens - off), n_rot = s.rot_dim ? kTerms : 0;
+    const uint32_t off = length % s.tokens, n0 = std::min(count, s.tokens - off), n_rot = s.rot_dim ? kWsumTerms : 0;
     CK_TRY(make_tables(ctx, s, off, n0, n_rot, true, cs, sn, n_limbs, tables, w));
     if (n0 == count) return CKKS_OK;
     const size_t done = (size_t)n0 * (s.rot_dim / 2), page = (size_t)(n_rot + 1) * (n_limbs + ctx->n_p) * ctx->n;
@@ -520,24 +305,24 @@ ckks_status ckks_rope(ckks_ctx *ctx, const ckks_buf *in, uint32_t count, const c
         CK_REQUIRE(ctx->n_p > 0, CKKS_EUNSUPPORTED, "rope: the context has no special primes");
         const uint32_t L = in[0].n_limbs;
         CK_REQUIRE(L >= 2 && L <= ctx->n_q, CKKS_ELEVEL, "rope: inputs need 2 to %u limbs, %u given", ctx->n_q, L);
-        CK_TRY(check_cts(ctx, in, count, L, "rope", "input"));
-        CK_TRY(check_cts(ctx, out, count, L - 1, "rope", "output"));
+        CK_TRY(check_cts(in, count, L, "rope", "input"));
+        CK_TRY(check_cts(out, count, L - 1, "rope", "output"));
         const size_t N = ctx->n, row_words = (size_t)(L + ctx->n_p) * N;
         std::vector<Range> ins(count), outs(count);
-        std::vector<Job> jobs(count);
+        std::vector<WsumCt> cts(count);
         for (uint32_t r = 0; r < count; r++) {
             ins[r] = {in[r].data, 2 * (size_t)L * N};
             outs[r] = {out[r].data, 2 * (size_t)(L - 1) * N};
-            jobs[r] = {in[r].data, 0, out[r].data, nullptr};
+            cts[r] = {in[r].data, 0, {out[r].data}, {}};
         }
         CK_TRY(check_overlap(outs, ins, "rope"));
-        Weights w[kWeights] = {};
-        CK_TRY(find_keys(ctx, &w[0], kTerms, 0, pair_step(s), key_steps, keys, n_keys, "rope"));
-        for (uint32_t j = 0; j < kTerms; j++) w[0].tab[j] = tables + j * row_words;
+        WsumKind kinds[kWsumKinds] = {};
+        CK_TRY(find_keys(ctx, &kinds[0], kWsumTerms, 0, pair_step(s), key_steps, keys, n_keys, "rope"));
+        for (uint32_t j = 0; j < kWsumTerms; j++) kinds[0].tab[0][j] = tables + j * row_words;
         const uint32_t shp[2] = {L, count};
         void *mem;
         CK_TRY(ctx_scratch(ctx, op_workspace_bytes(ctx, CKKS_OP_ROPE, shp), &mem));
-        CK_TRY(run_jobs(ctx, L, w, jobs, (uint64_t *)mem));
+        CK_TRY(wsum_run(ctx, L, 1, kinds, cts, (uint64_t *)mem));
         for (uint32_t r = 0; r < count; r++) out[r].scale = in[r].scale;
         return CKKS_OK;
     });
@@ -564,8 +349,8 @@ ckks_status ckks_cache_append(ckks_ctx *ctx, const ckks_buf *k, const ckks_buf *
         CK_REQUIRE(ctx->n_p > 0, CKKS_EUNSUPPORTED, "cache_append: the context has no special primes");
         const uint32_t L = k[0].n_limbs, T = s.tokens;
         CK_REQUIRE(L >= 2 && L <= ctx->n_q, CKKS_ELEVEL, "cache_append: inputs need 2 to %u limbs, %u given", ctx->n_q, L);
-        CK_TRY(check_cts(ctx, k, n_heads, L, "cache_append", "key"));
-        CK_TRY(check_cts(ctx, v, n_heads, L, "cache_append", "value"));
+        CK_TRY(check_cts(k, n_heads, L, "cache_append", "key"));
+        CK_TRY(check_cts(v, n_heads, L, "cache_append", "value"));
         CK_TRY(check_scales(k, n_heads, "cache_append", "key"));
         CK_TRY(check_scales(v, n_heads, "cache_append", "value"));
         const uint32_t b0 = length / T, blocks = (length + count - 1) / T - b0 + 1, off = length % T;
@@ -573,51 +358,53 @@ ckks_status ckks_cache_append(ckks_ctx *ctx, const ckks_buf *k, const ckks_buf *
                    length + count - 1, b0 + blocks - 1, cache->n_blocks);
         const size_t N = ctx->n, ctw = 2 * (size_t)(L - 1) * N;
         std::vector<Range> ins, outs;
-        std::vector<Job> jobs;
+        std::vector<WsumCt> cts;
         for (uint32_t kv = 0; kv < 2; kv++) {
             ckks_buf *pages = kv ? cache->v_pages : cache->k_pages;
             const ckks_buf *x = kv ? v : k;
+            const char *name = kv ? "value page" : "key page";
             for (uint32_t h = 0; h < n_heads; h++) {
                 ins.push_back({x[h].data, 2 * (size_t)L * N});
+                WsumCt ct{x[h].data, kv, {}, {}};
                 for (uint32_t b = 0; b < blocks; b++) {
                     const uint32_t p = cache->table[(size_t)h * cache->n_blocks + b0 + b];
-                    CK_REQUIRE(p < cache->n_pages, CKKS_EINVAL, "cache_append: head %u, block %u: page %u of %u", h, b0 + b, p,
-                               cache->n_pages);
-                    CK_TRY(check_cts(ctx, &pages[p], 1, L - 1, "cache_append", kv ? "value page" : "key page"));
-                    const uint64_t *prev = nullptr;
-                    if (b == 0 && off) {
-                        const uint32_t f = fork ? fork[h] : p;
-                        CK_REQUIRE(f < cache->n_pages, CKKS_EINVAL, "cache_append: head %u takes over page %u of %u", h, f,
-                                   cache->n_pages);
-                        CK_TRY(check_cts(ctx, &pages[f], 1, L - 1, "cache_append", kv ? "value page" : "key page"));
-                        CK_REQUIRE(pages[f].scale == x[h].scale, CKKS_ESCALE, "cache_append: page %u has scale %g, the new tokens %g",
-                                   f, pages[f].scale, x[h].scale);
-                        prev = pages[f].data;
-                        if (prev != pages[p].data) ins.push_back({prev, ctw});
-                    }
+                    CK_REQUIRE(p < cache->n_pages, CKKS_EINVAL, "cache_append: head %u, block %u: page %u of %u", h, b0 + b,
+                               p, cache->n_pages);
+                    CK_TRY(check_cts(&pages[p], 1, L - 1, "cache_append", name));
+                    ct.out[b] = pages[p].data;
                     outs.push_back({pages[p].data, ctw});
-                    jobs.push_back({x[h].data, (uint8_t)(2 * kv + b), pages[p].data, prev});
+                    if (b || !off) continue;
+                    // a started page goes on, itself or the one it is forked from
+                    const uint32_t f = fork ? fork[h] : p;
+                    CK_REQUIRE(f < cache->n_pages, CKKS_EINVAL, "cache_append: head %u takes over page %u of %u", h, f,
+                               cache->n_pages);
+                    CK_TRY(check_cts(&pages[f], 1, L - 1, "cache_append", name));
+                    CK_REQUIRE(pages[f].scale == x[h].scale, CKKS_ESCALE,
+                               "cache_append: page %u has scale %g, the new tokens %g", f, pages[f].scale, x[h].scale);
+                    ct.prev[b] = pages[f].data;
+                    if (pages[f].data != pages[p].data) ins.push_back({pages[f].data, ctw});
                 }
+                cts.push_back(ct);
             }
         }
         CK_TRY(check_overlap(outs, ins, "cache_append"));
-        // the keys' weights of either page, then the values'
+        // the keys' weights, then the values': either page's tables
         const size_t row_words = (size_t)(L + ctx->n_p) * N;
-        const uint32_t n_rot = s.rot_dim ? kTerms : 0;
+        const uint32_t n_rot = s.rot_dim ? kWsumTerms : 0;
         const int64_t base = -(int64_t)((off + T - src) % T) * s.feats;
-        Weights w[kWeights] = {};
+        WsumKind kinds[kWsumKinds] = {};
+        CK_TRY(find_keys(ctx, &kinds[0], n_rot ? n_rot : 1, base, n_rot ? pair_step(s) : 0, key_steps, keys, n_keys,
+                         "cache_append"));
+        CK_TRY(find_keys(ctx, &kinds[1], 1, base, 0, key_steps, keys, n_keys, "cache_append"));
         for (uint32_t b = 0; b < blocks; b++) {
             const uint64_t *t = tables + (size_t)b * (n_rot + 1) * row_words;
-            CK_TRY(find_keys(ctx, &w[b], n_rot ? n_rot : 1, base, n_rot ? pair_step(s) : 0, key_steps, keys, n_keys,
-                             "cache_append"));
-            for (uint32_t j = 0; j < w[b].n; j++) w[b].tab[j] = t + j * row_words;
-            CK_TRY(find_keys(ctx, &w[2 + b], 1, base, 0, key_steps, keys, n_keys, "cache_append"));
-            w[2 + b].tab[0] = t + n_rot * row_words;
+            for (uint32_t j = 0; j < kinds[0].n; j++) kinds[0].tab[b][j] = t + j * row_words;
+            kinds[1].tab[b][0] = t + n_rot * row_words;
         }
         const uint32_t shp[2] = {L, n_heads};
         void *mem;
         CK_TRY(ctx_scratch(ctx, op_workspace_bytes(ctx, CKKS_OP_CACHE_APPEND, shp), &mem));
-        CK_TRY(run_jobs(ctx, L, w, jobs, (uint64_t *)mem));
+        CK_TRY(wsum_run(ctx, L, blocks, kinds, cts, (uint64_t *)mem));
         for (uint32_t h = 0; h < n_heads; h++)
             for (uint32_t b = 0; b < blocks; b++) {
                 const uint32_t p = cache->table[(size_t)h * cache->n_blocks + b0 + b];

@@ -1,0 +1,718 @@
+// Weighted sums of rotations of a ciphertext (c0, c1) at level l, divided by P q_l:
+//
+//   t_j,k = sum_d sigma_gj(D_d) key_j,d,k + [k = 0] P sigma_gj(c0)     over Q_l u P (D the ModUp digits of c1)
+//   t_0,k = P c_k                                                       (a term that is not rotated)
+//   u_k   = sum_j pt_j t_j,k,            out = Rescale(ModDown(u))  (+ prev)
+//
+// The weights multiply before the division by P (they are encoded over Q_l u P), so a sum of rotations takes one ModUp
+// and one division where rotate, multiply and add take a ModDown per rotation: the double hoisting of Bossuat et al.
+// 2021.  ModDown(P x) = x exactly, so the unrotated term is what a plaintext product gives, and an output of that term
+// alone needs no ModUp and no P rows.
+//
+// Two passes a transform with fp64 arithmetic (N >= 2^14, every prime of the level below 2^50): after the ModUp
+//   1. k_wsum_intt8   u on the rows modulo q_l and P, with the row pass of their inverse transform;
+//   2. k_quot_col     its column pass: centred digits y_i of the P rows, U P^-1 of the q_l row;
+//   3. k_quot_col8    x_t = sum_i y_i [P / p_i]_t + P w for every target q_t, t < l, with the forward column pass
+//      (N = 2^16; k_quot_conv and a column pass elsewhere), w the centred top coefficient of the quotient by P:
+//      w = [(U - sum_i y_i [P / p_i]) P^-1]_{q_l}.  ModDown and rescale subtract Conv(y) P^-1 and then w, so
+//      out = (u - NTT(x)) (P q_l)^-1 holds for both together and the q_l row never leaves the coefficient domain;
+//   4. k_wsum_fin8    the forward row pass, u on the rows below q_l (in registers, never in HBM), the quotient, prev.
+// Elsewhere u is formed whole in exact 128-bit sums (k_wsum) and goes through the ModDown and rescale of the ring.
+#include <algorithm>
+
+#include "ks_args.h"
+#include "ops.h"
+#include "wsum.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+using A = nttc::Ar<true>;
+using nttc::kE;
+using nttc::kE8;
+
+struct Ct {
+    const uint64_t *c, *dig;   // [2][L][N]; its ModUp digits [nd][ext][N] (rotated kinds)
+    uint64_t *out[kWsumPages];
+    const uint64_t *prev[kWsumPages];
+    uint32_t kind;
+};
+struct Args {
+    WsumKind kind[kWsumKinds];
+    Ct ct[kWsumCts];
+};
+
+// The ring's sizes: L = level + 1 q-limbs, K special primes, ext = L + K, nd digits
+struct Dims {
+    uint32_t L, K, ext, nd, n_q, key_rows, log_n;
+    __device__ uint32_t prime(uint32_t row) const { return row < L ? row : n_q + (row - L); }
+};
+
+// ------------------------------------------------------------------------- in exact 128-bit sums, any ring -------------
+
+// u[z P + o][k][row][n] of ciphertext z, output o of P
+template <int P>
+__global__ __launch_bounds__(kThreads) void k_wsum(Args a, uint64_t *u, Dims d, const ulonglong2 *__restrict__ pmodq,
+                                                   const ModQ *__restrict__ mods)
+{
+    const uint32_t col = blockIdx.x * kThreads + threadIdx.x, row = blockIdx.y, z = blockIdx.z;
+    if (col >= (1u << d.log_n)) return;
+    const uint32_t prime = d.prime(row);
+    const ModQ m = mods[prime];
+    const Ct &ct = a.ct[z];
+    const WsumKind &w = a.kind[ct.kind];
+    const size_t at = ((size_t)row << d.log_n) + col;
+    const uint64_t pq = row < d.L ? pmodq[row].x : 0;
+    const uint64_t *c = ct.c + ((size_t)row << d.log_n), *dig = ct.dig + ((size_t)row << d.log_n);
+    acc128 acc[P][2] = {};
+    for (uint32_t j = 0; j < w.n; j++) {
+        acc128 t0{0, 0}, t1{0, 0};
+        if (w.key[j]) {
+            const uint32_t sc = auto_index(col, w.g[j], d.log_n);
+            const uint64_t *key = w.key[j] + ((size_t)prime << d.log_n) + col;
+            for (uint32_t i = 0; i < d.nd; i++) {
+                const uint64_t v = dig[((size_t)i * d.ext << d.log_n) + sc];
+                mac(t0, v, key[(size_t)(2 * i) * d.key_rows << d.log_n]);
+                mac(t1, v, key[(size_t)(2 * i + 1) * d.key_rows << d.log_n]);
+            }
+            if (row < d.L) mac(t0, c[sc], pq);
+        } else if (row < d.L) {
+            mac(t0, c[col], pq);
+            mac(t1, c[((size_t)d.L << d.log_n) + col], pq);
+        }
+        const uint64_t v0 = reduce128(t0, m), v1 = reduce128(t1, m);
+#pragma unroll
+        for (int o = 0; o < P; o++) {
+            const uint64_t pt = w.tab[o][j][at];
+            mac(acc[o][0], v0, pt);
+            mac(acc[o][1], v1, pt);
+        }
+    }
+#pragma unroll
+    for (int o = 0; o < P; o++) {
+        uint64_t *x = u + ((size_t)(z * P + o) * 2 * d.ext << d.log_n) + at;
+        x[0] = reduce128(acc[o][0], m);
+        x[(size_t)d.ext << d.log_n] = reduce128(acc[o][1], m);
+    }
+}
+
+// v[z P + o][k][row] = pt c_k: the outputs of unrotated kinds, with nothing to divide by P
+__global__ __launch_bounds__(kThreads) void k_wmul(Args a, uint64_t *v, Dims d, uint32_t pages,
+                                                   const ModQ *__restrict__ mods)
+{
+    const uint32_t col = blockIdx.x * kThreads + threadIdx.x, row = blockIdx.y, z = blockIdx.z;
+    if (col >= (1u << d.log_n)) return;
+    const ModQ m = mods[row];
+    const size_t at = ((size_t)row << d.log_n) + col, half = (size_t)d.L << d.log_n;
+    const Ct &ct = a.ct[z];
+    const uint64_t c0 = ct.c[at], c1 = ct.c[half + at];
+    for (uint32_t o = 0; o < pages; o++) {
+        const uint64_t pt = a.kind[ct.kind].tab[o][0][at];
+        uint64_t *x = v + (size_t)(z * pages + o) * 2 * half + at;
+        x[0] = mulmod(c0, pt, m);
+        x[half] = mulmod(c1, pt, m);
+    }
+}
+
+// out = x[z P + o] (+ prev), [2][l][N] each
+__global__ __launch_bounds__(kThreads) void k_emit(Args a, const uint64_t *x, uint32_t l, uint32_t pages, uint32_t log_n,
+                                                   const ModQ *__restrict__ mods)
+{
+    const uint32_t col = blockIdx.x * kThreads + threadIdx.x, row = blockIdx.y, z = blockIdx.z / pages,
+                   o = blockIdx.z % pages;
+    if (col >= (1u << log_n)) return;
+    const size_t at = ((size_t)row << log_n) + col;
+    uint64_t v = x[((size_t)blockIdx.z * 2 * l << log_n) + at];
+    const uint64_t *prev = a.ct[z].prev[o];
+    if (prev) v = addmod(v, prev[at], mods[row % l].q);
+    a.ct[z].out[o][at] = v;
+}
+
+// c1 of ciphertext z to out[z][L][N]
+__global__ __launch_bounds__(kThreads) void k_gather_c1(uint64_t *out, Args a, uint32_t L, uint32_t log_n)
+{
+    const uint32_t col = blockIdx.x * kThreads + threadIdx.x, row = blockIdx.y, z = blockIdx.z;
+    if (col >= (1u << log_n)) return;
+    out[(((size_t)z * L + row) << log_n) + col] = a.ct[z].c[(((size_t)L + row) << log_n) + col];
+}
+
+// ------------------------------------------------------------------------- two passes, fp64 ----------------------------
+
+// u of output o at 8 positions of one row, both components, as doubles: |u| <= 2.6 q (a term of at most 0.7 q after the
+// reduction of t, or 0.83 q unrotated).  Unrotated kinds: pt c without the factor P.
+// Every key, table and ciphertext word is read where it is used: the ciphertexts of a batch share keys and tables, which
+// neighbouring blocks find in L2.
+template <int ND, int NOUT>
+__device__ __forceinline__ void wsum8(const WsumKind &w, const Ct &ct, const Dims &d, uint32_t row, double pq, const A &ar,
+                                      const uint32_t (&pos)[kE8], double (&u)[NOUT][2][kE8])
+{
+    const uint32_t nd = ND > 0 ? (uint32_t)ND : d.nd;
+    constexpr int kUnroll = ND > 0 ? ND : 1;
+    const size_t rw = (size_t)row << d.log_n, half = (size_t)d.L << d.log_n;
+    const size_t kstride = (size_t)d.key_rows << d.log_n, dstride = (size_t)d.ext << d.log_n;
+    const bool q_row = row < d.L;
+#pragma unroll
+    for (int o = 0; o < NOUT; o++)
+#pragma unroll
+        for (int e = 0; e < kE8; e++) u[o][0][e] = u[o][1][e] = 0.0;
+    for (uint32_t j = 0; j < w.n; j++) {
+        double t0[kE8], t1[kE8];
+        if (w.key[j]) {
+            const uint32_t g = w.g[j];
+            uint32_t sc[kE8];
+#pragma unroll
+            for (int e = 0; e < kE8; e++) {
+                sc[e] = auto_index(pos[e], g, d.log_n);
+                t0[e] = t1[e] = 0.0;
+            }
+            const uint64_t *key = w.key[j] + ((size_t)d.prime(row) << d.log_n), *dig = ct.dig + rw;
+#pragma unroll kUnroll
+            for (uint32_t i = 0; i < nd; i++) {
+                const uint64_t *di = dig + i * dstride, *kb = key + 2 * i * kstride, *ka = kb + kstride;
+                uint64_t dv[kE8], bv[kE8], av[kE8];
+#pragma unroll
+                for (int e = 0; e < kE8; e++) {
+                    dv[e] = di[sc[e]];
+                    bv[e] = kb[pos[e]];
+                    av[e] = ka[pos[e]];
+                }
+#pragma unroll
+                for (int e = 0; e < kE8; e++) {
+                    const double v = A::from_u64(dv[e]);
+                    t0[e] += ar.mul(v, A::from_u64(bv[e]));
+                    t1[e] += ar.mul(v, A::from_u64(av[e]));
+                }
+                if ((i & 3) == 3) {
+#pragma unroll
+                    for (int e = 0; e < kE8; e++) {
+                        t0[e] = ar.red(t0[e]);
+                        t1[e] = ar.red(t1[e]);
+                    }
+                }
+            }
+            if (q_row) {
+#pragma unroll
+                for (int e = 0; e < kE8; e++) t0[e] += ar.mul(A::from_u64(ct.c[rw + sc[e]]), pq);
+            }
+#pragma unroll
+            for (int e = 0; e < kE8; e++) {
+                t0[e] = ar.red(t0[e]);
+                t1[e] = ar.red(t1[e]);
+            }
+        } else {
+            if (!q_row) continue;
+#pragma unroll
+            for (int e = 0; e < kE8; e++) {
+                t0[e] = A::from_u64(ct.c[rw + pos[e]]);
+                t1[e] = A::from_u64(ct.c[half + rw + pos[e]]);
+            }
+            if (w.rotated) {
+#pragma unroll
+                for (int e = 0; e < kE8; e++) {
+                    t0[e] = ar.mul(t0[e], pq);
+                    t1[e] = ar.mul(t1[e], pq);
+                }
+            }
+        }
+#pragma unroll
+        for (int o = 0; o < NOUT; o++) {
+            const uint64_t *tab = w.tab[o][j] + rw;
+#pragma unroll
+            for (int e = 0; e < kE8; e++) {
+                const double pt = A::from_u64(tab[pos[e]]);
+                u[o][0][e] += ar.mul(t0[e], pt);
+                u[o][1][e] += ar.mul(t1[e], pt);
+            }
+        }
+    }
+}
+
+// Block b of a launch over `tiles` tiles (a multiple of 8) of each of n ciphertexts: blocks go to the 8 XCDs in turn, and
+// the ciphertexts of one tile, which share its keys and tables, follow one another on one XCD.
+__device__ __forceinline__ void tile_of(uint32_t n, uint32_t &z, uint32_t &tile)
+{
+    const uint32_t xcd = blockIdx.x & 7u, rest = blockIdx.x >> 3;
+    z = rest % n;
+    tile = (rest / n) * 8 + xcd;
+}
+
+// 1. rows q_l and P (s = 0: q_l, s > 0: p_{s-1}) of u: up[z P + o][k][s], raw doubles below 2q after the row pass.  One
+// wave, two rows of 256 points, 8 positions a thread.
+template <int ND, int NOUT>
+__global__ __launch_bounds__(64) void k_wsum_intt8(Args a, uint64_t *up, Dims d, uint32_t n,
+                                                   const ulonglong2 *__restrict__ pmodq, const ModQ *__restrict__ mods,
+                                                   const double *__restrict__ itwf)
+{
+    __shared__ double tws[2][257];
+    __shared__ double tr[2][nttc::kTr8];
+    const uint32_t bpl = 1u << (d.log_n - 9);
+    uint32_t z, tile;
+    tile_of(n, z, tile);
+    const uint32_t s = tile / bpl, blk = tile % bpl, row = d.L - 1 + s, prime = d.prime(row);
+    const Ct &ct = a.ct[z];
+    const WsumKind &w = a.kind[ct.kind];
+    if (s && !w.rotated) return;
+    const A ar(mods[prime]);
+    const uint32_t sub = threadIdx.x >> 5, t = threadIdx.x & 31, h = blk * 2 + sub;
+    nttc::stage_twiddles8(tws[sub], itwf + ((size_t)prime << d.log_n), (1u << (d.log_n - 8)) + h, t, 32);
+    uint32_t pos[kE8];
+#pragma unroll
+    for (int e = 0; e < kE8; e++) pos[e] = h * 256 + nttc::u8<0>(t, e);
+    double u[NOUT][2][kE8];
+    wsum8<ND, NOUT>(w, ct, d, row, s ? 0.0 : (double)pmodq[row].x, ar, pos, u);
+    __syncthreads();
+#pragma unroll
+    for (int o = 0; o < NOUT; o++)
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            double x[kE8];
+#pragma unroll
+            for (int e = 0; e < kE8; e++) x[e] = ar.red(u[o][k][e]);
+            nttc::a_to_b8(x, tr[sub], t);
+            nttc::inv8_256(x, tws[sub], tr[sub], t, ar);
+            uint64_t *out = up + ((((size_t)(z * NOUT + o) * 2 + k) * (d.K + 1) + s) << d.log_n) + (size_t)h * 256;
+#pragma unroll
+            for (int e = 0; e < kE8; e++) nttc::st_stream(out + nttc::u8<0>(t, e), A::to_raw(x[e]));
+        }
+}
+
+// (-q/2, q/2] of |x| < q/2 + 2^49: the centred representative of an odd modulus
+__device__ __forceinline__ double centre(const A &ar, double x)
+{
+    const double v = ar.red(x), h = 0.5 * ar.q;
+    return v > h ? v - ar.q : v < -h ? v + ar.q : v;
+}
+
+// The division's constants: y_i takes N^-1 Qhat_i^-1, the q_l row N^-1 P^-1 (N^-1 alone for unrotated kinds)
+struct Quot {
+    const double *qhat_inv;    // [K]
+    const double *qhat_mod;    // [K][L] centred
+    const ulonglong2 *pinv, *qlinv, *pmodq;
+};
+
+// 2. column pass of those rows, in place: centred digits as doubles
+template <int LOGS>
+__global__ __launch_bounds__(256) void k_quot_col(uint64_t *up, Args a, Dims d, uint32_t pages, Quot qt,
+                                                  const ModQ *__restrict__ mods, const double *__restrict__ itwf)
+{
+    constexpr uint32_t TS = (1u << LOGS) / 16, kCols = 4096u >> LOGS, kBpr = 256 / kCols;
+    __shared__ double lds[LOGS > 4 ? kCols * ((1u << LOGS) + (1u << LOGS) / 16 + 1) : 1];
+    const uint32_t rr = blockIdx.x / kBpr, s = rr % (d.K + 1), p = rr / (d.K + 1);
+    const bool rot = a.kind[a.ct[p / 2 / pages].kind].rotated;
+    if (s && !rot) return;
+    const uint32_t prime = d.prime(d.L - 1 + s);
+    const A ar(mods[prime]);
+    A sc = ar;
+    if (s) sc.ninv = ar.scaled_twiddle(qt.qhat_inv[s - 1]);
+    else if (rot) sc.ninv = ar.scaled_twiddle((double)qt.pinv[d.L - 1].x);
+    const double *tw = itwf + ((size_t)prime << d.log_n);
+    const uint32_t col = threadIdx.x % kCols, t = threadIdx.x / kCols;
+    uint64_t *base = up + ((size_t)rr << d.log_n) + (blockIdx.x % kBpr) * kCols + col;
+    double x[kE];
+#pragma unroll
+    for (int k = 0; k < kE; k++) x[k] = A::from_raw(base[(size_t)(LOGS > 4 ? 16 * t + k : k) * 256]);
+    if (LOGS > 4) {
+        nttc::inv_low<LOGS, true>(x, tw, 1, t, ar);
+        nttc::transpose<LOGS, false>(x, lds, col, t);
+    }
+    nttc::inv_top<true, true>(x, tw, 1, sc);
+#pragma unroll
+    for (int k = 0; k < kE; k++) base[(size_t)(t + TS * k) * 256] = A::to_raw(centre(ar, x[k]));
+}
+
+// factor of source i in the conversion to q_l divided by P, [P / p_i P^-1]_{q_l}, centred
+__device__ __forceinline__ double top_factor(const Quot &qt, const Dims &d, int i, const A &top)
+{
+    return centre(top, top.mul(qt.qhat_mod[i * d.L + d.L - 1], (double)qt.pinv[d.L - 1].x));
+}
+
+// 3. The conversion fused with the forward column pass, N = 2^16 and at most 8 special primes (k_conv_col8's shape: block
+// (poly; 16 adjacent columns; group of t_per targets), 512 threads, 8 points of a 256-point column each, the digits of
+// the block's 4096 coefficients and w in registers for every target).  EXACT: K = 8.
+template <bool EXACT>
+__global__ __launch_bounds__(512) void k_quot_col8(uint64_t *out, const uint64_t *up, Args a, Dims d, uint32_t pages,
+                                                   uint32_t t_per, Quot qt, const ModQ *__restrict__ mods,
+                                                   const double *__restrict__ twf)
+{
+    __shared__ double s_mod[9 * kMaxPrimes];   // [K][targets], then [P]_t
+    __shared__ double s_top[8];
+    __shared__ double tws[2][256];
+    __shared__ double tr[16][nttc::kTr8], trb[16][nttc::kTr8];
+    constexpr uint32_t log_n = 16, n2 = 256;
+    const uint32_t p = blockIdx.x >> 4, blk = blockIdx.x & 15u;
+    const int K = EXACT ? 8 : (int)d.K, nt = (int)d.L - 1;
+    const int t0 = (int)(blockIdx.y * t_per), t1 = min(nt, t0 + (int)t_per);
+    if (t0 >= nt) return;
+    const bool rot = a.kind[a.ct[p / 2 / pages].kind].rotated;
+    const A top(mods[d.L - 1]);
+    if (rot) {
+        for (int k = threadIdx.x; k < K * nt; k += 512) s_mod[k] = qt.qhat_mod[(k / nt) * (int)d.L + k % nt];
+        for (int k = threadIdx.x; k < nt; k += 512) s_mod[8 * kMaxPrimes + k] = (double)qt.pmodq[k].x;
+        if (threadIdx.x < (uint32_t)K) s_top[threadIdx.x] = top_factor(qt, d, (int)threadIdx.x, top);
+    }
+    if (threadIdx.x < 255) tws[t0 & 1][threadIdx.x + 1] = twf[((size_t)t0 << log_n) + threadIdx.x + 1];
+    const uint32_t col = threadIdx.x & 15, t = threadIdx.x >> 4;
+    const uint32_t coff = blk * 16 + col;
+    const uint64_t *src = up + ((size_t)p * (d.K + 1) << log_n) + coff;
+    double y[8][kE8], w[kE8];
+#pragma unroll
+    for (int k = 0; k < kE8; k++) w[k] = A::from_raw(src[(size_t)nttc::u8<0>(t, k) * n2]);
+    if (rot) {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+#pragma unroll
+            for (int k = 0; k < kE8; k++)
+                if (EXACT || i < K) y[i][k] = A::from_raw(src[((size_t)(i + 1) << log_n) + (size_t)nttc::u8<0>(t, k) * n2]);
+    }
+    uint64_t *dst0 = out + ((size_t)p * nt << log_n) + coff;
+    __syncthreads();
+    if (rot) {
+#pragma unroll
+        for (int k = 0; k < kE8; k++) {
+            nttc::GridSum acc;
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (EXACT || i < K) acc.add(y[i][k], s_top[i]);
+            w[k] = centre(top, w[k] - top.red(acc.value(top)));
+        }
+    }
+    for (int tt = t0; tt < t1; tt++) {
+        const A ar(mods[tt]);
+        nttc::StageNext next{tws[(tt + 1) & 1], 0.0, tt + 1 < t1 && threadIdx.x < 255};
+        if (next.on) next.v = twf[((size_t)(tt + 1) << log_n) + threadIdx.x + 1];
+        double x[kE8];
+        if (rot) {
+            const double pt = s_mod[8 * kMaxPrimes + tt];
+#pragma unroll
+            for (int k = 0; k < kE8; k++) {
+                nttc::GridSum acc;
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if (EXACT || i < K) acc.add(y[i][k], s_mod[i * nt + tt]);
+                x[k] = ar.red(acc.value(ar) + ar.mul(w[k], pt));
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kE8; k++) x[k] = ar.red(w[k]);
+        }
+        nttc::fwd8_256_loop<nttc::kColMask8>(x, tws[tt & 1], tr[col], trb[col], t, ar, next);
+        uint64_t *dst = dst0 + ((size_t)tt << log_n);
+#pragma unroll
+        for (int k = 0; k < kE8; k++) nttc::st_stream(dst + (size_t)nttc::u8<2>(t, k) * n2, A::to_raw(x[k]));
+    }
+}
+
+// 3. The conversion alone (N < 2^16, or more than 8 special primes): thread = one coefficient, blockIdx.y a group of t_per
+// targets, blockIdx.z the polynomial; canonical residues out.
+template <int NS>
+__global__ __launch_bounds__(256) void k_quot_conv(uint64_t *out, const uint64_t *up, Args a, Dims d, uint32_t pages,
+                                                   uint32_t t_per, Quot qt, const ModQ *__restrict__ mods)
+{
+    __shared__ double s_mod[NS * kMaxPrimes], s_top[NS], s_p[kMaxPrimes];
+    __shared__ double2 s_tq[kMaxPrimes];
+    const uint32_t p = blockIdx.z;
+    const int K = (int)d.K, nt = (int)d.L - 1;
+    const int t0 = (int)(blockIdx.y * t_per), t1 = min(nt, t0 + (int)t_per), n = t1 - t0;
+    if (t0 >= nt) return;
+    const bool rot = a.kind[a.ct[p / 2 / pages].kind].rotated;
+    const A top(mods[d.L - 1]);
+    if (rot) {
+        for (int k = threadIdx.x; k < K * n; k += 256) s_mod[k] = qt.qhat_mod[(k / n) * (int)d.L + t0 + k % n];
+        if (threadIdx.x < (uint32_t)K) s_top[threadIdx.x] = top_factor(qt, d, (int)threadIdx.x, top);
+    }
+    for (int k = threadIdx.x; k < n; k += 256) {
+        s_tq[k] = make_double2(mods[t0 + k].qd, mods[t0 + k].qinvd);
+        s_p[k] = (double)qt.pmodq[t0 + k].x;
+    }
+    const uint32_t col = blockIdx.x * 256 + threadIdx.x;
+    const uint64_t *src = up + ((size_t)p * (d.K + 1) << d.log_n) + col;
+    double y[NS], w = A::from_raw(src[0]);
+    if (rot) {
+#pragma unroll
+        for (int i = 0; i < NS; i++) y[i] = A::from_raw(src[(size_t)(min(i, K - 1) + 1) << d.log_n]);
+    }
+    __syncthreads();
+    if (rot) {
+        nttc::GridSum acc;
+#pragma unroll
+        for (int i = 0; i < NS; i++) {
+            if (i < K) {
+                acc.add(y[i], s_top[i]);
+                if ((i & 7) == 7 && i + 1 < K) acc.fold(top);
+            }
+        }
+        w = centre(top, w - top.red(acc.value(top)));
+    }
+    uint64_t *dst = out + ((size_t)p * nt << d.log_n) + col;
+    for (int t = 0; t < n; t++) {
+        A ar;
+        ar.q = s_tq[t].x;
+        ar.qinv = s_tq[t].y;
+        double x = w;
+        if (rot) {
+            nttc::GridSum acc;
+#pragma unroll
+            for (int i = 0; i < NS; i++) {
+                if (i < K) {
+                    acc.add(y[i], s_mod[i * n + t]);
+                    if ((i & 7) == 7 && i + 1 < K) acc.fold(ar);
+                }
+            }
+            x = acc.value(ar) + ar.mul(w, s_p[t]);
+        }
+        dst[(size_t)(t0 + t) << d.log_n] = ar.to_canon(x);
+    }
+}
+
+// 4. out = (u - NTT(x)) (P q_l)^-1 (+ prev) on the rows below q_l: cw[z P + o][k][l] after the column pass.  Magnitudes in
+// units of q: column-pass rows below 4.3, transformed below 2.6, u below 2.6, products below 2.5: all below 8 q = 2^53.
+template <int ND, int NOUT>
+__global__ __launch_bounds__(64) void k_wsum_fin8(Args a, const uint64_t *__restrict__ cw, Dims d, uint32_t n, Quot qt,
+                                                  const ModQ *__restrict__ mods, const double *__restrict__ twf)
+{
+    __shared__ double tws[2][257];
+    __shared__ double tr[2][nttc::kTr8];
+    const uint32_t bpl = 1u << (d.log_n - 9), l = d.L - 1;
+    uint32_t z, tile;
+    tile_of(n, z, tile);
+    const uint32_t row = tile / bpl, blk = tile % bpl;
+    const Ct &ct = a.ct[z];
+    const WsumKind &w = a.kind[ct.kind];
+    const A ar(mods[row]);
+    const uint32_t sub = threadIdx.x >> 5, t = threadIdx.x & 31, h = blk * 2 + sub;
+    nttc::stage_twiddles8(tws[sub], twf + ((size_t)row << d.log_n), (1u << (d.log_n - 8)) + h, t, 32);
+    uint32_t pos[kE8];
+#pragma unroll
+    for (int e = 0; e < kE8; e++) pos[e] = h * 256 + nttc::u8<0>(t, e);
+    double u[NOUT][2][kE8];
+    wsum8<ND, NOUT>(w, ct, d, row, (double)qt.pmodq[row].x, ar, pos, u);
+    // (P q_l)^-1, or q_l^-1 where u has no factor P, canonical
+    double f = (double)qt.qlinv[row].x;
+    if (w.rotated) {
+        f = centre(ar, ar.mul(f, (double)qt.pinv[row].x));
+        f = f < 0.0 ? f + ar.q : f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int o = 0; o < NOUT; o++) {
+        const uint64_t *prev = ct.prev[o];
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const uint64_t *src = cw + ((((size_t)(z * NOUT + o) * 2 + k) * l + row) << d.log_n) + (size_t)h * 256;
+            const size_t at = ((size_t)(k * l + row) << d.log_n) + (size_t)h * 256;
+            double x[kE8];
+#pragma unroll
+            for (int e = 0; e < kE8; e++) x[e] = A::from_raw(nttc::ld_stream(src + nttc::u8<0>(t, e)));
+            nttc::fwd8_256<nttc::kRowMask8>(x, tws[sub], tr[sub], t, ar);
+            nttc::b_to_a8(x, tr[sub], t);
+#pragma unroll
+            for (int e = 0; e < kE8; e++) {
+                double r = ar.mul(u[o][k][e] - x[e], f);
+                if (prev) r += A::from_u64(prev[at + nttc::u8<0>(t, e)]);
+                nttc::st_stream(ct.out[o] + at + nttc::u8<0>(t, e), ar.to_canon(r));
+            }
+        }
+    }
+}
+
+dim3 grid_of(const ckks_ctx *ctx, uint32_t rows, uint32_t z) { return dim3((ctx->n + kThreads - 1) / kThreads, rows, z); }
+
+// the two-pass fp64 kernels run
+bool two_pass(const ckks_ctx *ctx, uint32_t level)
+{
+    return ctx->log_n >= 14 && f64_switch(ctx, level);
+}
+
+// Words of a batch.  The digits, with the staging rows of the ModUps that take any; then, two passes: the rows q_l and P of
+// u and the converted rows; elsewhere u, the quotient by P, the conversion's rows (before them, the gathered c1) and
+// the rescale's result.
+struct Scratch {
+    size_t dig, stage_rows, u, v, work, res, total;
+};
+Scratch scratch_of(const ckks_ctx *ctx, uint32_t L, uint32_t cts, uint32_t pages)
+{
+    const size_t N = ctx->n, K = ctx->n_p, ext = L + K, nd = n_digits(ctx, L - 1), outs = (size_t)cts * pages;
+    Scratch s{};
+    s.stage_rows = (size_t)cts * std::max<size_t>(ctx->alpha, L);
+    s.dig = cts * nd * ext * N + s.stage_rows * N;
+    s.u = outs * 2 * ext * N;
+    s.v = outs * 2 * L * N;
+    s.work = std::max(outs * 2, (size_t)cts) * L * N;
+    s.res = outs * 2 * (L - 1) * N;
+    s.total = s.dig + s.u + s.v + s.work + s.res;
+    return s;
+}
+
+Dims dims_of(const ckks_ctx *ctx, uint32_t L)
+{
+    return Dims{L, ctx->n_p, L + ctx->n_p, n_digits(ctx, L - 1), ctx->n_q, ctx->n_primes(), ctx->log_n};
+}
+
+// the digits of the first n_rot ciphertexts; c1 of ciphertexts that do not lie at one distance is gathered to `work` first
+ckks_status modup_cts(ckks_ctx *ctx, uint32_t L, const Args &a, uint32_t n_rot, uint64_t *dig, size_t stage_rows,
+                      uint64_t *work)
+{
+    const size_t N = ctx->n;
+    size_t stride = 2 * (size_t)L * N;
+    const uint64_t *c1 = a.ct[0].c + (size_t)L * N;
+    bool even = true;
+    for (uint32_t i = 1; i < n_rot; i++) even = even && a.ct[i].c == a.ct[0].c + i * stride;
+    if (!even) {
+        prof_begin(ctx, K_ELEM, 16.0 * N * L * n_rot);
+        hipLaunchKernelGGL(k_gather_c1, grid_of(ctx, L, n_rot), dim3(kThreads), 0, ctx->stream, work, a, L, ctx->log_n);
+        prof_end(ctx, K_ELEM);
+        HIP_TRY(hipGetLastError());
+        c1 = work;
+        stride = (size_t)L * N;
+    }
+    return ks_modup_batch(ctx, c1, stride, n_rot, L - 1, dig, stage_rows);
+}
+
+#define CK_ND(nd, GO)                                                                                                  do {                                                                                                                   switch (nd) {                                                                                                      case 1: GO(1); break;                                                                                              case 2: GO(2); break;                                                                                              case 3: GO(3); break;                                                                                              case 4: GO(4); break;                                                                                              default: GO(0); break;                                                                                             }                                                                                                              } while (0)
+
+// steps 1 to 4 for n ciphertexts whose digits are formed
+ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pages, const Dims &d, uint64_t *up,
+                          uint64_t *cw)
+{
+    const size_t N = ctx->n;
+    const uint32_t level = d.L - 1, bpl = 1u << (d.log_n - 9), polys = 2 * n * pages;
+    const ConvDev *cd;
+    CK_TRY(ctx_conv(ctx, (int)level, -1, &cd));
+    const Quot qt{cd->d_qhat_inv_f, cd->d_qhat_mod_f, ctx->d_pinv, ctx->d_qlinv + (size_t)level * ctx->n_q, ctx->d_pmodq};
+    // products of a row position: the digits' and the weights'
+    const double prods = 2.0 * 2 * d.nd + 2.0 * 3 * pages;
+    const double rows1 = (double)n * (d.K + 1) * N;
+    prof_begin(ctx, K_KEYIP, 8.0 * rows1 * (d.nd + 2.0 * pages), rows1 * (prods * 7.0 + 2 * pages * 4 * kOpsButterflyF64));
+#define CK_GO(ND)                                                                                                      do {                                                                                                                   const dim3 grid((d.K + 1) * bpl * n);                                                                              if (pages == 1)                                                                                                        hipLaunchKernelGGL((k_wsum_intt8<ND, 1>), grid, dim3(64), 0, ctx->stream, a, up, d, n, ctx->d_pmodq,                                    ctx->d_mod, ctx->d_itwf);                                                                   else                                                                                                                   hipLaunchKernelGGL((k_wsum_intt8<ND, 2>), grid, dim3(64), 0, ctx->stream, a, up, d, n, ctx->d_pmodq,                                    ctx->d_mod, ctx->d_itwf);                                                               } while (0)
+    CK_ND(d.nd, CK_GO);
+#undef CK_GO
+    prof_end(ctx, K_KEYIP);
+    HIP_TRY(hipGetLastError());
+
+    const double rows2 = (double)polys * (d.K + 1) * N;
+    prof_begin(ctx, K_NTT_INV_COL, 16.0 * rows2, rows2 * kOpsButterflyF64 * (d.log_n - 8) / 2);
+#define CK_COL(S)                                                                                                      hipLaunchKernelGGL(k_quot_col<S>, dim3(polys * (d.K + 1) * (256 / (4096u >> S))), dim3(256), 0, ctx->stream, up, a,                        d, pages, qt, ctx->d_mod, ctx->d_itwf)
+    switch (d.log_n) {
+    case 12: CK_COL(4); break;
+    case 13: CK_COL(5); break;
+    case 14: CK_COL(6); break;
+    case 15: CK_COL(7); break;
+    default: CK_COL(8); break;
+    }
+#undef CK_COL
+    prof_end(ctx, K_NTT_INV_COL);
+    HIP_TRY(hipGetLastError());
+
+    const bool fused = d.log_n == 16 && d.K <= 8;
+    prof_begin(ctx, K_CONV, 8.0 * N * polys * (d.K + 1.0 + level),
+               (double)N * polys * level * (d.K * 4.0 + 14.0 + (fused ? kOpsButterflyF64 * 4 : 0.0)));
+    if (fused) {
+        // one block a CU; fewer blocks than CUs: the targets split over blockIdx.y
+        const uint32_t blocks = polys * 16, groups = std::min(level, std::max(1u, 256u / blocks));
+        const uint32_t t_per = (level + groups - 1) / groups;
+        const dim3 grid(blocks, (level + t_per - 1) / t_per);
+        if (d.K == 8)
+            hipLaunchKernelGGL(k_quot_col8<true>, grid, dim3(512), 0, ctx->stream, cw, up, a, d, pages, t_per, qt, ctx->d_mod,
+                               ctx->d_twf);
+        else
+            hipLaunchKernelGGL(k_quot_col8<false>, grid, dim3(512), 0, ctx->stream, cw, up, a, d, pages, t_per, qt,
+                               ctx->d_mod, ctx->d_twf);
+    } else {
+        // groups of targets until the grid has 2048 blocks of four waves
+        const uint32_t blocks = polys * (ctx->n / 256), groups = std::min(level, std::max(1u, 2048u / blocks));
+        const uint32_t t_per = (level + groups - 1) / groups;
+        const dim3 grid(ctx->n / 256, (level + t_per - 1) / t_per, polys);
+        if (d.K <= 8)
+            hipLaunchKernelGGL(k_quot_conv<8>, grid, dim3(256), 0, ctx->stream, cw, up, a, d, pages, t_per, qt, ctx->d_mod);
+        else
+            hipLaunchKernelGGL(k_quot_conv<16>, grid, dim3(256), 0, ctx->stream, cw, up, a, d, pages, t_per, qt, ctx->d_mod);
+    }
+    prof_end(ctx, K_CONV);
+    HIP_TRY(hipGetLastError());
+    if (!fused) CK_TRY(launch_ntt_fwd_first_pass(ctx, cw, polys, level, limb_range(0, level)));
+
+    const double rows4 = (double)n * level * N;
+    prof_begin(ctx, K_MODDOWN, 8.0 * rows4 * (d.nd + 2.0 + 4.0 * pages),
+               rows4 * (prods * 7.0 + 2 * pages * (4 * kOpsButterflyF64 + 14.0)));
+#define CK_GO(ND)                                                                                                      do {                                                                                                                   const dim3 grid(level * bpl * n);                                                                                  if (pages == 1)                                                                                                        hipLaunchKernelGGL((k_wsum_fin8<ND, 1>), grid, dim3(64), 0, ctx->stream, a, cw, d, n, qt, ctx->d_mod,                                   ctx->d_twf);                                                                                else                                                                                                                   hipLaunchKernelGGL((k_wsum_fin8<ND, 2>), grid, dim3(64), 0, ctx->stream, a, cw, d, n, qt, ctx->d_mod,                                   ctx->d_twf);                                                                            } while (0)
+    CK_ND(d.nd, CK_GO);
+#undef CK_GO
+    prof_end(ctx, K_MODDOWN);
+    HIP_TRY(hipGetLastError());
+    return CKKS_OK;
+}
+
+// n ciphertexts, all of rotated kinds or all of unrotated ones, in exact 128-bit sums
+ckks_status exact_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pages, const Dims &d, bool rot, const Scratch &s,
+                       uint64_t *mem)
+{
+    const size_t N = ctx->n;
+    const uint32_t level = d.L - 1, outs = n * pages;
+    uint64_t *u = mem + s.dig, *v = u + s.u, *work = v + s.v, *res = work + s.work;
+    if (rot) {
+        prof_begin(ctx, K_KEYIP, 8.0 * N * d.ext * n * (d.nd + 1.0 + 2.0 * pages));
+        if (pages == 1)
+            hipLaunchKernelGGL(k_wsum<1>, grid_of(ctx, d.ext, n), dim3(kThreads), 0, ctx->stream, a, u, d, ctx->d_pmodq,
+                               ctx->d_mod);
+        else
+            hipLaunchKernelGGL(k_wsum<2>, grid_of(ctx, d.ext, n), dim3(kThreads), 0, ctx->stream, a, u, d, ctx->d_pmodq,
+                               ctx->d_mod);
+        prof_end(ctx, K_KEYIP);
+        HIP_TRY(hipGetLastError());
+        CK_TRY(ks_moddown(ctx, u, 2 * outs, level, nullptr, 1, nullptr, v, work));
+    } else {
+        prof_begin(ctx, K_ELEM, 8.0 * N * d.L * n * (2.0 + 2.0 * pages));
+        hipLaunchKernelGGL(k_wmul, grid_of(ctx, d.L, n), dim3(kThreads), 0, ctx->stream, a, v, d, pages, ctx->d_mod);
+        prof_end(ctx, K_ELEM);
+        HIP_TRY(hipGetLastError());
+    }
+    CK_TRY(rescale_many(ctx, v, outs, level, res, work));
+    prof_begin(ctx, K_ELEM, 8.0 * N * level * outs * 6.0);
+    hipLaunchKernelGGL(k_emit, grid_of(ctx, 2 * level, outs), dim3(kThreads), 0, ctx->stream, a, res, level, pages,
+                       ctx->log_n, ctx->d_mod);
+    prof_end(ctx, K_ELEM);
+    HIP_TRY(hipGetLastError());
+    return CKKS_OK;
+}
+
+}  // namespace
+
+size_t wsum_scratch_words(const ckks_ctx *ctx, uint32_t L, uint32_t cts, uint32_t pages)
+{
+    return scratch_of(ctx, L, std::min(cts, kWsumCts), pages).total;
+}
+
+ckks_status wsum_run(ckks_ctx *ctx, uint32_t L, uint32_t pages, const WsumKind *kinds, const std::vector<WsumCt> &cts,
+                     uint64_t *mem)
+{
+    const Dims d = dims_of(ctx, L);
+    const bool fast = two_pass(ctx, L - 1);
+    for (size_t r0 = 0; r0 < cts.size();) {
+        // a batch: rotated and unrotated ciphertexts together where the kernels take both
+        Args a{};
+        for (uint32_t i = 0; i < kWsumKinds; i++) a.kind[i] = kinds[i];
+        const bool first = kinds[cts[r0].kind].rotated;
+        uint32_t n = 0, n_rot = 0;
+        for (; n < kWsumCts && r0 + n < cts.size(); n++) {
+            const WsumCt &c = cts[r0 + n];
+            const bool rot = kinds[c.kind].rotated;
+            if (!fast && rot != first) break;
+            Ct &x = a.ct[n];
+            x.c = c.c;
+            x.kind = c.kind;
+            if (rot) x.dig = mem + (size_t)n_rot++ * d.nd * d.ext * ctx->n;
+            for (uint32_t o = 0; o < pages; o++) {
+                x.out[o] = c.out[o];
+                x.prev[o] = c.prev[o];
+            }
+        }
+        const Scratch s = scratch_of(ctx, L, n, pages);
+        if (n_rot) CK_TRY(modup_cts(ctx, L, a, n_rot, mem, s.stage_rows, mem + s.dig + s.u + s.v));
+        if (fast)
+            CK_TRY(two_pass_sums(ctx, a, n, pages, d, mem + s.dig, mem + s.dig + s.u));
+        else
+            CK_TRY(exact_sums(ctx, a, n, pages, d, first, s, mem));
+        r0 += n;
+    }
+    return CKKS_OK;
+}
