@@ -943,7 +943,7 @@ ckks_status ks_modup_batch(ckks_ctx *ctx, const uint64_t *c1, size_t in_stride, 
     const uint32_t K = ctx->n_p, ext = level + 1 + K, nd = n_digits(ctx, level), alpha = ctx->alpha;
     const size_t N = ctx->n, dig_ct = (size_t)nd * ext * N;
     const size_t cstride = count == 1 ? 0 : in_stride;
-    if (f64_switch(ctx, level)) return up_modup(ctx, c1, cstride, count, level, digits);
+    if (f64_switch(ctx, level)) return up_modup(ctx, PolySrc{c1, cstride, {}}, count, level, digits);
     // A few ciphertexts leave each digit's transforms of its converted rows too small to fill the chip: then one
     // forward transform runs over all ext rows of every digit (each digit's own rows are transformed along and
     // overwritten with their NTT-domain values afterwards): 2 launches in place of 2 nd.  With more ciphertexts

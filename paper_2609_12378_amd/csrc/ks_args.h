@@ -6,6 +6,15 @@
 
 constexpr int kRotBatch = 32;  // rotations per batched launch
 
+// The polynomials a ModUp reads: polynomial r at base + r stride, or (base null) at list[r].
+constexpr int kPolyList = 16;
+struct PolySrc {
+    const uint64_t *base;
+    size_t stride;
+    const uint64_t *list[kPolyList];
+    __device__ const uint64_t *at(uint32_t r) const { return base ? base + r * stride : list[r]; }
+};
+
 // the NTT-domain position that sigma_g moves to position j: 2 brev(j') + 1 = (2 brev(j) + 1) g mod 2N
 __device__ __forceinline__ uint32_t auto_index(uint32_t j, uint32_t g, uint32_t log_n)
 {

@@ -14,7 +14,7 @@
 #include <algorithm>
 
 #include "ckks_internal.h"
-#include "ntt_core.h"
+#include "ks_args.h"
 #include "ops.h"
 
 namespace {
@@ -44,9 +44,9 @@ struct Blocks {
     __device__ size_t at(uint32_t r, uint32_t l) const { return ((size_t)(r * nd + l / alpha) * ext + l) << log_n; }
 };
 
-// 1. rows of 256 points, 8 per block of 128 threads: inverse row pass of limb l of c1 + r stride to its row
-__global__ __launch_bounds__(128) void k_up_row(uint64_t *dst, const uint64_t *__restrict__ c1, size_t stride, Blocks bl,
-                                                const ModQ *__restrict__ mods, const double *__restrict__ itwf)
+// 1. rows of 256 points, 8 per block of 128 threads: inverse row pass of limb l of polynomial r to its row
+__global__ __launch_bounds__(128) void k_up_row(uint64_t *dst, PolySrc c1, Blocks bl, const ModQ *__restrict__ mods,
+                                                const double *__restrict__ itwf)
 {
     __shared__ double lds[8 * 273];
     const uint32_t n1 = 1u << (bl.log_n - 8), per = n1 / 8;
@@ -54,7 +54,7 @@ __global__ __launch_bounds__(128) void k_up_row(uint64_t *dst, const uint64_t *_
     const uint32_t sub = threadIdx.x >> 4, t = threadIdx.x & 15u, h = (blockIdx.x % per) * 8 + sub;
     const A ar(mods[l]);
     const double *tw = itwf + ((size_t)l << bl.log_n);
-    const uint64_t *in = c1 + r * stride + ((size_t)l << bl.log_n) + (size_t)h * 256;
+    const uint64_t *in = c1.at(r) + ((size_t)l << bl.log_n) + (size_t)h * 256;
     uint64_t *out = dst + bl.at(r, l) + (size_t)h * 256;
     double x[kE];
 #pragma unroll
@@ -142,20 +142,27 @@ __global__ __launch_bounds__(256) void k_up_conv(uint64_t *out, const uint64_t *
 // sub-transforms on them (nttc::fwd8_256_loop with the column pass's lazy-reduction mask) and writes the rows as raw
 // doubles, the inter-pass form the row passes read.  The converted rows thus cross HBM once instead of three times.
 // Target t + 1's twiddles (Psi[1..255]) are staged into the idle half of a double-buffered table while target t is
-// transformed.  EXACT: every block has 8 sources.  32 rotations at 24 limbs: 600 us with a reduced product per term and
+// transformed.  NS: the block's sources.  32 rotations at 24 limbs: 600 us with a reduced product per term and
 // the digits formed here, 550 us with the one quotient, 505 us from ready digits; with 212 registers it runs two
 // waves a SIMD.  Blocks of 8 columns (256 threads, two independent blocks a CU) measured the same within 1% on every
 // call, so the two barriers per target are not what bounds it: the fp64 pipes at their sustained clock are.
-template <bool EXACT>
-__global__ __launch_bounds__(512) void k_conv_col8(uint64_t *out, const uint64_t *in, Blocks bl, uint32_t t_per,
-                                                   const ModQ *__restrict__ mods, const double *__restrict__ twf)
+struct ConvLds {
+    double mod[8 * kMaxPrimes];
+    double tws[2][256];
+    double tr[16][nttc::kTr8], trb[16][nttc::kTr8];
+};
+template <int NS>
+__device__ __forceinline__ void conv_col8(uint64_t *out, const uint64_t *in, const Blocks &bl, uint32_t t_per,
+                                          const ModQ *__restrict__ mods, const double *__restrict__ twf, ConvLds &lds)
 {
-    __shared__ double s_mod[8 * kMaxPrimes];
-    __shared__ double tws[2][256];
-    __shared__ double tr[16][nttc::kTr8], trb[16][nttc::kTr8];
     constexpr uint32_t log_n = 16, n2 = 256;
+    double *s_mod = lds.mod;
+    auto &tws = lds.tws;
+    auto &tr = lds.tr;
+    auto &trb = lds.trb;
     const uint32_t r = blockIdx.x >> 4, blk = blockIdx.x & 15u, j = blockIdx.z, lo = bl.lo(j);
-    const int ns = EXACT ? 8 : (int)(bl.hi(j) - lo), nt = (int)bl.targets(j);
+    constexpr int ns = NS;
+    const int nt = (int)bl.targets(j);
     const int t0 = (int)(blockIdx.y * t_per), t1 = min(nt, t0 + (int)t_per);
     if (t0 >= nt) return;
     for (int k = threadIdx.x; k < ns * nt; k += 512) s_mod[k] = bl.mod[j][k];
@@ -164,12 +171,11 @@ __global__ __launch_bounds__(512) void k_conv_col8(uint64_t *out, const uint64_t
     const uint32_t col = threadIdx.x & 15, t = threadIdx.x >> 4;
     const uint32_t coff = blk * 16 + col;
     const uint64_t *src = in + bl.at(r, lo) + coff;
-    double y[8][kE8];
+    double y[NS][kE8];
 #pragma unroll
-    for (int i = 0; i < 8; i++)
+    for (int i = 0; i < NS; i++)
 #pragma unroll
-        for (int k = 0; k < kE8; k++)
-            if (EXACT || i < ns) y[i][k] = A::from_raw(src[((size_t)i << log_n) + (size_t)nttc::u8<0>(t, k) * n2]);
+        for (int k = 0; k < kE8; k++) y[i][k] = A::from_raw(src[((size_t)i << log_n) + (size_t)nttc::u8<0>(t, k) * n2]);
     uint64_t *dst0 = out + ((size_t)(r * bl.nd + j) * bl.out_rows << log_n) + coff;
     __syncthreads();
     for (int tt = t0; tt < t1; tt++) {
@@ -182,14 +188,36 @@ __global__ __launch_bounds__(512) void k_conv_col8(uint64_t *out, const uint64_t
         for (int k = 0; k < kE8; k++) {
             nttc::GridSum acc;
 #pragma unroll
-            for (int i = 0; i < 8; i++)
-                if (EXACT || i < ns) acc.add(y[i][k], s_mod[i * nt + tt]);
+            for (int i = 0; i < NS; i++) acc.add(y[i][k], s_mod[i * nt + tt]);
             x[k] = ar.red(acc.value(ar));
         }
         nttc::fwd8_256_loop<nttc::kColMask8>(x, tws[tt & 1], tr[col], trb[col], t, ar, next);
         uint64_t *dst = dst0 + ((size_t)row << log_n);
 #pragma unroll
         for (int k = 0; k < kE8; k++) nttc::st_stream(dst + (size_t)nttc::u8<2>(t, k) * n2, A::to_raw(x[k]));
+    }
+}
+
+// the block's number of sources at compile time: FULL when every block of the launch has 8
+template <bool FULL>
+__global__ __launch_bounds__(512) void k_conv_col8(uint64_t *out, const uint64_t *in, Blocks bl, uint32_t t_per,
+                                                   const ModQ *__restrict__ mods, const double *__restrict__ twf)
+{
+    __shared__ ConvLds lds;
+    const uint32_t j = blockIdx.z;
+    if constexpr (FULL) {
+        conv_col8<8>(out, in, bl, t_per, mods, twf, lds);
+    } else {
+        switch (bl.hi(j) - bl.lo(j)) {
+        case 1: conv_col8<1>(out, in, bl, t_per, mods, twf, lds); break;
+        case 2: conv_col8<2>(out, in, bl, t_per, mods, twf, lds); break;
+        case 3: conv_col8<3>(out, in, bl, t_per, mods, twf, lds); break;
+        case 4: conv_col8<4>(out, in, bl, t_per, mods, twf, lds); break;
+        case 5: conv_col8<5>(out, in, bl, t_per, mods, twf, lds); break;
+        case 6: conv_col8<6>(out, in, bl, t_per, mods, twf, lds); break;
+        case 7: conv_col8<7>(out, in, bl, t_per, mods, twf, lds); break;
+        default: conv_col8<8>(out, in, bl, t_per, mods, twf, lds); break;
+        }
     }
 }
 
@@ -226,12 +254,11 @@ __global__ __launch_bounds__(256) void k_up_fcol(uint64_t *data, Blocks bl, cons
     for (int k = 0; k < kE; k++) base[(size_t)(LOGS > 4 ? 16 * t + k : k) * 256] = A::to_raw(x[k]);
 }
 
-// 4. forward row pass, canonical out; a digit's own rows take the polynomial's.  Input below 4.3 q: stages 0, 2, 4, 6
+// 4. forward row pass, canonical out; a digit's own rows take the polynomial's (own_rows) or are left as they are.  Input below 4.3 q: stages 0, 2, 4, 6
 // reducing keep every value below 7 q.
 constexpr unsigned kUpRowMask = 0x55;
-__global__ __launch_bounds__(128) void k_up_frow(uint64_t *data, const uint64_t *__restrict__ c1, size_t stride,
-                                                 Blocks bl, const ModQ *__restrict__ mods,
-                                                 const double *__restrict__ twf)
+__global__ __launch_bounds__(128) void k_up_frow(uint64_t *data, PolySrc c1, Blocks bl, bool own_rows,
+                                                 const ModQ *__restrict__ mods, const double *__restrict__ twf)
 {
     __shared__ double lds[8 * 273];
     const uint32_t n1 = 1u << (bl.log_n - 8), per = n1 / 8;
@@ -239,7 +266,8 @@ __global__ __launch_bounds__(128) void k_up_frow(uint64_t *data, const uint64_t 
     const uint32_t sub = threadIdx.x >> 4, t = threadIdx.x & 15u, h = (blockIdx.x % per) * 8 + sub;
     uint64_t *base = data + ((size_t)rr << bl.log_n) + (size_t)h * 256;
     if (row >= bl.lo(j) && row < bl.hi(j)) {
-        const uint64_t *in = c1 + r * stride + ((size_t)row << bl.log_n) + (size_t)h * 256;
+        if (!own_rows) return;
+        const uint64_t *in = c1.at(r) + ((size_t)row << bl.log_n) + (size_t)h * 256;
         uint64_t v[kE];
 #pragma unroll
         for (int k = 0; k < kE; k++) v[k] = in[t + 16 * k];
@@ -343,7 +371,7 @@ bool f64_level_ok(const ckks_ctx *ctx, uint32_t level)
     return true;
 }
 
-ckks_status up_modup(ckks_ctx *ctx, const uint64_t *c1, size_t stride, uint32_t count, uint32_t level, uint64_t *digits)
+ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t level, uint64_t *digits, bool own_rows)
 {
     Blocks bl{};
     bl.nd = n_digits(ctx, level);
@@ -366,7 +394,7 @@ ckks_status up_modup(ckks_ctx *ctx, const uint64_t *c1, size_t stride, uint32_t 
     const uint32_t per = 1u << (ctx->log_n - 11);  // blocks of eight 256-point rows
     const double res = (double)count * bl.L * ctx->n;
     prof_begin(ctx, K_NTT_INV_ROW, 16.0 * res, res * kOpsButterflyF64 * 4);
-    hipLaunchKernelGGL(k_up_row, dim3(count * bl.L * per), dim3(128), 0, ctx->stream, digits, c1, stride, bl, ctx->d_mod,
+    hipLaunchKernelGGL(k_up_row, dim3(count * bl.L * per), dim3(128), 0, ctx->stream, digits, c1, bl, ctx->d_mod,
                        ctx->d_itwf);
     prof_end(ctx, K_NTT_INV_ROW);
     HIP_TRY(hipGetLastError());
@@ -390,7 +418,7 @@ ckks_status up_modup(ckks_ctx *ctx, const uint64_t *c1, size_t stride, uint32_t 
         HIP_TRY(hipGetLastError());
     }
     prof_begin(ctx, K_NTT_FWD_ROW, 16.0 * rows * ctx->n, (double)rows * ctx->n * kOpsButterflyF64 * 4);
-    hipLaunchKernelGGL(k_up_frow, dim3(rows * per), dim3(128), 0, ctx->stream, digits, c1, stride, bl, ctx->d_mod,
+    hipLaunchKernelGGL(k_up_frow, dim3(rows * per), dim3(128), 0, ctx->stream, digits, c1, bl, own_rows, ctx->d_mod,
                        ctx->d_twf);
     prof_end(ctx, K_NTT_FWD_ROW);
     HIP_TRY(hipGetLastError());

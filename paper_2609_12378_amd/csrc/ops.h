@@ -105,9 +105,11 @@ inline bool f64_switch(const ckks_ctx *ctx, uint32_t level)
 {
     return !ctx->int_only && level < ctx->f64_level.size() && ctx->f64_level[level];
 }
-// ModUp of `count` polynomials at c1 + r stride into digits [count][nd][level+1+n_p][N]; needs no other memory
-ckks_status up_modup(ckks_ctx *ctx, const uint64_t *c1, size_t stride, uint32_t count, uint32_t level,
-                     uint64_t *digits);
+// ModUp of `count` polynomials into digits [count][nd][level+1+n_p][N]; needs no other memory.  Without own_rows a
+// digit's own rows, which hold the polynomial's, are left unwritten.
+struct PolySrc;
+ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t level, uint64_t *digits,
+                     bool own_rows = true);
 // up: [polys][n_p][N] rows modulo P after the row pass of their inverse transform (raw doubles below 2q): finishes it,
 // converts to the level's q limbs and runs the first forward pass into cw ([polys][level+1][N] raw doubles)
 ckks_status up_moddown(ckks_ctx *ctx, uint64_t *up, uint32_t polys, uint32_t level, uint64_t *cw);

@@ -44,7 +44,7 @@ struct Args {
 
 // The ring's sizes: L = level + 1 q-limbs, K special primes, ext = L + K, nd digits
 struct Dims {
-    uint32_t L, K, ext, nd, n_q, key_rows, log_n;
+    uint32_t L, K, ext, nd, alpha, n_q, key_rows, log_n;
     __device__ uint32_t prime(uint32_t row) const { return row < L ? row : n_q + (row - L); }
 };
 
@@ -140,8 +140,8 @@ __global__ __launch_bounds__(kThreads) void k_gather_c1(uint64_t *out, Args a, u
 
 // u of output o at 8 positions of one row, both components, as doubles: |u| <= 2.6 q (a term of at most 0.7 q after the
 // reduction of t, or 0.83 q unrotated).  Unrotated kinds: pt c without the factor P.
-// Every key, table and ciphertext word is read where it is used: the ciphertexts of a batch share keys and tables, which
-// neighbouring blocks find in L2.
+// A digit's own rows are the ciphertext's (the ModUp leaves them out).  Every key, table and ciphertext word is read
+// where it is used: the ciphertexts of a batch share keys and tables, which neighbouring blocks find in L2.
 template <int ND, int NOUT>
 __device__ __forceinline__ void wsum8(const WsumKind &w, const Ct &ct, const Dims &d, uint32_t row, double pq, const A &ar,
                                       const uint32_t (&pos)[kE8], double (&u)[NOUT][2][kE8])
@@ -166,9 +166,10 @@ __device__ __forceinline__ void wsum8(const WsumKind &w, const Ct &ct, const Dim
                 t0[e] = t1[e] = 0.0;
             }
             const uint64_t *key = w.key[j] + ((size_t)d.prime(row) << d.log_n), *dig = ct.dig + rw;
+            const uint32_t own = q_row ? row / d.alpha : ~0u;
 #pragma unroll kUnroll
             for (uint32_t i = 0; i < nd; i++) {
-                const uint64_t *di = dig + i * dstride, *kb = key + 2 * i * kstride, *ka = kb + kstride;
+                const uint64_t *di = i == own ? ct.c + half + rw : dig + i * dstride, *kb = key + 2 * i * kstride, *ka = kb + kstride;
                 uint64_t dv[kE8], bv[kE8], av[kE8];
 #pragma unroll
                 for (int e = 0; e < kE8; e++) {
@@ -330,7 +331,7 @@ __device__ __forceinline__ double top_factor(const Quot &qt, const Dims &d, int 
 // (poly; 16 adjacent columns; group of t_per targets), 512 threads, 8 points of a 256-point column each, the digits of
 // the block's 4096 coefficients and w in registers for every target).  EXACT: K = 8.
 template <bool EXACT>
-__global__ __launch_bounds__(512) void k_quot_col8(uint64_t *out, const uint64_t *up, Args a, Dims d, uint32_t pages,
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_quot_col8(uint64_t *out, const uint64_t *up, Args a, Dims d, uint32_t pages,
                                                    uint32_t t_per, Quot qt, const ModQ *__restrict__ mods,
                                                    const double *__restrict__ twf)
 {
@@ -383,14 +384,16 @@ __global__ __launch_bounds__(512) void k_quot_col8(uint64_t *out, const uint64_t
         double x[kE8];
         if (rot) {
             const double pt = s_mod[8 * kMaxPrimes + tt];
+            nttc::GridSum acc[kE8];
 #pragma unroll
-            for (int k = 0; k < kE8; k++) {
-                nttc::GridSum acc;
+            for (int i = 0; i < 8; i++)
+                if (EXACT || i < K) {
+                    const double m = s_mod[i * nt + tt];
 #pragma unroll
-                for (int i = 0; i < 8; i++)
-                    if (EXACT || i < K) acc.add(y[i][k], s_mod[i * nt + tt]);
-                x[k] = ar.red(acc.value(ar) + ar.mul(w[k], pt));
-            }
+                    for (int k = 0; k < kE8; k++) acc[k].add(y[i][k], m);
+                }
+#pragma unroll
+            for (int k = 0; k < kE8; k++) x[k] = ar.red(acc[k].value(ar) + ar.mul(w[k], pt));
         } else {
 #pragma unroll
             for (int k = 0; k < kE8; k++) x[k] = ar.red(w[k]);
@@ -545,16 +548,23 @@ Scratch scratch_of(const ckks_ctx *ctx, uint32_t L, uint32_t cts, uint32_t pages
 
 Dims dims_of(const ckks_ctx *ctx, uint32_t L)
 {
-    return Dims{L, ctx->n_p, L + ctx->n_p, n_digits(ctx, L - 1), ctx->n_q, ctx->n_primes(), ctx->log_n};
+    return Dims{L, ctx->n_p, L + ctx->n_p, n_digits(ctx, L - 1), ctx->alpha, ctx->n_q, ctx->n_primes(), ctx->log_n};
 }
 
-// the digits of the first n_rot ciphertexts; c1 of ciphertexts that do not lie at one distance is gathered to `work` first
-ckks_status modup_cts(ckks_ctx *ctx, uint32_t L, const Args &a, uint32_t n_rot, uint64_t *dig, size_t stage_rows,
-                      uint64_t *work)
+// the digits of the first n_rot ciphertexts; for the ModUps that take polynomials at one distance only, c1 of ciphertexts
+// that lie elsewhere is gathered to `work` first
+ckks_status modup_cts(ckks_ctx *ctx, uint32_t L, const Args &a, uint32_t n_rot, bool fast, uint64_t *dig,
+                      size_t stage_rows, uint64_t *work)
 {
     const size_t N = ctx->n;
     size_t stride = 2 * (size_t)L * N;
     const uint64_t *c1 = a.ct[0].c + (size_t)L * N;
+    if (fast) {
+        static_assert(kWsumCts <= (uint32_t)kPolyList, "a batch's polynomials fit the list");
+        PolySrc src{};
+        for (uint32_t i = 0; i < n_rot; i++) src.list[i] = a.ct[i].c + (size_t)L * N;
+        return up_modup(ctx, src, n_rot, L - 1, dig, false);
+    }
     bool even = true;
     for (uint32_t i = 1; i < n_rot; i++) even = even && a.ct[i].c == a.ct[0].c + i * stride;
     if (!even) {
@@ -707,7 +717,7 @@ ckks_status wsum_run(ckks_ctx *ctx, uint32_t L, uint32_t pages, const WsumKind *
             }
         }
         const Scratch s = scratch_of(ctx, L, n, pages);
-        if (n_rot) CK_TRY(modup_cts(ctx, L, a, n_rot, mem, s.stage_rows, mem + s.dig + s.u + s.v));
+        if (n_rot) CK_TRY(modup_cts(ctx, L, a, n_rot, fast, mem, s.stage_rows, mem + s.dig + s.u + s.v));
         if (fast)
             CK_TRY(two_pass_sums(ctx, a, n, pages, d, mem + s.dig, mem + s.dig + s.u));
         else
