@@ -138,14 +138,70 @@ __global__ __launch_bounds__(kThreads) void k_gather_c1(uint64_t *out, Args a, u
 
 // ------------------------------------------------------------------------- two passes, fp64 ----------------------------
 
-// u of output o at 8 positions of one row, both components, as doubles: |u| <= 2.6 q (a term of at most 0.7 q after the
-// reduction of t, or 0.83 q unrotated).  Unrotated kinds: pt c without the factor P.
-// A digit's own rows are the ciphertext's (the ModUp leaves them out).  Every key, table and ciphertext word is read
-// where it is used: the ciphertexts of a batch share keys and tables, which neighbouring blocks find in L2.
+// sum_i a_i w_i mod q of at most 4 products of canonical residues under one quotient (nttc::GridSum with twice its grid:
+// u = 2^51, so |sum| < 4 2^100 = 2^51 u, and lo is at most 4 2^50 = 2^52).  value(): |x| <= q/2 + 1.
+struct ProductSum {
+    static constexpr double kGrid = 0x1.8p+103;   // 1.5 2^52 u
+    double hi, lo;
+    __device__ ProductSum() : hi(kGrid), lo(0.0) {}
+    __device__ void add(double a, double w)
+    {
+        const double t = fma(a, w, hi);
+        const double h = t - hi;
+        lo += fma(a, w, -h);
+        hi = t;
+    }
+    __device__ double value(const A &ar) const
+    {
+        const double h = hi - kGrid;
+        return ar.red(fma(-rint(h * ar.qinv), ar.q, h) + lo);
+    }
+    __device__ void fold(const A &ar)
+    {
+        lo = value(ar);
+        hi = kGrid;
+    }
+};
+
+// Two adjacent words, read and written in one 16-byte access (rows are 8-byte aligned): the vector memory units take a
+// wave's 64 addresses at the same rate whatever their width, and at 8 bytes they, not HBM, bounded these kernels.
+struct __attribute__((aligned(8))) Pair {
+    uint64_t x, y;
+};
+__device__ __forceinline__ Pair ld2(const uint64_t *p) { return *(const Pair *)p; }
+
+// The positions of a thread in a row, in the layout the transforms end in and inverse ones start from (nttc::u8<2>): at,
+// at + 1, at + 2, at + 3 and the same 128 further, at a multiple of four.  sigma_g reads position j at j' with
+// 2 brev(j') + 1 = (2 brev(j) + 1) g mod 2N.  Bit 0 of j is the top bit of 2 brev(j) + 1 modulo 2N, which an odd g leaves in
+// place up to a carry from below: the partner j + 1 of an even j is read at j' ^ 1, so a pair is one access too.
+struct Positions {
+    uint32_t at, log_n;
+    __device__ uint32_t pos(int e) const { return at + ((uint32_t)(e >> 2) << 7) + (uint32_t)(e & 3); }
+    __device__ uint32_t start(uint32_t g) const { return (2u * (__brev(at) >> (32 - log_n)) + 1u) * g; }
+    // j' of pos(e), e even; kg = start(g).  Bit 7 of the position adds 2^(log_n - 7) g to k g, bit 1 adds N/2 g.
+    __device__ uint32_t source(uint32_t kg, uint32_t g, int e) const
+    {
+        const uint32_t dk = ((uint32_t)(e >> 2) << (log_n - 7)) + ((uint32_t)(e & 2) << (log_n - 2));
+        return (__brev(kg + dk * g) >> (31 - log_n)) & ((1u << log_n) - 1);
+    }
+};
+// the words of sigma_g(p) at an even position and the next, j' = source of the even one
+__device__ __forceinline__ Pair ld2_auto(const uint64_t *p, uint32_t src)
+{
+    const Pair v = ld2(p + (src & ~1u));
+    return src & 1u ? Pair{v.y, v.x} : v;
+}
+
+// u of output o at the 8 positions of a thread, both components, as doubles: |u| <= 2.6 q (a term of at most 0.7 q after
+// the reduction of t, or 0.83 q unrotated).  Unrotated kinds: pt c without the factor P.  A digit's own rows are the
+// ciphertext's (the ModUp leaves them out).  Every key, table and ciphertext word is read where it is used: the
+// ciphertexts of a batch share keys and tables, which neighbouring blocks find in L2.  Four positions at a time: the
+// words and sums of all eight would leave a SIMD two waves instead of three.
 template <int ND, int NOUT>
 __device__ __forceinline__ void wsum8(const WsumKind &w, const Ct &ct, const Dims &d, uint32_t row, double pq, const A &ar,
-                                      const uint32_t (&pos)[kE8], double (&u)[NOUT][2][kE8])
+                                      const Positions &ps, double (&u)[NOUT][2][kE8])
 {
+    constexpr int kC = 4;
     const uint32_t nd = ND > 0 ? (uint32_t)ND : d.nd;
     constexpr int kUnroll = ND > 0 ? ND : 1;
     const size_t rw = (size_t)row << d.log_n, half = (size_t)d.L << d.log_n;
@@ -156,73 +212,89 @@ __device__ __forceinline__ void wsum8(const WsumKind &w, const Ct &ct, const Dim
 #pragma unroll
         for (int e = 0; e < kE8; e++) u[o][0][e] = u[o][1][e] = 0.0;
     for (uint32_t j = 0; j < w.n; j++) {
-        double t0[kE8], t1[kE8];
-        if (w.key[j]) {
-            const uint32_t g = w.g[j];
-            uint32_t sc[kE8];
+        const uint32_t g = w.g[j], kg = ps.start(g);
+        const uint64_t *wk = w.key[j];
+        if (!wk && !q_row) continue;
+        const uint64_t *key = wk + ((size_t)d.prime(row) << d.log_n), *dig = ct.dig + rw;
+        const uint32_t own = q_row ? row / d.alpha : ~0u;
 #pragma unroll
-            for (int e = 0; e < kE8; e++) {
-                sc[e] = auto_index(pos[e], g, d.log_n);
-                t0[e] = t1[e] = 0.0;
-            }
-            const uint64_t *key = w.key[j] + ((size_t)d.prime(row) << d.log_n), *dig = ct.dig + rw;
-            const uint32_t own = q_row ? row / d.alpha : ~0u;
+        for (int e0 = 0; e0 < kE8; e0 += kC) {
+            double t0[kC], t1[kC];
+            if (wk) {
+                ProductSum s0[kC], s1[kC];
+                uint32_t sc[2];
+#pragma unroll
+                for (int e = 0; e < 2; e++) sc[e] = ps.source(kg, g, e0 + 2 * e);
+                if (q_row) {
+#pragma unroll
+                    for (int e = 0; e < 2; e++) {
+                        const Pair v = ld2_auto(ct.c + rw, sc[e]);
+                        s0[2 * e].add(A::from_u64(v.x), pq);
+                        s0[2 * e + 1].add(A::from_u64(v.y), pq);
+                    }
+                }
 #pragma unroll kUnroll
-            for (uint32_t i = 0; i < nd; i++) {
-                const uint64_t *di = i == own ? ct.c + half + rw : dig + i * dstride, *kb = key + 2 * i * kstride, *ka = kb + kstride;
-                uint64_t dv[kE8], bv[kE8], av[kE8];
+                for (uint32_t i = 0; i < nd; i++) {
+                    const uint64_t *di = i == own ? ct.c + half + rw : dig + i * dstride, *kb = key + 2 * i * kstride,
+                                   *ka = kb + kstride;
+                    Pair dv[2], bv[2], av[2];
 #pragma unroll
-                for (int e = 0; e < kE8; e++) {
-                    dv[e] = di[sc[e]];
-                    bv[e] = kb[pos[e]];
-                    av[e] = ka[pos[e]];
+                    for (int e = 0; e < 2; e++) {
+                        dv[e] = ld2_auto(di, sc[e]);
+                        bv[e] = ld2(kb + ps.pos(e0 + 2 * e));
+                        av[e] = ld2(ka + ps.pos(e0 + 2 * e));
+                    }
+                    if (i && i % 3 == 0) {   // s0 holds the c0 term and three products
+#pragma unroll
+                        for (int e = 0; e < kC; e++) {
+                            s0[e].fold(ar);
+                            s1[e].fold(ar);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 2; e++) {
+                        const double v0 = A::from_u64(dv[e].x), v1 = A::from_u64(dv[e].y);
+                        s0[2 * e].add(v0, A::from_u64(bv[e].x));
+                        s1[2 * e].add(v0, A::from_u64(av[e].x));
+                        s0[2 * e + 1].add(v1, A::from_u64(bv[e].y));
+                        s1[2 * e + 1].add(v1, A::from_u64(av[e].y));
+                    }
                 }
 #pragma unroll
-                for (int e = 0; e < kE8; e++) {
-                    const double v = A::from_u64(dv[e]);
-                    t0[e] += ar.mul(v, A::from_u64(bv[e]));
-                    t1[e] += ar.mul(v, A::from_u64(av[e]));
+                for (int e = 0; e < kC; e++) {
+                    t0[e] = s0[e].value(ar);
+                    t1[e] = s1[e].value(ar);
                 }
-                if ((i & 3) == 3) {
+            } else {
 #pragma unroll
-                    for (int e = 0; e < kE8; e++) {
-                        t0[e] = ar.red(t0[e]);
-                        t1[e] = ar.red(t1[e]);
+                for (int e = 0; e < 2; e++) {
+                    const uint64_t *c = ct.c + rw + ps.pos(e0 + 2 * e);
+                    const Pair v0 = ld2(c), v1 = ld2(c + half);
+                    t0[2 * e] = A::from_u64(v0.x);
+                    t0[2 * e + 1] = A::from_u64(v0.y);
+                    t1[2 * e] = A::from_u64(v1.x);
+                    t1[2 * e + 1] = A::from_u64(v1.y);
+                }
+                if (w.rotated) {
+#pragma unroll
+                    for (int e = 0; e < kC; e++) {
+                        t0[e] = ar.mul(t0[e], pq);
+                        t1[e] = ar.mul(t1[e], pq);
                     }
                 }
             }
-            if (q_row) {
 #pragma unroll
-                for (int e = 0; e < kE8; e++) t0[e] += ar.mul(A::from_u64(ct.c[rw + sc[e]]), pq);
-            }
+            for (int o = 0; o < NOUT; o++) {
+                const uint64_t *tab = w.tab[o][j] + rw;
 #pragma unroll
-            for (int e = 0; e < kE8; e++) {
-                t0[e] = ar.red(t0[e]);
-                t1[e] = ar.red(t1[e]);
-            }
-        } else {
-            if (!q_row) continue;
-#pragma unroll
-            for (int e = 0; e < kE8; e++) {
-                t0[e] = A::from_u64(ct.c[rw + pos[e]]);
-                t1[e] = A::from_u64(ct.c[half + rw + pos[e]]);
-            }
-            if (w.rotated) {
-#pragma unroll
-                for (int e = 0; e < kE8; e++) {
-                    t0[e] = ar.mul(t0[e], pq);
-                    t1[e] = ar.mul(t1[e], pq);
+                for (int e = 0; e < kC; e += 2) {
+                    const Pair v = ld2(tab + ps.pos(e0 + e));
+                    const double p0 = A::from_u64(v.x), p1 = A::from_u64(v.y);
+                    u[o][0][e0 + e] += ar.mul(t0[e], p0);
+                    u[o][1][e0 + e] += ar.mul(t1[e], p0);
+                    u[o][0][e0 + e + 1] += ar.mul(t0[e + 1], p1);
+                    u[o][1][e0 + e + 1] += ar.mul(t1[e + 1], p1);
                 }
-            }
-        }
-#pragma unroll
-        for (int o = 0; o < NOUT; o++) {
-            const uint64_t *tab = w.tab[o][j] + rw;
-#pragma unroll
-            for (int e = 0; e < kE8; e++) {
-                const double pt = A::from_u64(tab[pos[e]]);
-                u[o][0][e] += ar.mul(t0[e], pt);
-                u[o][1][e] += ar.mul(t1[e], pt);
             }
         }
     }
@@ -256,11 +328,9 @@ __global__ __launch_bounds__(64) void k_wsum_intt8(Args a, uint64_t *up, Dims d,
     const A ar(mods[prime]);
     const uint32_t sub = threadIdx.x >> 5, t = threadIdx.x & 31, h = blk * 2 + sub;
     nttc::stage_twiddles8(tws[sub], itwf + ((size_t)prime << d.log_n), (1u << (d.log_n - 8)) + h, t, 32);
-    uint32_t pos[kE8];
-#pragma unroll
-    for (int e = 0; e < kE8; e++) pos[e] = h * 256 + nttc::u8<0>(t, e);
+    const Positions ps{h * 256 + 4 * t, d.log_n};
     double u[NOUT][2][kE8];
-    wsum8<ND, NOUT>(w, ct, d, row, s ? 0.0 : (double)pmodq[row].x, ar, pos, u);
+    wsum8<ND, NOUT>(w, ct, d, row, s ? 0.0 : (double)pmodq[row].x, ar, ps, u);
     __syncthreads();
 #pragma unroll
     for (int o = 0; o < NOUT; o++)
@@ -269,12 +339,24 @@ __global__ __launch_bounds__(64) void k_wsum_intt8(Args a, uint64_t *up, Dims d,
             double x[kE8];
 #pragma unroll
             for (int e = 0; e < kE8; e++) x[e] = ar.red(u[o][k][e]);
-            nttc::a_to_b8(x, tr[sub], t);
             nttc::inv8_256(x, tws[sub], tr[sub], t, ar);
             uint64_t *out = up + ((((size_t)(z * NOUT + o) * 2 + k) * (d.K + 1) + s) << d.log_n) + (size_t)h * 256;
 #pragma unroll
             for (int e = 0; e < kE8; e++) nttc::st_stream(out + nttc::u8<0>(t, e), A::to_raw(x[e]));
         }
+}
+
+// the integer r in [0, 2^52) as a word: the mantissa of 2^52 + r
+__device__ __forceinline__ uint64_t to_word(double r)
+{
+    return (uint64_t)__double_as_longlong(r + 4503599627370496.0) & 0x000FFFFFFFFFFFFFull;
+}
+
+// x f mod q, canonical: |x| < 8 q reduced to q/2 + 1, times f in [0, q) at most 0.7 q
+__device__ __forceinline__ uint64_t quotient(const A &ar, double x, double f)
+{
+    const double r = ar.mul(ar.red(x), f);
+    return to_word(r < 0.0 ? r + ar.q : r);
 }
 
 // (-q/2, q/2] of |x| < q/2 + 2^49: the centred representative of an odd modulus
@@ -482,13 +564,12 @@ __global__ __launch_bounds__(64) void k_wsum_fin8(Args a, const uint64_t *__rest
     const Ct &ct = a.ct[z];
     const WsumKind &w = a.kind[ct.kind];
     const A ar(mods[row]);
+    const uint64_t q = mods[row].q;
     const uint32_t sub = threadIdx.x >> 5, t = threadIdx.x & 31, h = blk * 2 + sub;
     nttc::stage_twiddles8(tws[sub], twf + ((size_t)row << d.log_n), (1u << (d.log_n - 8)) + h, t, 32);
-    uint32_t pos[kE8];
-#pragma unroll
-    for (int e = 0; e < kE8; e++) pos[e] = h * 256 + nttc::u8<0>(t, e);
+    const Positions ps{h * 256 + 4 * t, d.log_n};
     double u[NOUT][2][kE8];
-    wsum8<ND, NOUT>(w, ct, d, row, (double)qt.pmodq[row].x, ar, pos, u);
+    wsum8<ND, NOUT>(w, ct, d, row, (double)qt.pmodq[row].x, ar, ps, u);
     // (P q_l)^-1, or q_l^-1 where u has no factor P, canonical
     double f = (double)qt.qlinv[row].x;
     if (w.rotated) {
@@ -499,20 +580,34 @@ __global__ __launch_bounds__(64) void k_wsum_fin8(Args a, const uint64_t *__rest
 #pragma unroll
     for (int o = 0; o < NOUT; o++) {
         const uint64_t *prev = ct.prev[o];
+        // both components' rows and page words asked for together, before the first transform
+        double x[2][kE8];
+        Pair pv[2][kE8 / 2];
 #pragma unroll
         for (int k = 0; k < 2; k++) {
             const uint64_t *src = cw + ((((size_t)(z * NOUT + o) * 2 + k) * l + row) << d.log_n) + (size_t)h * 256;
-            const size_t at = ((size_t)(k * l + row) << d.log_n) + (size_t)h * 256;
-            double x[kE8];
 #pragma unroll
-            for (int e = 0; e < kE8; e++) x[e] = A::from_raw(nttc::ld_stream(src + nttc::u8<0>(t, e)));
-            nttc::fwd8_256<nttc::kRowMask8>(x, tws[sub], tr[sub], t, ar);
-            nttc::b_to_a8(x, tr[sub], t);
+            for (int e = 0; e < kE8; e++) x[k][e] = A::from_raw(nttc::ld_stream(src + nttc::u8<0>(t, e)));
+        }
+        if (prev) {
 #pragma unroll
-            for (int e = 0; e < kE8; e++) {
-                double r = ar.mul(u[o][k][e] - x[e], f);
-                if (prev) r += A::from_u64(prev[at + nttc::u8<0>(t, e)]);
-                nttc::st_stream(ct.out[o] + at + nttc::u8<0>(t, e), ar.to_canon(r));
+            for (int k = 0; k < 2; k++)
+#pragma unroll
+                for (int e = 0; e < kE8; e += 2) pv[k][e / 2] = ld2(prev + ((size_t)(k * l + row) << d.log_n) + ps.pos(e));
+        }
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            nttc::fwd8_256<nttc::kRowMask8>(x[k], tws[sub], tr[sub], t, ar);
+#pragma unroll
+            for (int e = 0; e < kE8; e += 2) {
+                Pair v;
+                v.x = quotient(ar, u[o][k][e] - x[k][e], f);
+                v.y = quotient(ar, u[o][k][e + 1] - x[k][e + 1], f);
+                if (prev) {
+                    v.x = addmod(v.x, pv[k][e / 2].x, q);
+                    v.y = addmod(v.y, pv[k][e / 2].y, q);
+                }
+                *(Pair *)(ct.out[o] + ((size_t)(k * l + row) << d.log_n) + ps.pos(e)) = v;
             }
         }
     }
