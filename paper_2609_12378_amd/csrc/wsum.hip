@@ -163,28 +163,48 @@ struct ProductSum {
     }
 };
 
-// Two adjacent words, read and written in one 16-byte access (rows are 8-byte aligned): the vector memory units take a
-// wave's 64 addresses at the same rate whatever their width, and at 8 bytes they, not HBM, bounded these kernels.
+// Two adjacent words, read and written in one 16-byte access (rows are 8-byte aligned).
 struct __attribute__((aligned(8))) Pair {
     uint64_t x, y;
 };
 __device__ __forceinline__ Pair ld2(const uint64_t *p) { return *(const Pair *)p; }
 
-// The positions of a thread in a row, in the layout the transforms end in and inverse ones start from (nttc::u8<2>): at,
-// at + 1, at + 2, at + 3 and the same 128 further, at a multiple of four.  sigma_g reads position j at j' with
-// 2 brev(j') + 1 = (2 brev(j) + 1) g mod 2N.  Bit 0 of j is the top bit of 2 brev(j) + 1 modulo 2N, which an odd g leaves in
-// place up to a carry from below: the partner j + 1 of an even j is read at j' ^ 1, so a pair is one access too.
+// The positions of thread t (of 32) in a row of 256: pairs (j, j + 1) at j = 64 c + 4 (t & 15) + 2 (t >> 4), register
+// e = 2 c + (0 or 1), so a wave's access is whole cache lines.  It is the layout that the transforms end in and inverse
+// ones start from (nttc::u8<2>, four adjacent positions a thread) with position bits 1 and 6 exchanged, which is one
+// swap of lane rows a register (swap_1_6).
+// sigma_g reads position j at j' with 2 brev(j') + 1 = (2 brev(j) + 1) g mod 2N.  Bit 0 of j is the top bit of
+// 2 brev(j) + 1 modulo 2N, which an odd g leaves in place up to a carry from below: the partner j + 1 of an even j is read
+// at j' ^ 1; likewise the sources of 64 aligned positions are 64 aligned positions.  So gathers are pairs and whole lines
+// as well.  (8-byte accesses, or 16-byte ones at a stride of 32, cost twice the requests to L2, which bound the kernels.)
 struct Positions {
     uint32_t at, log_n;
-    __device__ uint32_t pos(int e) const { return at + ((uint32_t)(e >> 2) << 7) + (uint32_t)(e & 3); }
+    __device__ Positions(uint32_t h, uint32_t t, uint32_t log_n_)
+        : at(h * 256 + 4 * (t & 15u) + 2 * (t >> 4)), log_n(log_n_)
+    {
+    }
+    __device__ uint32_t pos(int e) const { return at + 64u * (uint32_t)(e >> 1) + (uint32_t)(e & 1); }
     __device__ uint32_t start(uint32_t g) const { return (2u * (__brev(at) >> (32 - log_n)) + 1u) * g; }
-    // j' of pos(e), e even; kg = start(g).  Bit 7 of the position adds 2^(log_n - 7) g to k g, bit 1 adds N/2 g.
+    // j' of pos(e), e even; kg = start(g).  Bits 6 and 7 of the position add 2^(log_n - 6) g and 2^(log_n - 7) g.
     __device__ uint32_t source(uint32_t kg, uint32_t g, int e) const
     {
-        const uint32_t dk = ((uint32_t)(e >> 2) << (log_n - 7)) + ((uint32_t)(e & 2) << (log_n - 2));
+        const uint32_t dk = ((uint32_t)(e & 2) << (log_n - 7)) + ((uint32_t)(e >> 2) << (log_n - 7));
         return (__brev(kg + dk * g) >> (31 - log_n)) & ((1u << log_n) - 1);
     }
 };
+// u8<2> to Positions' order and back: registers e and e | 2 (e & 2 clear) exchange lane rows 1 (of e) and 0 (of e | 2)
+__device__ __forceinline__ void swap_1_6(double (&x)[kE8])
+{
+#pragma unroll
+    for (int e = 0; e < kE8; e++) {
+        if (e & 2) continue;
+        const uint64_t a = A::to_raw(x[e]), b = A::to_raw(x[e | 2]);
+        const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)a, (uint32_t)b, false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(a >> 32), (uint32_t)(b >> 32), false, false);
+        x[e] = A::from_raw((uint64_t)hi[0] << 32 | lo[0]);
+        x[e | 2] = A::from_raw((uint64_t)hi[1] << 32 | lo[1]);
+    }
+}
 // the words of sigma_g(p) at an even position and the next, j' = source of the even one
 __device__ __forceinline__ Pair ld2_auto(const uint64_t *p, uint32_t src)
 {
@@ -192,110 +212,153 @@ __device__ __forceinline__ Pair ld2_auto(const uint64_t *p, uint32_t src)
     return src & 1u ? Pair{v.y, v.x} : v;
 }
 
+// The words that one term takes at PU pairs of positions: c0 (and, unrotated, c1 in place of the first digit), the digits,
+// the key's two halves, the tables.  A unit's loads are issued together, and the next unit's before its own sums: what
+// bounds these kernels otherwise is the wait on one row after another with two or three waves a SIMD.
+template <int ND, int PU, int NOUT>
+struct Unit {
+    Pair c[PU], dig[ND][PU], b[ND][PU], a[ND][PU], tab[NOUT][PU];
+    uint32_t flip[PU];
+};
+constexpr int unit_pairs(int) { return 1; }
+
+struct NoTail {
+    __device__ void operator()() const {}
+};
+
 // u of output o at the 8 positions of a thread, both components, as doubles: |u| <= 2.6 q (a term of at most 0.7 q after
 // the reduction of t, or 0.83 q unrotated).  Unrotated kinds: pt c without the factor P.  A digit's own rows are the
-// ciphertext's (the ModUp leaves them out).  Every key, table and ciphertext word is read where it is used: the
-// ciphertexts of a batch share keys and tables, which neighbouring blocks find in L2.  Four positions at a time: the
-// words and sums of all eight would leave a SIMD two waves instead of three.
-template <int ND, int NOUT>
+// ciphertext's (the ModUp leaves them out).  Q: the row is one of the q limbs (the P rows have no c terms).  tail() is
+// called when the last loads here are out.
+template <int ND, int NOUT, bool Q, typename Tail>
 __device__ __forceinline__ void wsum8(const WsumKind &w, const Ct &ct, const Dims &d, uint32_t row, double pq, const A &ar,
-                                      const Positions &ps, double (&u)[NOUT][2][kE8])
+                                      const Positions &ps, double (&u)[NOUT][2][kE8], Tail tail)
 {
-    constexpr int kC = 4;
-    const uint32_t nd = ND > 0 ? (uint32_t)ND : d.nd;
-    constexpr int kUnroll = ND > 0 ? ND : 1;
+    constexpr int PU = unit_pairs(ND), kUnits = 4 / PU;
+    using U = Unit<ND, PU, NOUT>;
     const size_t rw = (size_t)row << d.log_n, half = (size_t)d.L << d.log_n;
     const size_t kstride = (size_t)d.key_rows << d.log_n, dstride = (size_t)d.ext << d.log_n;
-    const bool q_row = row < d.L;
+    const size_t krow = (size_t)d.prime(row) << d.log_n;
+    const uint64_t *c0 = ct.c + rw;
+    const uint32_t own = Q ? row / d.alpha : ~0u;
+    auto load = [&](U &x, uint32_t j, int p0) {
+        __builtin_amdgcn_sched_barrier(0);
+        const uint32_t g = w.g[j], kg = ps.start(g);
+        const uint64_t *key = w.key[j] + krow;
+#pragma unroll
+        for (int e = 0; e < PU; e++) {
+            const uint32_t sc = ps.source(kg, g, 2 * (p0 + e)), at = sc & ~1u;
+            x.flip[e] = sc & 1u;
+            if constexpr (Q) x.c[e] = ld2(c0 + at);
+#pragma unroll
+            for (int i = 0; i < ND; i++)
+                x.dig[i][e] = ld2((Q && (uint32_t)i == own ? ct.c + half : ct.dig + i * dstride) + rw + at);
+        }
+#pragma unroll
+        for (int e = 0; e < PU; e++) {
+            const uint32_t at = ps.pos(2 * (p0 + e));
+#pragma unroll
+            for (int i = 0; i < ND; i++) {
+                x.b[i][e] = ld2(key + 2 * i * kstride + at);
+                x.a[i][e] = ld2(key + (2 * i + 1) * kstride + at);
+            }
+#pragma unroll
+            for (int o = 0; o < NOUT; o++) x.tab[o][e] = ld2(w.tab[o][j] + rw + at);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto weigh = [&](const Pair &tab, int o, int e, double t0, double t1, double s0, double s1) {
+        const double p0 = A::from_u64(tab.x), p1 = A::from_u64(tab.y);
+        u[o][0][e] += ar.mul(t0, p0);
+        u[o][1][e] += ar.mul(t1, p0);
+        u[o][0][e + 1] += ar.mul(s0, p1);
+        u[o][1][e + 1] += ar.mul(s1, p1);
+    };
+    // keeps the sums of one unit ahead of the next unit's loads: the compiler would gather them all behind the last load,
+    // with every unit's words in registers
+    auto done = [&] {
+#pragma unroll
+        for (int o = 0; o < NOUT; o++)
+#pragma unroll
+            for (int e = 0; e < kE8; e++) asm volatile("" : "+v"(u[o][0][e]), "+v"(u[o][1][e]));
+    };
+    auto use = [&](const U &x, int p0) {
+#pragma unroll
+        for (int e = 0; e < PU; e++) {
+            const bool f = x.flip[e];
+            ProductSum s0, s1, r0, r1;   // both components at the even position, then at the odd one
+            if constexpr (Q) {
+                s0.add(A::from_u64(f ? x.c[e].y : x.c[e].x), pq);
+                r0.add(A::from_u64(f ? x.c[e].x : x.c[e].y), pq);
+            }
+#pragma unroll
+            for (int i = 0; i < ND; i++) {
+                if (i && i % 3 == 0) {   // s0 and r0 hold the c0 term and three products
+                    s0.fold(ar);
+                    s1.fold(ar);
+                    r0.fold(ar);
+                    r1.fold(ar);
+                }
+                const double v0 = A::from_u64(f ? x.dig[i][e].y : x.dig[i][e].x),
+                             v1 = A::from_u64(f ? x.dig[i][e].x : x.dig[i][e].y);
+                s0.add(v0, A::from_u64(x.b[i][e].x));
+                s1.add(v0, A::from_u64(x.a[i][e].x));
+                r0.add(v1, A::from_u64(x.b[i][e].y));
+                r1.add(v1, A::from_u64(x.a[i][e].y));
+            }
+            const double t0 = s0.value(ar), t1 = s1.value(ar), t2 = r0.value(ar), t3 = r1.value(ar);
+#pragma unroll
+            for (int o = 0; o < NOUT; o++) weigh(x.tab[o][e], o, 2 * (p0 + e), t0, t1, t2, t3);
+        }
+        done();
+    };
 #pragma unroll
     for (int o = 0; o < NOUT; o++)
 #pragma unroll
         for (int e = 0; e < kE8; e++) u[o][0][e] = u[o][1][e] = 0.0;
-    for (uint32_t j = 0; j < w.n; j++) {
-        const uint32_t g = w.g[j], kg = ps.start(g);
-        const uint64_t *wk = w.key[j];
-        if (!wk && !q_row) continue;
-        const uint64_t *key = wk + ((size_t)d.prime(row) << d.log_n), *dig = ct.dig + rw;
-        const uint32_t own = q_row ? row / d.alpha : ~0u;
+    const uint32_t first = w.key[0] ? 0 : 1, n = w.n;
+    U x0, x1;
+    if (first < n) load(x0, first, 0);
+    if (Q && first) {
+        // the unrotated term: two pairs at a time
 #pragma unroll
-        for (int e0 = 0; e0 < kE8; e0 += kC) {
-            double t0[kC], t1[kC];
-            if (wk) {
-                ProductSum s0[kC], s1[kC];
-                uint32_t sc[2];
+        for (int p0 = 0; p0 < 4; p0 += 2) {
+            Pair v0[2], v1[2], tab[NOUT][2];
 #pragma unroll
-                for (int e = 0; e < 2; e++) sc[e] = ps.source(kg, g, e0 + 2 * e);
-                if (q_row) {
+            for (int e = 0; e < 2; e++) {
+                const uint32_t at = ps.pos(2 * (p0 + e));
+                v0[e] = ld2(c0 + at);
+                v1[e] = ld2(c0 + half + at);
 #pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        const Pair v = ld2_auto(ct.c + rw, sc[e]);
-                        s0[2 * e].add(A::from_u64(v.x), pq);
-                        s0[2 * e + 1].add(A::from_u64(v.y), pq);
-                    }
-                }
-#pragma unroll kUnroll
-                for (uint32_t i = 0; i < nd; i++) {
-                    const uint64_t *di = i == own ? ct.c + half + rw : dig + i * dstride, *kb = key + 2 * i * kstride,
-                                   *ka = kb + kstride;
-                    Pair dv[2], bv[2], av[2];
+                for (int o = 0; o < NOUT; o++) tab[o][e] = ld2(w.tab[o][0] + rw + at);
+            }
+            if (p0 && first >= n) tail();
 #pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        dv[e] = ld2_auto(di, sc[e]);
-                        bv[e] = ld2(kb + ps.pos(e0 + 2 * e));
-                        av[e] = ld2(ka + ps.pos(e0 + 2 * e));
-                    }
-                    if (i && i % 3 == 0) {   // s0 holds the c0 term and three products
-#pragma unroll
-                        for (int e = 0; e < kC; e++) {
-                            s0[e].fold(ar);
-                            s1[e].fold(ar);
-                        }
-                    }
-#pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        const double v0 = A::from_u64(dv[e].x), v1 = A::from_u64(dv[e].y);
-                        s0[2 * e].add(v0, A::from_u64(bv[e].x));
-                        s1[2 * e].add(v0, A::from_u64(av[e].x));
-                        s0[2 * e + 1].add(v1, A::from_u64(bv[e].y));
-                        s1[2 * e + 1].add(v1, A::from_u64(av[e].y));
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < kC; e++) {
-                    t0[e] = s0[e].value(ar);
-                    t1[e] = s1[e].value(ar);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 2; e++) {
-                    const uint64_t *c = ct.c + rw + ps.pos(e0 + 2 * e);
-                    const Pair v0 = ld2(c), v1 = ld2(c + half);
-                    t0[2 * e] = A::from_u64(v0.x);
-                    t0[2 * e + 1] = A::from_u64(v0.y);
-                    t1[2 * e] = A::from_u64(v1.x);
-                    t1[2 * e + 1] = A::from_u64(v1.y);
-                }
+            for (int e = 0; e < 2; e++) {
+                double t0 = A::from_u64(v0[e].x), t1 = A::from_u64(v1[e].x), t2 = A::from_u64(v0[e].y),
+                       t3 = A::from_u64(v1[e].y);
                 if (w.rotated) {
-#pragma unroll
-                    for (int e = 0; e < kC; e++) {
-                        t0[e] = ar.mul(t0[e], pq);
-                        t1[e] = ar.mul(t1[e], pq);
-                    }
+                    t0 = ar.mul(t0, pq);
+                    t1 = ar.mul(t1, pq);
+                    t2 = ar.mul(t2, pq);
+                    t3 = ar.mul(t3, pq);
                 }
-            }
 #pragma unroll
-            for (int o = 0; o < NOUT; o++) {
-                const uint64_t *tab = w.tab[o][j] + rw;
-#pragma unroll
-                for (int e = 0; e < kC; e += 2) {
-                    const Pair v = ld2(tab + ps.pos(e0 + e));
-                    const double p0 = A::from_u64(v.x), p1 = A::from_u64(v.y);
-                    u[o][0][e0 + e] += ar.mul(t0[e], p0);
-                    u[o][1][e0 + e] += ar.mul(t1[e], p0);
-                    u[o][0][e0 + e + 1] += ar.mul(t0[e + 1], p1);
-                    u[o][1][e0 + e + 1] += ar.mul(t1[e + 1], p1);
-                }
+                for (int o = 0; o < NOUT; o++) weigh(tab[o][e], o, 2 * (p0 + e), t0, t1, t2, t3);
             }
+            done();
+        }
+    }
+    for (uint32_t j = first; j < n; j++) {
+        // two register sets in turn; the last unit's successor is the term after it, or the tail
+#pragma unroll
+        for (int k = 0; k < kUnits; k += 2) {
+            load(x1, j, (k + 1) * PU);
+            use(x0, k * PU);
+            if (k + 2 < kUnits) load(x0, j, (k + 2) * PU);
+            else if (j + 1 < n) load(x0, j + 1, 0);
+            else tail();
+            use(x1, (k + 1) * PU);
         }
     }
 }
@@ -328,9 +391,10 @@ __global__ __launch_bounds__(64) void k_wsum_intt8(Args a, uint64_t *up, Dims d,
     const A ar(mods[prime]);
     const uint32_t sub = threadIdx.x >> 5, t = threadIdx.x & 31, h = blk * 2 + sub;
     nttc::stage_twiddles8(tws[sub], itwf + ((size_t)prime << d.log_n), (1u << (d.log_n - 8)) + h, t, 32);
-    const Positions ps{h * 256 + 4 * t, d.log_n};
+    const Positions ps(h, t, d.log_n);
     double u[NOUT][2][kE8];
-    wsum8<ND, NOUT>(w, ct, d, row, s ? 0.0 : (double)pmodq[row].x, ar, ps, u);
+    if (s) wsum8<ND, NOUT, false>(w, ct, d, row, 0.0, ar, ps, u, NoTail());
+    else wsum8<ND, NOUT, true>(w, ct, d, row, (double)pmodq[row].x, ar, ps, u, NoTail());
     __syncthreads();
 #pragma unroll
     for (int o = 0; o < NOUT; o++)
@@ -339,6 +403,7 @@ __global__ __launch_bounds__(64) void k_wsum_intt8(Args a, uint64_t *up, Dims d,
             double x[kE8];
 #pragma unroll
             for (int e = 0; e < kE8; e++) x[e] = ar.red(u[o][k][e]);
+            swap_1_6(x);
             nttc::inv8_256(x, tws[sub], tr[sub], t, ar);
             uint64_t *out = up + ((((size_t)(z * NOUT + o) * 2 + k) * (d.K + 1) + s) << d.log_n) + (size_t)h * 256;
 #pragma unroll
@@ -567,9 +632,21 @@ __global__ __launch_bounds__(64) void k_wsum_fin8(Args a, const uint64_t *__rest
     const uint64_t q = mods[row].q;
     const uint32_t sub = threadIdx.x >> 5, t = threadIdx.x & 31, h = blk * 2 + sub;
     nttc::stage_twiddles8(tws[sub], twf + ((size_t)row << d.log_n), (1u << (d.log_n - 8)) + h, t, 32);
-    const Positions ps{h * 256 + 4 * t, d.log_n};
+    const Positions ps(h, t, d.log_n);
+    // an output's transform rows, both components: the first one's asked for ahead of the last sums
+    double x[2][kE8];
+    auto ask = [&](int o) {
+        __builtin_amdgcn_sched_barrier(0);
+        const uint64_t *src = cw + (((size_t)(z * NOUT + o) * 2 * l + row) << d.log_n) + (size_t)h * 256;
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+#pragma unroll
+            for (int e = 0; e < kE8; e++)
+                x[k][e] = A::from_raw(nttc::ld_stream(src + ((size_t)k * l << d.log_n) + nttc::u8<0>(t, e)));
+        __builtin_amdgcn_sched_barrier(0);
+    };
     double u[NOUT][2][kE8];
-    wsum8<ND, NOUT>(w, ct, d, row, (double)qt.pmodq[row].x, ar, ps, u);
+    wsum8<ND, NOUT, true>(w, ct, d, row, (double)qt.pmodq[row].x, ar, ps, u, [&] { ask(0); });
     // (P q_l)^-1, or q_l^-1 where u has no factor P, canonical
     double f = (double)qt.qlinv[row].x;
     if (w.rotated) {
@@ -579,25 +656,20 @@ __global__ __launch_bounds__(64) void k_wsum_fin8(Args a, const uint64_t *__rest
     __syncthreads();
 #pragma unroll
     for (int o = 0; o < NOUT; o++) {
+        if (o) ask(o);
         const uint64_t *prev = ct.prev[o];
-        // both components' rows and page words asked for together, before the first transform
-        double x[2][kE8];
         Pair pv[2][kE8 / 2];
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-            const uint64_t *src = cw + ((((size_t)(z * NOUT + o) * 2 + k) * l + row) << d.log_n) + (size_t)h * 256;
-#pragma unroll
-            for (int e = 0; e < kE8; e++) x[k][e] = A::from_raw(nttc::ld_stream(src + nttc::u8<0>(t, e)));
-        }
         if (prev) {
 #pragma unroll
             for (int k = 0; k < 2; k++)
 #pragma unroll
-                for (int e = 0; e < kE8; e += 2) pv[k][e / 2] = ld2(prev + ((size_t)(k * l + row) << d.log_n) + ps.pos(e));
+                for (int e = 0; e < kE8; e += 2)
+                    pv[k][e / 2] = ld2(prev + ((size_t)(k * l + row) << d.log_n) + ps.pos(e));
         }
 #pragma unroll
         for (int k = 0; k < 2; k++) {
             nttc::fwd8_256<nttc::kRowMask8>(x[k], tws[sub], tr[sub], t, ar);
+            swap_1_6(x[k]);
 #pragma unroll
             for (int e = 0; e < kE8; e += 2) {
                 Pair v;
@@ -618,7 +690,7 @@ dim3 grid_of(const ckks_ctx *ctx, uint32_t rows, uint32_t z) { return dim3((ctx-
 // the two-pass fp64 kernels run
 bool two_pass(const ckks_ctx *ctx, uint32_t level)
 {
-    return ctx->log_n >= 14 && f64_switch(ctx, level);
+    return ctx->log_n >= 14 && f64_switch(ctx, level) && n_digits(ctx, level) <= 5;
 }
 
 // Words of a batch.  The digits, with the staging rows of the ModUps that take any; then, two passes: the rows q_l and P of
@@ -673,7 +745,7 @@ ckks_status modup_cts(ckks_ctx *ctx, uint32_t L, const Args &a, uint32_t n_rot, 
     return ks_modup_batch(ctx, c1, stride, n_rot, L - 1, dig, stage_rows);
 }
 
-#define CK_ND(nd, GO)                                                                                                  do {                                                                                                                   switch (nd) {                                                                                                      case 1: GO(1); break;                                                                                              case 2: GO(2); break;                                                                                              case 3: GO(3); break;                                                                                              case 4: GO(4); break;                                                                                              default: GO(0); break;                                                                                             }                                                                                                              } while (0)
+#define CK_ND(nd, GO)                                                                                                  do {                                                                                                                   switch (nd) {                                                                                                      case 1: GO(1); break;                                                                                              case 2: GO(2); break;                                                                                              case 3: GO(3); break;                                                                                              case 4: GO(4); break;                                                                                              default: GO(5); break;                                                                                             }                                                                                                              } while (0)
 
 // steps 1 to 4 for n ciphertexts whose digits are formed
 ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pages, const Dims &d, uint64_t *up,
