@@ -646,7 +646,7 @@ __global__ __launch_bounds__(64) void k_wsum_fin8(Args a, const uint64_t *__rest
         __builtin_amdgcn_sched_barrier(0);
     };
     double u[NOUT][2][kE8];
-    wsum8<ND, NOUT, true>(w, ct, d, row, (double)qt.pmodq[row].x, ar, ps, u, [&] { ask(0); });
+    wsum8<ND, NOUT, true>(w, ct, d, row, (double)qt.pmodq[row].x, ar, ps, u, NoTail());
     // (P q_l)^-1, or q_l^-1 where u has no factor P, canonical
     double f = (double)qt.qlinv[row].x;
     if (w.rotated) {
@@ -656,7 +656,7 @@ __global__ __launch_bounds__(64) void k_wsum_fin8(Args a, const uint64_t *__rest
     __syncthreads();
 #pragma unroll
     for (int o = 0; o < NOUT; o++) {
-        if (o) ask(o);
+        ask(o);
         const uint64_t *prev = ct.prev[o];
         Pair pv[2][kE8 / 2];
         if (prev) {
