@@ -151,9 +151,12 @@ struct ConvLds {
     double tws[2][256];
     double tr[16][nttc::kTr8], trb[16][nttc::kTr8];
 };
-template <int NS>
+// COLS: `in` holds the sources after the row pass of their inverse transform, and each source's column pass is run here
+// as well, its row asked for while the one before is transformed.
+template <int NS, bool COLS>
 __device__ __forceinline__ void conv_col8(uint64_t *out, const uint64_t *in, const Blocks &bl, uint32_t t_per,
-                                          const ModQ *__restrict__ mods, const double *__restrict__ twf, ConvLds &lds)
+                                          const ModQ *__restrict__ mods, const double *__restrict__ twf,
+                                          const double *__restrict__ itwf, ConvLds &lds)
 {
     constexpr uint32_t log_n = 16, n2 = 256;
     double *s_mod = lds.mod;
@@ -166,22 +169,58 @@ __device__ __forceinline__ void conv_col8(uint64_t *out, const uint64_t *in, con
     const int t0 = (int)(blockIdx.y * t_per), t1 = min(nt, t0 + (int)t_per);
     if (t0 >= nt) return;
     for (int k = threadIdx.x; k < ns * nt; k += 512) s_mod[k] = bl.mod[j][k];
-    if (threadIdx.x < 255)
-        tws[t0 & 1][threadIdx.x + 1] = twf[((size_t)bl.out_prime(bl.out_row(j, t0)) << log_n) + threadIdx.x + 1];
     const uint32_t col = threadIdx.x & 15, t = threadIdx.x >> 4;
     const uint32_t coff = blk * 16 + col;
     const uint64_t *src = in + bl.at(r, lo) + coff;
-    double y[NS][kE8];
-#pragma unroll
-    for (int i = 0; i < NS; i++)
-#pragma unroll
-        for (int k = 0; k < kE8; k++) y[i][k] = A::from_raw(src[((size_t)i << log_n) + (size_t)nttc::u8<0>(t, k) * n2]);
     uint64_t *dst0 = out + ((size_t)(r * bl.nd + j) * bl.out_rows << log_n) + coff;
+    const bool stages = threadIdx.x < 255;
+    const double *first = twf + ((size_t)bl.out_prime(bl.out_row(j, t0)) << log_n) + threadIdx.x + 1;
+    double y[NS][kE8];
+    // target tt's twiddles are in half (tt - t0 + base) & 1 of the table
+    constexpr int base = COLS ? NS : 0;
+    if constexpr (COLS) {
+        auto itw = [&](int i) { return itwf[((size_t)bl.src_prime(lo + i) << log_n) + threadIdx.x + 1]; };
+        if (stages) tws[0][threadIdx.x + 1] = itw(0);
+        double next[kE8];
+        auto ask = [&](int i) {
+#pragma unroll
+            for (int k = 0; k < kE8; k++)
+                next[k] = A::from_raw(src[((size_t)i << log_n) + (size_t)nttc::u8<2>(t, k) * n2]);
+        };
+        ask(0);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NS; i++) {
+            const A ar(mods[bl.src_prime(lo + i)]);
+            A sc = ar;
+            sc.ninv = ar.scaled_twiddle(bl.inv[j][i]);
+            const double wn = sc.scaled_twiddle(tws[i & 1][1]);
+            nttc::StageNext nx{tws[(i + 1) & 1], 0.0, stages && i + 1 < NS};
+            if (nx.on) nx.v = itw(i + 1);
+#pragma unroll
+            for (int k = 0; k < kE8; k++) y[i][k] = next[k];
+            if (i + 1 < NS) ask(i + 1);
+            nttc::inv8_256_loop(y[i], tws[i & 1], tr[col], trb[col], t, ar, sc.ninv, wn, nx);
+#pragma unroll
+            for (int k = 0; k < kE8; k++) {
+                y[i][k] = ar.red(y[i][k]);
+                asm volatile("" : "+v"(y[i][k]));   // here, not where it is used: the transform's words are free again
+            }
+        }
+        if (stages) tws[base & 1][threadIdx.x + 1] = *first;
+    } else {
+        if (stages) tws[0][threadIdx.x + 1] = *first;
+#pragma unroll
+        for (int i = 0; i < NS; i++)
+#pragma unroll
+            for (int k = 0; k < kE8; k++) y[i][k] = A::from_raw(src[((size_t)i << log_n) + (size_t)nttc::u8<0>(t, k) * n2]);
+    }
     __syncthreads();
     for (int tt = t0; tt < t1; tt++) {
         const uint32_t row = bl.out_row(j, tt);
         const A ar(mods[bl.out_prime(row)]);
-        nttc::StageNext next{tws[(tt + 1) & 1], 0.0, tt + 1 < t1 && threadIdx.x < 255};
+        const double *tw = tws[(tt - t0 + base) & 1];
+        nttc::StageNext next{tws[(tt - t0 + base + 1) & 1], 0.0, tt + 1 < t1 && stages};
         if (next.on) next.v = twf[((size_t)bl.out_prime(bl.out_row(j, tt + 1)) << log_n) + threadIdx.x + 1];
         double x[kE8];
 #pragma unroll
@@ -191,7 +230,7 @@ __device__ __forceinline__ void conv_col8(uint64_t *out, const uint64_t *in, con
             for (int i = 0; i < NS; i++) acc.add(y[i][k], s_mod[i * nt + tt]);
             x[k] = ar.red(acc.value(ar));
         }
-        nttc::fwd8_256_loop<nttc::kColMask8>(x, tws[tt & 1], tr[col], trb[col], t, ar, next);
+        nttc::fwd8_256_loop<nttc::kColMask8>(x, tw, tr[col], trb[col], t, ar, next);
         uint64_t *dst = dst0 + ((size_t)row << log_n);
 #pragma unroll
         for (int k = 0; k < kE8; k++) nttc::st_stream(dst + (size_t)nttc::u8<2>(t, k) * n2, A::to_raw(x[k]));
@@ -199,26 +238,29 @@ __device__ __forceinline__ void conv_col8(uint64_t *out, const uint64_t *in, con
 }
 
 // the block's number of sources at compile time: FULL when every block of the launch has 8
-template <bool FULL>
+template <bool FULL, bool COLS>
 __global__ __launch_bounds__(512) void k_conv_col8(uint64_t *out, const uint64_t *in, Blocks bl, uint32_t t_per,
-                                                   const ModQ *__restrict__ mods, const double *__restrict__ twf)
+                                                   const ModQ *__restrict__ mods, const double *__restrict__ twf,
+                                                   const double *__restrict__ itwf)
 {
     __shared__ ConvLds lds;
     const uint32_t j = blockIdx.z;
+#define CK_NS(N) conv_col8<N, COLS>(out, in, bl, t_per, mods, twf, itwf, lds)
     if constexpr (FULL) {
-        conv_col8<8>(out, in, bl, t_per, mods, twf, lds);
+        CK_NS(8);
     } else {
         switch (bl.hi(j) - bl.lo(j)) {
-        case 1: conv_col8<1>(out, in, bl, t_per, mods, twf, lds); break;
-        case 2: conv_col8<2>(out, in, bl, t_per, mods, twf, lds); break;
-        case 3: conv_col8<3>(out, in, bl, t_per, mods, twf, lds); break;
-        case 4: conv_col8<4>(out, in, bl, t_per, mods, twf, lds); break;
-        case 5: conv_col8<5>(out, in, bl, t_per, mods, twf, lds); break;
-        case 6: conv_col8<6>(out, in, bl, t_per, mods, twf, lds); break;
-        case 7: conv_col8<7>(out, in, bl, t_per, mods, twf, lds); break;
-        default: conv_col8<8>(out, in, bl, t_per, mods, twf, lds); break;
+        case 1: CK_NS(1); break;
+        case 2: CK_NS(2); break;
+        case 3: CK_NS(3); break;
+        case 4: CK_NS(4); break;
+        case 5: CK_NS(5); break;
+        case 6: CK_NS(6); break;
+        case 7: CK_NS(7); break;
+        default: CK_NS(8); break;
         }
     }
+#undef CK_NS
 }
 
 // masks of the forward stages that reduce (ntt.hip: column output below 2 q, or below 4.3 q from k_conv_col8)
@@ -312,7 +354,15 @@ ckks_status launch_col_digits(ckks_ctx *ctx, uint64_t *data, uint32_t count, con
 // columns of 256 points and few enough sources for the registers of the fused conversion
 bool conv_fused(const ckks_ctx *ctx, uint32_t max_src) { return ctx->log_n == 16 && max_src <= 8; }
 
-// the conversion of every block of `count` entries; max_src, max_tgt over the blocks
+// the fused conversion takes the sources' column passes too: with a block for every CU, so that no block's targets are
+// split (each part would transform the sources again)
+bool conv_cols(const ckks_ctx *ctx, uint32_t max_src, uint32_t count, const Blocks &bl)
+{
+    return conv_fused(ctx, max_src) && count * 16 * bl.nd >= 256;
+}
+
+// the conversion of every block of `count` entries; max_src, max_tgt over the blocks; the sources are digits, or (conv_cols)
+// rows after the row pass of their inverse transform
 ckks_status launch_blocks_conv(ckks_ctx *ctx, uint64_t *out, const uint64_t *in, uint32_t count, const Blocks &bl,
                                uint32_t max_src, uint32_t max_tgt, bool exact8)
 {
@@ -324,12 +374,15 @@ ckks_status launch_blocks_conv(ckks_ctx *ctx, uint64_t *out, const uint64_t *in,
         const uint32_t blocks = count * 16 * bl.nd, groups = std::min(max_tgt, std::max(1u, 256u / blocks));
         const uint32_t t_per = (max_tgt + groups - 1) / groups;
         const dim3 grid(count * 16, (max_tgt + t_per - 1) / t_per, bl.nd);
-        if (exact8)
-            hipLaunchKernelGGL(k_conv_col8<true>, grid, dim3(512), 0, ctx->stream, out, in, bl, t_per, ctx->d_mod,
-                               ctx->d_twf);
-        else
-            hipLaunchKernelGGL(k_conv_col8<false>, grid, dim3(512), 0, ctx->stream, out, in, bl, t_per, ctx->d_mod,
-                               ctx->d_twf);
+        const bool cols = conv_cols(ctx, max_src, count, bl);
+#define CK_CC(FULL, COLS)                                                                                          \
+    hipLaunchKernelGGL((k_conv_col8<FULL, COLS>), grid, dim3(512), 0, ctx->stream, out, in, bl, t_per, ctx->d_mod,   \
+                       ctx->d_twf, ctx->d_itwf)
+        if (exact8 && cols) CK_CC(true, true);
+        else if (exact8) CK_CC(true, false);
+        else if (cols) CK_CC(false, true);
+        else CK_CC(false, false);
+#undef CK_CC
     } else {
         // groups of targets until the grid has 2048 blocks of four waves (two waves a SIMD)
         for (uint32_t r0 = 0; r0 < count; r0 += 65535u / bl.nd) {
@@ -398,7 +451,7 @@ ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t 
                        ctx->d_itwf);
     prof_end(ctx, K_NTT_INV_ROW);
     HIP_TRY(hipGetLastError());
-    CK_TRY(launch_col_digits(ctx, digits, count, bl));
+    if (!conv_cols(ctx, max_src, count, bl)) CK_TRY(launch_col_digits(ctx, digits, count, bl));
     CK_TRY(launch_blocks_conv(ctx, digits, digits, count, bl, max_src, max_tgt, exact8));
     const uint32_t rows = count * bl.nd * bl.ext;
     if (!conv_fused(ctx, max_src)) {
@@ -438,7 +491,7 @@ ckks_status up_moddown(ckks_ctx *ctx, uint64_t *up, uint32_t polys, uint32_t lev
     bl.out_rows = level + 1;
     bl.inv[0] = cd->d_qhat_inv_f;
     bl.mod[0] = cd->d_qhat_mod_f;
-    CK_TRY(launch_col_digits(ctx, up, polys, bl));
+    if (!conv_cols(ctx, ctx->n_p, polys, bl)) CK_TRY(launch_col_digits(ctx, up, polys, bl));
     CK_TRY(launch_blocks_conv(ctx, cw, up, polys, bl, ctx->n_p, level + 1, ctx->n_p == 8));
     if (!conv_fused(ctx, ctx->n_p))
         CK_TRY(launch_ntt_fwd_first_pass(ctx, cw, polys, level + 1, limb_range(0, level + 1)));

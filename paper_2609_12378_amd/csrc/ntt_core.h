@@ -513,6 +513,39 @@ __device__ __forceinline__ void inv8_256(double (&x)[kE8], const double *itws, d
     inv8_stage<0, 0>(x, itws, t, ar);
 }
 
+// inv8_256 for a block that runs it again and again, in two barriers (tr, trb and hook() as in fwd8_256_loop), its last
+// stage times f N^-1: ninv = f N^-1 mod q and wn = itws[1] f N^-1 mod q, both canonical.
+template <typename Hook = NoHook>
+__device__ __forceinline__ void inv8_256_loop(double (&x)[kE8], const double *itws, double *tr, double *trb, uint32_t t,
+                                              const Ar<true> &ar, double ninv, double wn, Hook hook = Hook())
+{
+    inv8_stage<2, 7>(x, itws, t, ar);
+    inv8_stage<2, 6>(x, itws, t, ar);
+#pragma unroll
+    for (int k = 0; k < kE8; k++) tr[pad_cb(u8<2>(t, k))] = x[k];
+    __syncthreads();
+    hook();
+#pragma unroll
+    for (int k = 0; k < kE8; k++) x[k] = tr[pad_cb(u8<1>(t, k))];
+    inv8_stage<1, 5>(x, itws, t, ar);
+    inv8_stage<1, 4>(x, itws, t, ar);
+    inv8_stage<1, 3>(x, itws, t, ar);
+#pragma unroll
+    for (int k = 0; k < kE8; k++) trb[pad_ac(u8<1>(t, k))] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kE8; k++) x[k] = trb[pad_ac(u8<0>(t, k))];
+    inv8_stage<0, 2>(x, itws, t, ar);
+    inv8_stage<0, 1>(x, itws, t, ar);
+    // stage 0 pairs the points that differ in bit 7, registers k and k | 4
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const double u = x[k] + x[k | 4], v = x[k] - x[k | 4];
+        x[k] = ar.mul(u, ninv);
+        x[k | 4] = ar.mul(v, wn);
+    }
+}
+
 // twiddle table of a 256-point sub-transform with base B: tws[2^s + g] = Psi[B 2^s + g]
 // for 1 <= 2^s + g < 256; filled by `nthreads` threads starting at thread `tid`
 __device__ __forceinline__ void stage_twiddles8(double *tws, const double *tw, uint32_t B, uint32_t tid,

@@ -476,11 +476,12 @@ __device__ __forceinline__ double top_factor(const Quot &qt, const Dims &d, int 
 
 // 3. The conversion fused with the forward column pass, N = 2^16 and at most 8 special primes (k_conv_col8's shape: block
 // (poly; 16 adjacent columns; group of t_per targets), 512 threads, 8 points of a 256-point column each, the digits of
-// the block's 4096 coefficients and w in registers for every target).  EXACT: K = 8.
-template <bool EXACT>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_quot_col8(uint64_t *out, const uint64_t *up, Args a, Dims d, uint32_t pages,
+// the block's 4096 coefficients and w in registers for every target).  EXACT: K = 8.  COLS: `up` holds the rows after the
+// row pass of their inverse transforms, whose column passes run here as well (step 2 is not a launch of its own).
+template <bool EXACT, bool COLS>
+__global__ __launch_bounds__(512) void k_quot_col8(uint64_t *out, const uint64_t *up, Args a, Dims d, uint32_t pages,
                                                    uint32_t t_per, Quot qt, const ModQ *__restrict__ mods,
-                                                   const double *__restrict__ twf)
+                                                   const double *__restrict__ twf, const double *__restrict__ itwf)
 {
     __shared__ double s_mod[9 * kMaxPrimes];   // [K][targets], then [P]_t
     __shared__ double s_top[8];
@@ -498,21 +499,65 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int k = threadIdx.x; k < nt; k += 512) s_mod[8 * kMaxPrimes + k] = (double)qt.pmodq[k].x;
         if (threadIdx.x < (uint32_t)K) s_top[threadIdx.x] = top_factor(qt, d, (int)threadIdx.x, top);
     }
-    if (threadIdx.x < 255) tws[t0 & 1][threadIdx.x + 1] = twf[((size_t)t0 << log_n) + threadIdx.x + 1];
     const uint32_t col = threadIdx.x & 15, t = threadIdx.x >> 4;
     const uint32_t coff = blk * 16 + col;
     const uint64_t *src = up + ((size_t)p * (d.K + 1) << log_n) + coff;
+    uint64_t *dst0 = out + ((size_t)p * nt << log_n) + coff;
+    const bool stages = threadIdx.x < 255;
+    const double *first = twf + ((size_t)t0 << log_n) + threadIdx.x + 1;
     double y[8][kE8], w[kE8];
-#pragma unroll
-    for (int k = 0; k < kE8; k++) w[k] = A::from_raw(src[(size_t)nttc::u8<0>(t, k) * n2]);
-    if (rot) {
-#pragma unroll
-        for (int i = 0; i < 8; i++)
+    int turn = 0;   // target tt's twiddles are in half (tt - t0 + turn) & 1 of the table
+    if constexpr (COLS) {
+        // rows P, then q_l, each asked for while the one before is transformed
+        double next[kE8];
+        const int rows = rot ? K + 1 : 1;
+        auto slot = [&](int i) { return rot && i < K ? i + 1 : 0; };
+        auto itw = [&](int i) { return itwf[((size_t)d.prime(d.L - 1 + slot(i)) << log_n) + threadIdx.x + 1]; };
+        auto ask = [&](int i) {
 #pragma unroll
             for (int k = 0; k < kE8; k++)
-                if (EXACT || i < K) y[i][k] = A::from_raw(src[((size_t)(i + 1) << log_n) + (size_t)nttc::u8<0>(t, k) * n2]);
+                next[k] = A::from_raw(src[((size_t)slot(i) << log_n) + (size_t)nttc::u8<2>(t, k) * n2]);
+        };
+        auto column = [&](double (&x)[kE8], int i) {
+            const uint32_t s = slot(i);
+            const A ar(mods[d.prime(d.L - 1 + s)]);
+            A sc = ar;
+            if (s) sc.ninv = ar.scaled_twiddle(qt.qhat_inv[s - 1]);
+            else if (rot) sc.ninv = ar.scaled_twiddle((double)qt.pinv[d.L - 1].x);
+            const double wn = sc.scaled_twiddle(tws[i & 1][1]);
+            nttc::StageNext nx{tws[(i + 1) & 1], 0.0, stages && i + 1 < rows};
+            if (nx.on) nx.v = itw(i + 1);
+#pragma unroll
+            for (int k = 0; k < kE8; k++) x[k] = next[k];
+            if (i + 1 < rows) ask(i + 1);
+            nttc::inv8_256_loop(x, tws[i & 1], tr[col], trb[col], t, ar, sc.ninv, wn, nx);
+#pragma unroll
+            for (int k = 0; k < kE8; k++) x[k] = centre(ar, x[k]);
+        };
+        if (stages) tws[0][threadIdx.x + 1] = itw(0);
+        ask(0);
+        __syncthreads();
+        if (rot) {
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (EXACT || i < K) column(y[i], i);
+        }
+        column(w, rows - 1);
+        turn = rows;
+        if (stages) tws[turn & 1][threadIdx.x + 1] = *first;
+    } else {
+        if (stages) tws[0][threadIdx.x + 1] = *first;
+#pragma unroll
+        for (int k = 0; k < kE8; k++) w[k] = A::from_raw(src[(size_t)nttc::u8<0>(t, k) * n2]);
+        if (rot) {
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+#pragma unroll
+                for (int k = 0; k < kE8; k++)
+                    if (EXACT || i < K)
+                        y[i][k] = A::from_raw(src[((size_t)(i + 1) << log_n) + (size_t)nttc::u8<0>(t, k) * n2]);
+        }
     }
-    uint64_t *dst0 = out + ((size_t)p * nt << log_n) + coff;
     __syncthreads();
     if (rot) {
 #pragma unroll
@@ -526,7 +571,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
     for (int tt = t0; tt < t1; tt++) {
         const A ar(mods[tt]);
-        nttc::StageNext next{tws[(tt + 1) & 1], 0.0, tt + 1 < t1 && threadIdx.x < 255};
+        const double *tw = tws[(tt - t0 + turn) & 1];
+        nttc::StageNext next{tws[(tt - t0 + turn + 1) & 1], 0.0, tt + 1 < t1 && stages};
         if (next.on) next.v = twf[((size_t)(tt + 1) << log_n) + threadIdx.x + 1];
         double x[kE8];
         if (rot) {
@@ -545,7 +591,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
             for (int k = 0; k < kE8; k++) x[k] = ar.red(w[k]);
         }
-        nttc::fwd8_256_loop<nttc::kColMask8>(x, tws[tt & 1], tr[col], trb[col], t, ar, next);
+        nttc::fwd8_256_loop<nttc::kColMask8>(x, tw, tr[col], trb[col], t, ar, next);
         uint64_t *dst = dst0 + ((size_t)tt << log_n);
 #pragma unroll
         for (int k = 0; k < kE8; k++) nttc::st_stream(dst + (size_t)nttc::u8<2>(t, k) * n2, A::to_raw(x[k]));
@@ -766,21 +812,25 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
     prof_end(ctx, K_KEYIP);
     HIP_TRY(hipGetLastError());
 
-    const double rows2 = (double)polys * (d.K + 1) * N;
-    prof_begin(ctx, K_NTT_INV_COL, 16.0 * rows2, rows2 * kOpsButterflyF64 * (d.log_n - 8) / 2);
-#define CK_COL(S)                                                                                                      hipLaunchKernelGGL(k_quot_col<S>, dim3(polys * (d.K + 1) * (256 / (4096u >> S))), dim3(256), 0, ctx->stream, up, a,                        d, pages, qt, ctx->d_mod, ctx->d_itwf)
-    switch (d.log_n) {
-    case 12: CK_COL(4); break;
-    case 13: CK_COL(5); break;
-    case 14: CK_COL(6); break;
-    case 15: CK_COL(7); break;
-    default: CK_COL(8); break;
-    }
-#undef CK_COL
-    prof_end(ctx, K_NTT_INV_COL);
-    HIP_TRY(hipGetLastError());
-
     const bool fused = d.log_n == 16 && d.K <= 8;
+    // with a block for every CU, no block's targets are split and its columns are transformed where they are converted
+    const bool cols = fused && polys * 16 >= 256;
+    const double rows2 = (double)polys * (d.K + 1) * N;
+    if (!cols) {
+        prof_begin(ctx, K_NTT_INV_COL, 16.0 * rows2, rows2 * kOpsButterflyF64 * (d.log_n - 8) / 2);
+#define CK_COL(S)                                                                                                      hipLaunchKernelGGL(k_quot_col<S>, dim3(polys * (d.K + 1) * (256 / (4096u >> S))), dim3(256), 0, ctx->stream, up, a,                        d, pages, qt, ctx->d_mod, ctx->d_itwf)
+        switch (d.log_n) {
+        case 12: CK_COL(4); break;
+        case 13: CK_COL(5); break;
+        case 14: CK_COL(6); break;
+        case 15: CK_COL(7); break;
+        default: CK_COL(8); break;
+        }
+#undef CK_COL
+        prof_end(ctx, K_NTT_INV_COL);
+        HIP_TRY(hipGetLastError());
+    }
+
     prof_begin(ctx, K_CONV, 8.0 * N * polys * (d.K + 1.0 + level),
                (double)N * polys * level * (d.K * 4.0 + 14.0 + (fused ? kOpsButterflyF64 * 4 : 0.0)));
     if (fused) {
@@ -788,12 +838,14 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
         const uint32_t blocks = polys * 16, groups = std::min(level, std::max(1u, 256u / blocks));
         const uint32_t t_per = (level + groups - 1) / groups;
         const dim3 grid(blocks, (level + t_per - 1) / t_per);
-        if (d.K == 8)
-            hipLaunchKernelGGL(k_quot_col8<true>, grid, dim3(512), 0, ctx->stream, cw, up, a, d, pages, t_per, qt, ctx->d_mod,
-                               ctx->d_twf);
-        else
-            hipLaunchKernelGGL(k_quot_col8<false>, grid, dim3(512), 0, ctx->stream, cw, up, a, d, pages, t_per, qt,
-                               ctx->d_mod, ctx->d_twf);
+#define CK_QC(EXACT, COLS)                                                                                         \
+    hipLaunchKernelGGL((k_quot_col8<EXACT, COLS>), grid, dim3(512), 0, ctx->stream, cw, up, a, d, pages, t_per, qt,  \
+                       ctx->d_mod, ctx->d_twf, ctx->d_itwf)
+        if (d.K == 8 && cols) CK_QC(true, true);
+        else if (d.K == 8) CK_QC(true, false);
+        else if (cols) CK_QC(false, true);
+        else CK_QC(false, false);
+#undef CK_QC
     } else {
         // groups of targets until the grid has 2048 blocks of four waves
         const uint32_t blocks = polys * (ctx->n / 256), groups = std::min(level, std::max(1u, 2048u / blocks));
