@@ -150,6 +150,8 @@ struct ConvLds {
     double mod[8 * kMaxPrimes];
     double tws[2][256];
     double tr[16][nttc::kTr8], trb[16][nttc::kTr8];
+    nttc::LimbConst tgt[kMaxPrimes];
+    nttc::InvConst src[8];
 };
 // COLS: `in` holds the sources after the row pass of their inverse transform, and each source's column pass is run here
 // as well, its row asked for while the one before is transformed.
@@ -169,6 +171,7 @@ __device__ __forceinline__ void conv_col8(uint64_t *out, const uint64_t *in, con
     const int t0 = (int)(blockIdx.y * t_per), t1 = min(nt, t0 + (int)t_per);
     if (t0 >= nt) return;
     for (int k = threadIdx.x; k < ns * nt; k += 512) s_mod[k] = bl.mod[j][k];
+    for (int k = threadIdx.x; k < nt; k += 512) lds.tgt[k].set(A(mods[bl.out_prime(bl.out_row(j, k))]));
     const uint32_t col = threadIdx.x & 15, t = threadIdx.x >> 4;
     const uint32_t coff = blk * 16 + col;
     const uint64_t *src = in + bl.at(r, lo) + coff;
@@ -179,9 +182,16 @@ __device__ __forceinline__ void conv_col8(uint64_t *out, const uint64_t *in, con
     // target tt's twiddles are in half (tt - t0 + base) & 1 of the table
     constexpr int base = COLS ? NS : 0;
     if constexpr (COLS) {
-        auto itw = [&](int i) { return itwf[((size_t)bl.src_prime(lo + i) << log_n) + threadIdx.x + 1]; };
+        // source i's twiddles, asked for two sources ahead
+        auto itw = [&](int i) {
+            return stages && i < NS ? itwf[((size_t)bl.src_prime(lo + i) << log_n) + threadIdx.x + 1] : 0.0;
+        };
+        if (threadIdx.x < NS) {
+            const uint32_t prime = bl.src_prime(lo + threadIdx.x);
+            lds.src[threadIdx.x].set(A(mods[prime]), bl.inv[j][threadIdx.x], itwf[((size_t)prime << log_n) + 1]);
+        }
         if (stages) tws[0][threadIdx.x + 1] = itw(0);
-        double next[kE8];
+        double next[kE8], tw1 = itw(1);
         auto ask = [&](int i) {
 #pragma unroll
             for (int k = 0; k < kE8; k++)
@@ -191,16 +201,14 @@ __device__ __forceinline__ void conv_col8(uint64_t *out, const uint64_t *in, con
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < NS; i++) {
-            const A ar(mods[bl.src_prime(lo + i)]);
-            A sc = ar;
-            sc.ninv = ar.scaled_twiddle(bl.inv[j][i]);
-            const double wn = sc.scaled_twiddle(tws[i & 1][1]);
-            nttc::StageNext nx{tws[(i + 1) & 1], 0.0, stages && i + 1 < NS};
-            if (nx.on) nx.v = itw(i + 1);
+            const A ar = lds.src[i].m.get();
+            const nttc::StageNext nx{tws[(i + 1) & 1], tw1, stages && i + 1 < NS};
 #pragma unroll
             for (int k = 0; k < kE8; k++) y[i][k] = next[k];
             if (i + 1 < NS) ask(i + 1);
-            nttc::inv8_256_loop(y[i], tws[i & 1], tr[col], trb[col], t, ar, sc.ninv, wn, nx);
+            tw1 = itw(i + 2);
+            nttc::inv8_256_loop(y[i], tws[i & 1], tr[col], trb[col], t, ar, nttc::uniform(lds.src[i].ninv),
+                                nttc::uniform(lds.src[i].wn), nx);
 #pragma unroll
             for (int k = 0; k < kE8; k++) {
                 y[i][k] = ar.red(y[i][k]);
@@ -218,7 +226,7 @@ __device__ __forceinline__ void conv_col8(uint64_t *out, const uint64_t *in, con
     __syncthreads();
     for (int tt = t0; tt < t1; tt++) {
         const uint32_t row = bl.out_row(j, tt);
-        const A ar(mods[bl.out_prime(row)]);
+        const A ar = lds.tgt[tt].get();
         const double *tw = tws[(tt - t0 + base) & 1];
         nttc::StageNext next{tws[(tt - t0 + base + 1) & 1], 0.0, tt + 1 < t1 && stages};
         if (next.on) next.v = twf[((size_t)bl.out_prime(bl.out_row(j, tt + 1)) << log_n) + threadIdx.x + 1];

@@ -513,6 +513,44 @@ __device__ __forceinline__ void inv8_256(double (&x)[kE8], const double *itws, d
     inv8_stage<0, 0>(x, itws, t, ar);
 }
 
+// Constants of a limb that a block staged in LDS (a loop over limbs would wait for scalar loads of them at its first LDS
+// access), read back as scalars.
+__device__ __forceinline__ double uniform(double v)
+{
+    const uint64_t b = (uint64_t)__double_as_longlong(v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b),
+                   hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32));
+    return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+struct LimbConst {
+    double q, qinv;
+    __device__ void set(const Ar<true> &ar)
+    {
+        q = ar.q;
+        qinv = ar.qinv;
+    }
+    __device__ Ar<true> get() const
+    {
+        Ar<true> ar;
+        ar.q = uniform(q);
+        ar.qinv = uniform(qinv);
+        return ar;
+    }
+};
+// the same with an inverse transform's last factors: f N^-1, and w f N^-1 with w the last stage's twiddle
+struct InvConst {
+    LimbConst m;
+    double ninv, wn;
+    __device__ void set(const Ar<true> &ar, double f, double w)
+    {
+        m.set(ar);
+        Ar<true> sc = ar;
+        sc.ninv = ar.scaled_twiddle(f);
+        ninv = sc.ninv;
+        wn = sc.scaled_twiddle(w);
+    }
+};
+
 // inv8_256 for a block that runs it again and again, in two barriers (tr, trb and hook() as in fwd8_256_loop), its last
 // stage times f N^-1: ninv = f N^-1 mod q and wn = itws[1] f N^-1 mod q, both canonical.
 template <typename Hook = NoHook>

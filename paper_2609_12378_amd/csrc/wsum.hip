@@ -487,6 +487,8 @@ __global__ __launch_bounds__(512) void k_quot_col8(uint64_t *out, const uint64_t
     __shared__ double s_top[8];
     __shared__ double tws[2][256];
     __shared__ double tr[16][nttc::kTr8], trb[16][nttc::kTr8];
+    __shared__ nttc::LimbConst s_tgt[kMaxPrimes];
+    __shared__ nttc::InvConst s_src[9];
     constexpr uint32_t log_n = 16, n2 = 256;
     const uint32_t p = blockIdx.x >> 4, blk = blockIdx.x & 15u;
     const int K = EXACT ? 8 : (int)d.K, nt = (int)d.L - 1;
@@ -499,6 +501,7 @@ __global__ __launch_bounds__(512) void k_quot_col8(uint64_t *out, const uint64_t
         for (int k = threadIdx.x; k < nt; k += 512) s_mod[8 * kMaxPrimes + k] = (double)qt.pmodq[k].x;
         if (threadIdx.x < (uint32_t)K) s_top[threadIdx.x] = top_factor(qt, d, (int)threadIdx.x, top);
     }
+    for (int k = threadIdx.x; k < nt; k += 512) s_tgt[k].set(A(mods[k]));
     const uint32_t col = threadIdx.x & 15, t = threadIdx.x >> 4;
     const uint32_t coff = blk * 16 + col;
     const uint64_t *src = up + ((size_t)p * (d.K + 1) << log_n) + coff;
@@ -512,29 +515,38 @@ __global__ __launch_bounds__(512) void k_quot_col8(uint64_t *out, const uint64_t
         double next[kE8];
         const int rows = rot ? K + 1 : 1;
         auto slot = [&](int i) { return rot && i < K ? i + 1 : 0; };
-        auto itw = [&](int i) { return itwf[((size_t)d.prime(d.L - 1 + slot(i)) << log_n) + threadIdx.x + 1]; };
+        // row i's twiddles, asked for two rows ahead
+        auto itw = [&](int i) {
+            return stages && i < rows ? itwf[((size_t)d.prime(d.L - 1 + slot(i)) << log_n) + threadIdx.x + 1] : 0.0;
+        };
+        if (threadIdx.x < (uint32_t)rows) {
+            const int s = slot((int)threadIdx.x);
+            const uint32_t prime = d.prime(d.L - 1 + s);
+            const double f = s ? qt.qhat_inv[s - 1] : rot ? (double)qt.pinv[d.L - 1].x : 1.0;
+            s_src[threadIdx.x].set(A(mods[prime]), f, itwf[((size_t)prime << log_n) + 1]);
+        }
+        if (stages) tws[0][threadIdx.x + 1] = itw(0);
+        double tw1 = itw(1);
         auto ask = [&](int i) {
 #pragma unroll
             for (int k = 0; k < kE8; k++)
                 next[k] = A::from_raw(src[((size_t)slot(i) << log_n) + (size_t)nttc::u8<2>(t, k) * n2]);
         };
         auto column = [&](double (&x)[kE8], int i) {
-            const uint32_t s = slot(i);
-            const A ar(mods[d.prime(d.L - 1 + s)]);
-            A sc = ar;
-            if (s) sc.ninv = ar.scaled_twiddle(qt.qhat_inv[s - 1]);
-            else if (rot) sc.ninv = ar.scaled_twiddle((double)qt.pinv[d.L - 1].x);
-            const double wn = sc.scaled_twiddle(tws[i & 1][1]);
-            nttc::StageNext nx{tws[(i + 1) & 1], 0.0, stages && i + 1 < rows};
-            if (nx.on) nx.v = itw(i + 1);
+            const A ar = s_src[i].m.get();
+            const nttc::StageNext nx{tws[(i + 1) & 1], tw1, stages && i + 1 < rows};
 #pragma unroll
             for (int k = 0; k < kE8; k++) x[k] = next[k];
             if (i + 1 < rows) ask(i + 1);
-            nttc::inv8_256_loop(x, tws[i & 1], tr[col], trb[col], t, ar, sc.ninv, wn, nx);
+            tw1 = itw(i + 2);
+            nttc::inv8_256_loop(x, tws[i & 1], tr[col], trb[col], t, ar, nttc::uniform(s_src[i].ninv),
+                                nttc::uniform(s_src[i].wn), nx);
 #pragma unroll
-            for (int k = 0; k < kE8; k++) x[k] = centre(ar, x[k]);
+            for (int k = 0; k < kE8; k++) {
+                x[k] = centre(ar, x[k]);
+                asm volatile("" : "+v"(x[k]));   // here, not where it is used: the transform's words are free again
+            }
         };
-        if (stages) tws[0][threadIdx.x + 1] = itw(0);
         ask(0);
         __syncthreads();
         if (rot) {
@@ -570,7 +582,7 @@ __global__ __launch_bounds__(512) void k_quot_col8(uint64_t *out, const uint64_t
         }
     }
     for (int tt = t0; tt < t1; tt++) {
-        const A ar(mods[tt]);
+        const A ar = s_tgt[tt].get();
         const double *tw = tws[(tt - t0 + turn) & 1];
         nttc::StageNext next{tws[(tt - t0 + turn + 1) & 1], 0.0, tt + 1 < t1 && stages};
         if (next.on) next.v = twf[((size_t)(tt + 1) << log_n) + threadIdx.x + 1];
