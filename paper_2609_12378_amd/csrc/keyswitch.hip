@@ -938,7 +938,7 @@ ckks_status ks_modup_batch(ckks_ctx *ctx, const uint64_t *c1, size_t in_stride, 
 {
     if (!count) return CKKS_OK;
     if (blk_switch(ctx, level) && (size_t)count * (level + 1) <= stage_rows)
-        return blk_modup(ctx, c1, count == 1 ? 0 : in_stride, nullptr, count, level, digits,
+        return blk_modup(ctx, PolySrc{c1, count == 1 ? 0 : in_stride, {}}, nullptr, count, level, digits,
                          digits + (size_t)count * n_digits(ctx, level) * (level + 1 + ctx->n_p) * ctx->n);
     const uint32_t K = ctx->n_p, ext = level + 1 + K, nd = n_digits(ctx, level), alpha = ctx->alpha;
     const size_t N = ctx->n, dig_ct = (size_t)nd * ext * N;
@@ -994,7 +994,7 @@ ckks_status ks_mul_relin_blk(ckks_ctx *ctx, const uint64_t *a, const uint64_t *b
     const uint32_t L = level + 1, ext = L + ctx->n_p, nd = n_digits(ctx, level);
     const size_t N = ctx->n;
     uint64_t *digits = work, *rest = digits + (size_t)nd * ext * N;
-    CK_TRY(blk_modup(ctx, a + (size_t)L * N, 0, b, 1, level, digits, rest));
+    CK_TRY(blk_modup(ctx, PolySrc{a + (size_t)L * N, 0, {}}, b, 1, level, digits, rest));
     RotArgs ra{};
     ra.count = 1;
     ra.g[0] = 1;

@@ -138,10 +138,10 @@ ckks_status blk_decrypt(ckks_ctx *ctx, uint64_t *pt, const uint64_t *c0, const u
                         uint32_t limbs);
 // rescale of `polys` polynomials c ([polys][l+1][N]) into out ([polys][l][N]); work: polys N words
 ckks_status blk_rescale(ckks_ctx *ctx, const uint64_t *c, uint32_t polys, uint32_t l, uint64_t *out, uint64_t *work);
-// ModUp of `count` polynomials at c1 + r stride, or (b set, count 1) of the product of the second components of the
-// ciphertexts whose second components start at c1 and at b + (level+1) N; stage: count (level+1) N words
-ckks_status blk_modup(ckks_ctx *ctx, const uint64_t *c1, size_t stride, const uint64_t *b, uint32_t count,
-                      uint32_t level, uint64_t *digits, uint64_t *stage);
+// ModUp of `count` polynomials, or (b set, count 1) of the product of the second components of the ciphertexts whose
+// second components start at c1 and at b + (level+1) N; stage: count (level+1) N words
+ckks_status blk_modup(ckks_ctx *ctx, const PolySrc &c1, const uint64_t *b, uint32_t count, uint32_t level,
+                      uint64_t *digits, uint64_t *stage);
 // a rotation batch; with ta, tb2 (ciphertexts) the addends are the first two components of their tensor product.
 // work: count 2 (level+1+n_p) N words
 struct RotArgs;

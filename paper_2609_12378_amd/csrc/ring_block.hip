@@ -271,11 +271,10 @@ struct Digits {
     uint32_t nd, alpha, L, K, n_q;
     const double *inv[kMaxPrimes], *mod[kMaxPrimes];
 };
-// A polynomial that is switched: c1 at base + r stride for entry r of the batch, or (b set) the product of the second
-// components of the ciphertexts a and b ([2][L][N] each), formed where it is read
+// A polynomial that is switched: c1 of entry r of the batch, or (b set) the product of the second components of the
+// ciphertexts a and b ([2][L][N] each), formed where it is read
 struct Source {
-    const uint64_t *base;
-    size_t stride;
+    PolySrc c1;
     const uint64_t *b;
 };
 
@@ -342,7 +341,7 @@ __global__ __launch_bounds__(blk::Shape<LOGN>::NT) void k_blk_digits(double *y, 
     const A ar(tb.mods[l]);
     const blk::ColTw<LOGN> cw(table<LOGN>(tb.itwf, l));
     const blk::RowTw<LOGN> rw(table<LOGN>(tb.itwf, l));
-    const uint64_t *in = src.base + r * src.stride + ((size_t)l << LOGN);
+    const uint64_t *in = src.c1.at(r) + ((size_t)l << LOGN);
     double x[kE];
 #pragma unroll
     for (int k = 0; k < kE; k++) {
@@ -369,7 +368,7 @@ void k_blk_modup(uint64_t *digits, const double *__restrict__ y, Source src, Dig
     const A ar(tb.mods[prime]);
     uint64_t *o = digits + ((((size_t)r * dg.nd + j) * ext + row) << LOGN);
     if (row >= lo && row < hi) {
-        const uint64_t *in = src.base + r * src.stride + ((size_t)row << LOGN);
+        const uint64_t *in = src.c1.at(r) + ((size_t)row << LOGN);
 #pragma unroll
         for (int k = 0; k < kE; k++) {
             const uint32_t p = blk::row_pos(t, k);
@@ -716,8 +715,8 @@ ckks_status blk_rescale(ckks_ctx *ctx, const uint64_t *c, uint32_t polys, uint32
     return CKKS_OK;
 }
 
-ckks_status blk_modup(ckks_ctx *ctx, const uint64_t *c1, size_t stride, const uint64_t *b, uint32_t count,
-                      uint32_t level, uint64_t *digits, uint64_t *stage)
+ckks_status blk_modup(ckks_ctx *ctx, const PolySrc &c1, const uint64_t *b, uint32_t count, uint32_t level,
+                      uint64_t *digits, uint64_t *stage)
 {
     Digits dg{};
     dg.nd = n_digits(ctx, level);
@@ -738,7 +737,8 @@ ckks_status blk_modup(ckks_ctx *ctx, const uint64_t *c1, size_t stride, const ui
     // a launch takes at most 65535 entries (blockIdx.y and z)
     for (uint32_t r0 = 0; r0 < count; r0 += 65535u) {
         const uint32_t cnt = std::min(count - r0, 65535u);
-        const Source src{c1 + r0 * stride, stride, b};
+        Source src{c1, b};
+        if (c1.base) src.c1.base += r0 * c1.stride;
         uint64_t *d = digits + (size_t)r0 * dg.nd * ext * N;
         double *yr = y + (size_t)r0 * dg.L * N;
         prof_begin(ctx, K_NTT_INV_ROW, 16.0 * cnt * dg.L * N);

@@ -20,33 +20,15 @@
 // Elsewhere u is formed whole in exact 128-bit sums (k_wsum) and goes through the ModDown and rescale of the ring.
 #include <algorithm>
 
-#include "ks_args.h"
 #include "ops.h"
-#include "wsum.h"
+#include "wsum_args.h"
 
 namespace {
 
 constexpr int kThreads = 256;
-using A = nttc::Ar<true>;
+using namespace wsum;
 using nttc::kE;
 using nttc::kE8;
-
-struct Ct {
-    const uint64_t *c, *dig;   // [2][L][N]; its ModUp digits [nd][ext][N] (rotated kinds)
-    uint64_t *out[kWsumPages];
-    const uint64_t *prev[kWsumPages];
-    uint32_t kind;
-};
-struct Args {
-    WsumKind kind[kWsumKinds];
-    Ct ct[kWsumCts];
-};
-
-// The ring's sizes: L = level + 1 q-limbs, K special primes, ext = L + K, nd digits
-struct Dims {
-    uint32_t L, K, ext, nd, alpha, n_q, key_rows, log_n;
-    __device__ uint32_t prime(uint32_t row) const { return row < L ? row : n_q + (row - L); }
-};
 
 // ------------------------------------------------------------------------- in exact 128-bit sums, any ring -------------
 
@@ -137,31 +119,6 @@ __global__ __launch_bounds__(kThreads) void k_gather_c1(uint64_t *out, Args a, u
 }
 
 // ------------------------------------------------------------------------- two passes, fp64 ----------------------------
-
-// sum_i a_i w_i mod q of at most 4 products of canonical residues under one quotient (nttc::GridSum with twice its grid:
-// u = 2^51, so |sum| < 4 2^100 = 2^51 u, and lo is at most 4 2^50 = 2^52).  value(): |x| <= q/2 + 1.
-struct ProductSum {
-    static constexpr double kGrid = 0x1.8p+103;   // 1.5 2^52 u
-    double hi, lo;
-    __device__ ProductSum() : hi(kGrid), lo(0.0) {}
-    __device__ void add(double a, double w)
-    {
-        const double t = fma(a, w, hi);
-        const double h = t - hi;
-        lo += fma(a, w, -h);
-        hi = t;
-    }
-    __device__ double value(const A &ar) const
-    {
-        const double h = hi - kGrid;
-        return ar.red(fma(-rint(h * ar.qinv), ar.q, h) + lo);
-    }
-    __device__ void fold(const A &ar)
-    {
-        lo = value(ar);
-        hi = kGrid;
-    }
-};
 
 // Two adjacent words, read and written in one 16-byte access (rows are 8-byte aligned).
 struct __attribute__((aligned(8))) Pair {
@@ -411,33 +368,6 @@ __global__ __launch_bounds__(64) void k_wsum_intt8(Args a, uint64_t *up, Dims d,
         }
 }
 
-// the integer r in [0, 2^52) as a word: the mantissa of 2^52 + r
-__device__ __forceinline__ uint64_t to_word(double r)
-{
-    return (uint64_t)__double_as_longlong(r + 4503599627370496.0) & 0x000FFFFFFFFFFFFFull;
-}
-
-// x f mod q, canonical: |x| < 8 q reduced to q/2 + 1, times f in [0, q) at most 0.7 q
-__device__ __forceinline__ uint64_t quotient(const A &ar, double x, double f)
-{
-    const double r = ar.mul(ar.red(x), f);
-    return to_word(r < 0.0 ? r + ar.q : r);
-}
-
-// (-q/2, q/2] of |x| < q/2 + 2^49: the centred representative of an odd modulus
-__device__ __forceinline__ double centre(const A &ar, double x)
-{
-    const double v = ar.red(x), h = 0.5 * ar.q;
-    return v > h ? v - ar.q : v < -h ? v + ar.q : v;
-}
-
-// The division's constants: y_i takes N^-1 Qhat_i^-1, the q_l row N^-1 P^-1 (N^-1 alone for unrotated kinds)
-struct Quot {
-    const double *qhat_inv;    // [K]
-    const double *qhat_mod;    // [K][L] centred
-    const ulonglong2 *pinv, *qlinv, *pmodq;
-};
-
 // 2. column pass of those rows, in place: centred digits as doubles
 template <int LOGS>
 __global__ __launch_bounds__(256) void k_quot_col(uint64_t *up, Args a, Dims d, uint32_t pages, Quot qt,
@@ -466,12 +396,6 @@ __global__ __launch_bounds__(256) void k_quot_col(uint64_t *up, Args a, Dims d, 
     nttc::inv_top<true, true>(x, tw, 1, sc);
 #pragma unroll
     for (int k = 0; k < kE; k++) base[(size_t)(t + TS * k) * 256] = A::to_raw(centre(ar, x[k]));
-}
-
-// factor of source i in the conversion to q_l divided by P, [P / p_i P^-1]_{q_l}, centred
-__device__ __forceinline__ double top_factor(const Quot &qt, const Dims &d, int i, const A &top)
-{
-    return centre(top, top.mul(qt.qhat_mod[i * d.L + d.L - 1], (double)qt.pinv[d.L - 1].x));
 }
 
 // 3. The conversion fused with the forward column pass, N = 2^16 and at most 8 special primes (k_conv_col8's shape: block
@@ -745,10 +669,10 @@ __global__ __launch_bounds__(64) void k_wsum_fin8(Args a, const uint64_t *__rest
 
 dim3 grid_of(const ckks_ctx *ctx, uint32_t rows, uint32_t z) { return dim3((ctx->n + kThreads - 1) / kThreads, rows, z); }
 
-// the two-pass fp64 kernels run
-bool two_pass(const ckks_ctx *ctx, uint32_t level)
+// the fp64 kernels run: in two passes, or (N = 2^12 and 2^13, blk_switch) in whole rows
+bool fp64_sums(const ckks_ctx *ctx, uint32_t level)
 {
-    return ctx->log_n >= 14 && f64_switch(ctx, level) && n_digits(ctx, level) <= 5;
+    return f64_switch(ctx, level) && n_digits(ctx, level) <= 5;
 }
 
 // Words of a batch.  The digits, with the staging rows of the ModUps that take any; then, two passes: the rows q_l and P of
@@ -778,7 +702,7 @@ Dims dims_of(const ckks_ctx *ctx, uint32_t L)
 
 // the digits of the first n_rot ciphertexts; for the ModUps that take polynomials at one distance only, c1 of ciphertexts
 // that lie elsewhere is gathered to `work` first
-ckks_status modup_cts(ckks_ctx *ctx, uint32_t L, const Args &a, uint32_t n_rot, bool fast, uint64_t *dig,
+ckks_status modup_cts(ckks_ctx *ctx, uint32_t L, const Args &a, uint32_t n_rot, bool fast, bool rows, uint64_t *dig,
                       size_t stage_rows, uint64_t *work)
 {
     const size_t N = ctx->n;
@@ -788,6 +712,8 @@ ckks_status modup_cts(ckks_ctx *ctx, uint32_t L, const Args &a, uint32_t n_rot, 
         static_assert(kWsumCts <= (uint32_t)kPolyList, "a batch's polynomials fit the list");
         PolySrc src{};
         for (uint32_t i = 0; i < n_rot; i++) src.list[i] = a.ct[i].c + (size_t)L * N;
+        if (rows)
+            return blk_modup(ctx, src, nullptr, n_rot, L - 1, dig, dig + (size_t)n_rot * n_digits(ctx, L - 1) * (L + ctx->n_p) * N);
         return up_modup(ctx, src, n_rot, L - 1, dig, false);
     }
     bool even = true;
@@ -927,7 +853,7 @@ ckks_status wsum_run(ckks_ctx *ctx, uint32_t L, uint32_t pages, const WsumKind *
                      uint64_t *mem)
 {
     const Dims d = dims_of(ctx, L);
-    const bool fast = two_pass(ctx, L - 1);
+    const bool fast = fp64_sums(ctx, L - 1), rows = fast && blk_switch(ctx, L - 1);
     for (size_t r0 = 0; r0 < cts.size();) {
         // a batch: rotated and unrotated ciphertexts together where the kernels take both
         Args a{};
@@ -948,8 +874,10 @@ ckks_status wsum_run(ckks_ctx *ctx, uint32_t L, uint32_t pages, const WsumKind *
             }
         }
         const Scratch s = scratch_of(ctx, L, n, pages);
-        if (n_rot) CK_TRY(modup_cts(ctx, L, a, n_rot, fast, mem, s.stage_rows, mem + s.dig + s.u + s.v));
-        if (fast)
+        if (n_rot) CK_TRY(modup_cts(ctx, L, a, n_rot, fast, rows, mem, s.stage_rows, mem + s.dig + s.u + s.v));
+        if (rows)
+            CK_TRY(wsum_blk_sums(ctx, a, n, pages, d, mem + s.dig));
+        else if (fast)
             CK_TRY(two_pass_sums(ctx, a, n, pages, d, mem + s.dig, mem + s.dig + s.u));
         else
             CK_TRY(exact_sums(ctx, a, n, pages, d, first, s, mem));
