@@ -39,10 +39,16 @@ constexpr int kMaxPrimes = 64;
 constexpr int kMaxLimbMap = 96;
 
 // Row r of a [rows][N] launch uses prime index prime[r % n] (r / n is the batch
-// index).
+// index).  groups > 0: rows r % n < skip_end with (r % n) / skip = (r / n) % groups are
+// left as they are (the digits' own rows of a ModUp).
 struct LimbMap {
     uint32_t n;
     uint8_t prime[kMaxLimbMap];
+    uint32_t groups, skip, skip_end;
+    __device__ bool skips(uint32_t batch, uint32_t slot) const
+    {
+        return groups && slot < skip_end && slot / skip == batch % groups;
+    }
 };
 
 // Device constants of one fast basis conversion, from the primes src[0..ns) to
@@ -97,6 +103,7 @@ struct ckks_ctx {
     std::map<std::pair<int, int>, ConvDev> conv;  // (level, digit) ; digit -1 = ModDown
     ulonglong2 *d_pinv = nullptr;        // [n_q] (P^-1 mod q_i, Shoup)
     ulonglong2 *d_pmodq = nullptr;       // [n_q] ([P]_{q_i}, Shoup)
+    ulonglong2 *d_pqlinv = nullptr;      // [n_q][n_q] ((P q_l)^-1 mod q_i, Shoup) row l
     ulonglong2 *d_qlinv = nullptr;       // [n_q][n_q] (q_l^-1 mod q_i, Shoup) row l
 
     Arena arena;                    // scratch of the calls

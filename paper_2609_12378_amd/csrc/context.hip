@@ -211,18 +211,22 @@ static ckks_status build_tables(ckks_ctx *c)
     CK_TRY(upload((void **)&c->d_pos_slot, inv_pos.data(), inv_pos.size() * sizeof(uint32_t)));
 
     // P mod q_i, P^-1 mod q_i, q_l^-1 mod q_i
-    std::vector<ulonglong2> pm(c->n_q), pinv(c->n_q), qlinv((size_t)c->n_q * c->n_q);
+    std::vector<ulonglong2> pm(c->n_q), pinv(c->n_q), qlinv((size_t)c->n_q * c->n_q), pqlinv(qlinv.size());
     for (uint32_t i = 0; i < c->n_q; i++) {
         const uint64_t q = c->primes[i];
         uint64_t P = 1;
         for (uint32_t j = 0; j < c->n_p; j++) P = hm::mul(P, c->primes[c->n_q + j] % q, q);
         pm[i] = shoup_pair(P, q);
         pinv[i] = shoup_pair(hm::inv(P, q), q);
-        for (uint32_t l = 0; l < c->n_q; l++)
-            qlinv[(size_t)l * c->n_q + i] = shoup_pair(l == i ? 0 : hm::inv(c->primes[l] % q, q), q);
+        for (uint32_t l = 0; l < c->n_q; l++) {
+            const uint64_t v = l == i ? 0 : hm::inv(c->primes[l] % q, q);
+            qlinv[(size_t)l * c->n_q + i] = shoup_pair(v, q);
+            pqlinv[(size_t)l * c->n_q + i] = shoup_pair(hm::mul(v, pinv[i].x, q), q);
+        }
     }
     CK_TRY(upload((void **)&c->d_pmodq, pm.data(), pm.size() * sizeof(ulonglong2)));
     CK_TRY(upload((void **)&c->d_pinv, pinv.data(), pinv.size() * sizeof(ulonglong2)));
+    CK_TRY(upload((void **)&c->d_pqlinv, pqlinv.data(), pqlinv.size() * sizeof(ulonglong2)));
     CK_TRY(upload((void **)&c->d_qlinv, qlinv.data(), qlinv.size() * sizeof(ulonglong2)));
     return CKKS_OK;
 }
@@ -481,7 +485,7 @@ void ckks_ctx_destroy(ckks_ctx *c)
     if (c->arena.external) c->arena.base = nullptr;  // the caller's workspace
     void *ptrs[] = {c->d_mod, c->d_tw, c->d_itw, c->d_twf, c->d_itwf, c->d_fft_w, c->d_fft_wc, c->d_fft_twist, c->d_slot_pos,
                     c->d_pos_slot,
-                    c->d_pinv, c->d_pmodq, c->d_qlinv, c->arena.base};
+                    c->d_pinv, c->d_pmodq, c->d_qlinv, c->d_pqlinv, c->arena.base};
     for (void *p : ptrs)
         if (p) (void)hipFree(p);
     for (auto &kv : c->conv) {

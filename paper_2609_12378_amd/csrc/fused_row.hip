@@ -5,6 +5,7 @@
 //
 //   rescale     out_i = (c_i - NTT(top mod q_i)) q_l^-1, top the centred coefficients of the top limb
 //   ModDown     out_i = (u_i - NTT(conv)) P^-1 + addend            (integer arithmetic; fp64 has k_ks_finish8)
+//   weighted sums: the same with (P q_l)^-1                        (either arithmetic)
 //   decryption  pt = c0 + c1 NTT(s)
 //   encryption  (c0, c1) = (NTT(e) + m - a NTT(s), a)
 #include <algorithm>
@@ -331,18 +332,22 @@ ckks_status fused_rescale(ckks_ctx *ctx, const uint64_t *c, uint32_t polys, uint
     return CKKS_OK;
 }
 
-ckks_status fused_moddown_int(ckks_ctx *ctx, uint32_t level, const RotArgs &ra, const uint64_t *u, const uint64_t *cw)
+ckks_status fused_quotient(ckks_ctx *ctx, uint32_t limbs, uint32_t u_rows, const RotArgs &ra, const uint64_t *u,
+                           const uint64_t *cw, const ulonglong2 *w)
 {
     FinArgs a{};
     a.in = cw;
     a.c = u;
-    a.limbs = level + 1;
-    a.c_rows = level + 1 + ctx->n_p;
+    a.limbs = limbs;
+    a.c_rows = u_rows;
     a.polys = 2 * ra.count;
     a.log_n = ctx->log_n;
-    a.w = ctx->d_pinv;
+    a.w = w;
     prof_begin(ctx, K_MODDOWN, 8.0 * ctx->n * a.limbs * ra.count * 7.0);
-    launch_fin<false, FIN_MODDOWN>(ctx, a, ra);
+    if (ntt_uses_f64(ctx, limbs))
+        launch_fin<true, FIN_MODDOWN>(ctx, a, ra);
+    else
+        launch_fin<false, FIN_MODDOWN>(ctx, a, ra);
     prof_end(ctx, K_MODDOWN);
     HIP_TRY(hipGetLastError());
     return CKKS_OK;

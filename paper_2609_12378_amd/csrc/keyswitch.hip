@@ -877,7 +877,7 @@ ckks_status ks_rotate_batch(ckks_ctx *ctx, uint32_t level, uint32_t count, const
     CK_TRY(launch_conv(ctx, cd, u + (size_t)L * N, ext, cw, L, L, 0, 2 * count));
     if (rows256) {
         CK_TRY(launch_ntt_fwd_first_pass(ctx, cw, 2 * count, L, limb_range(0, L)));
-        return fused_moddown_int(ctx, level, ra, u, cw);
+        return fused_quotient(ctx, level + 1, level + 1 + ctx->n_p, ra, u, cw, ctx->d_pinv);
     }
     CK_TRY(launch_ntt(ctx, cw, 2 * count * L, limb_range(0, L), false));
     {
@@ -981,6 +981,25 @@ ckks_status ks_modup_batch(ckks_ctx *ctx, const uint64_t *c1, size_t in_stride, 
         }
     }
     return CKKS_OK;
+}
+
+ckks_status ks_modup_staged(ckks_ctx *ctx, uint64_t *c1, uint32_t count, uint32_t level, uint64_t *digits)
+{
+    const uint32_t L = level + 1, ext = L + ctx->n_p, nd = n_digits(ctx, level);
+    const size_t N = ctx->n;
+    CK_TRY(launch_ntt(ctx, c1, count * L, limb_range(0, L), true));
+    for (uint32_t j = 0; j < nd; j++) {
+        const uint32_t lo = digit_lo(ctx, j), hi = digit_hi(ctx, j, level);
+        const ConvDev *cd;
+        CK_TRY(ctx_conv(ctx, (int)level, (int)j, &cd));
+        CK_TRY(launch_conv(ctx, cd, c1 + lo * N, L, digits + (size_t)j * ext * N, nd * ext, lo, hi - lo, count));
+    }
+    LimbMap m = limb_range(0, L);
+    for (uint32_t i = 0; i < ctx->n_p; i++) m.prime[m.n++] = (uint8_t)(ctx->n_q + i);
+    m.groups = nd;
+    m.skip = ctx->alpha;
+    m.skip_end = L;
+    return launch_ntt_strided(ctx, digits, nd * count, ext, m, false);
 }
 
 ckks_status ks_modup(ckks_ctx *ctx, const uint64_t *c, uint32_t level, uint64_t *digits, size_t stage_rows)

@@ -53,10 +53,9 @@ struct acc128 {
 };
 __device__ __forceinline__ void mac(acc128 &acc, uint64_t a, uint64_t b)
 {
-    const uint64_t lo = a * b;
-    const uint64_t hi = mulhi64(a, b);
-    acc.lo += lo;
-    acc.hi += hi + (acc.lo < lo ? 1u : 0u);
+    // one 128-bit product and sum: four 32-bit multiply-adds and carries (a * b and mulhi64 apart are seven multiplies)
+    const unsigned __int128 s = ((unsigned __int128)acc.hi << 64 | acc.lo) + (unsigned __int128)a * b;
+    acc = acc128{(uint64_t)s, (uint64_t)(s >> 64)};
 }
 // Exact x mod q for a 128-bit x, canonical result.
 __device__ __forceinline__ uint64_t reduce128(acc128 x, const ModQ &m)

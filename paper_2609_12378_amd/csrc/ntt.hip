@@ -98,6 +98,7 @@ __global__ __launch_bounds__(256) void ntt_col(uint64_t *data, LimbMap map, uint
     E *lds = (E *)lds_raw;
     uint32_t slot;
     const size_t row = row_of_block(blockIdx.x / blocks_per_row, map.n, bstride, &slot);
+    if (map.skips(blockIdx.x / blocks_per_row / map.n, slot)) return;
     const uint32_t blk = blockIdx.x % blocks_per_row;
     const uint32_t prime = map.prime[slot];
     const Ar<F> ar(mods[prime]);
@@ -320,6 +321,7 @@ __global__ __launch_bounds__(LOGN ? 128 : 256) void ntt_row(uint64_t *data, Limb
     } else {
         poly = row_of_block(blockIdx.x / blocks_per_poly, map.n, bstride, &slot);
         h = (blockIdx.x % blocks_per_poly) * rows_per_block + sub;
+        if (map.skips(blockIdx.x / blocks_per_poly / map.n, slot)) return;
     }
     const uint32_t prime = map.prime[slot];
     const Ar<F> ar(mods[prime]);
@@ -396,7 +398,7 @@ hipError_t launch_row(ckks_ctx *ctx, uint64_t *data, uint32_t batch, uint32_t bs
     if constexpr (LOGS == 8 && !F) {
         // integer arithmetic, batches of whole octets: each block's 8 rows share their (16-byte) twiddle pairs
         // (with the fp64 arithmetic the rows of one polynomial measured as fast, with 6% less fetch)
-        if (ctx->log_n == 16 && batch % 8 == 0) {
+        if (ctx->log_n == 16 && batch % 8 == 0 && !map.groups) {
             hipLaunchKernelGGL((ntt_row<LOGS, INV, FIRST, LAST, F, 16, true>), grid, block, 0, ctx->stream, data, map,
                                bstride, ctx->d_mod, tw, ctx->log_n, rows, bpp);
             return hipGetLastError();

@@ -17,7 +17,8 @@
 //      w = [(U - sum_i y_i [P / p_i]) P^-1]_{q_l}.  ModDown and rescale subtract Conv(y) P^-1 and then w, so
 //      out = (u - NTT(x)) (P q_l)^-1 holds for both together and the q_l row never leaves the coefficient domain;
 //   4. k_wsum_fin8    the forward row pass, u on the rows below q_l (in registers, never in HBM), the quotient, prev.
-// Elsewhere u is formed whole in exact 128-bit sums (k_wsum) and goes through the ModDown and rescale of the ring.
+// Rings of 2^12 and 2^13 points do the same in whole rows (wsum_block.hip), other primes and rings in exact 128-bit sums
+// (wsum_exact.hip).
 #include <algorithm>
 
 #include "ops.h"
@@ -30,101 +31,7 @@ using namespace wsum;
 using nttc::kE;
 using nttc::kE8;
 
-// ------------------------------------------------------------------------- in exact 128-bit sums, any ring -------------
-
-// u[z P + o][k][row][n] of ciphertext z, output o of P
-template <int P>
-__global__ __launch_bounds__(kThreads) void k_wsum(Args a, uint64_t *u, Dims d, const ulonglong2 *__restrict__ pmodq,
-                                                   const ModQ *__restrict__ mods)
-{
-    const uint32_t col = blockIdx.x * kThreads + threadIdx.x, row = blockIdx.y, z = blockIdx.z;
-    if (col >= (1u << d.log_n)) return;
-    const uint32_t prime = d.prime(row);
-    const ModQ m = mods[prime];
-    const Ct &ct = a.ct[z];
-    const WsumKind &w = a.kind[ct.kind];
-    const size_t at = ((size_t)row << d.log_n) + col;
-    const uint64_t pq = row < d.L ? pmodq[row].x : 0;
-    const uint64_t *c = ct.c + ((size_t)row << d.log_n), *dig = ct.dig + ((size_t)row << d.log_n);
-    acc128 acc[P][2] = {};
-    for (uint32_t j = 0; j < w.n; j++) {
-        acc128 t0{0, 0}, t1{0, 0};
-        if (w.key[j]) {
-            const uint32_t sc = auto_index(col, w.g[j], d.log_n);
-            const uint64_t *key = w.key[j] + ((size_t)prime << d.log_n) + col;
-            for (uint32_t i = 0; i < d.nd; i++) {
-                const uint64_t v = dig[((size_t)i * d.ext << d.log_n) + sc];
-                mac(t0, v, key[(size_t)(2 * i) * d.key_rows << d.log_n]);
-                mac(t1, v, key[(size_t)(2 * i + 1) * d.key_rows << d.log_n]);
-            }
-            if (row < d.L) mac(t0, c[sc], pq);
-        } else if (row < d.L) {
-            mac(t0, c[col], pq);
-            mac(t1, c[((size_t)d.L << d.log_n) + col], pq);
-        }
-        const uint64_t v0 = reduce128(t0, m), v1 = reduce128(t1, m);
-#pragma unroll
-        for (int o = 0; o < P; o++) {
-            const uint64_t pt = w.tab[o][j][at];
-            mac(acc[o][0], v0, pt);
-            mac(acc[o][1], v1, pt);
-        }
-    }
-#pragma unroll
-    for (int o = 0; o < P; o++) {
-        uint64_t *x = u + ((size_t)(z * P + o) * 2 * d.ext << d.log_n) + at;
-        x[0] = reduce128(acc[o][0], m);
-        x[(size_t)d.ext << d.log_n] = reduce128(acc[o][1], m);
-    }
-}
-
-// v[z P + o][k][row] = pt c_k: the outputs of unrotated kinds, with nothing to divide by P
-__global__ __launch_bounds__(kThreads) void k_wmul(Args a, uint64_t *v, Dims d, uint32_t pages,
-                                                   const ModQ *__restrict__ mods)
-{
-    const uint32_t col = blockIdx.x * kThreads + threadIdx.x, row = blockIdx.y, z = blockIdx.z;
-    if (col >= (1u << d.log_n)) return;
-    const ModQ m = mods[row];
-    const size_t at = ((size_t)row << d.log_n) + col, half = (size_t)d.L << d.log_n;
-    const Ct &ct = a.ct[z];
-    const uint64_t c0 = ct.c[at], c1 = ct.c[half + at];
-    for (uint32_t o = 0; o < pages; o++) {
-        const uint64_t pt = a.kind[ct.kind].tab[o][0][at];
-        uint64_t *x = v + (size_t)(z * pages + o) * 2 * half + at;
-        x[0] = mulmod(c0, pt, m);
-        x[half] = mulmod(c1, pt, m);
-    }
-}
-
-// out = x[z P + o] (+ prev), [2][l][N] each
-__global__ __launch_bounds__(kThreads) void k_emit(Args a, const uint64_t *x, uint32_t l, uint32_t pages, uint32_t log_n,
-                                                   const ModQ *__restrict__ mods)
-{
-    const uint32_t col = blockIdx.x * kThreads + threadIdx.x, row = blockIdx.y, z = blockIdx.z / pages,
-                   o = blockIdx.z % pages;
-    if (col >= (1u << log_n)) return;
-    const size_t at = ((size_t)row << log_n) + col;
-    uint64_t v = x[((size_t)blockIdx.z * 2 * l << log_n) + at];
-    const uint64_t *prev = a.ct[z].prev[o];
-    if (prev) v = addmod(v, prev[at], mods[row % l].q);
-    a.ct[z].out[o][at] = v;
-}
-
-// c1 of ciphertext z to out[z][L][N]
-__global__ __launch_bounds__(kThreads) void k_gather_c1(uint64_t *out, Args a, uint32_t L, uint32_t log_n)
-{
-    const uint32_t col = blockIdx.x * kThreads + threadIdx.x, row = blockIdx.y, z = blockIdx.z;
-    if (col >= (1u << log_n)) return;
-    out[(((size_t)z * L + row) << log_n) + col] = a.ct[z].c[(((size_t)L + row) << log_n) + col];
-}
-
 // ------------------------------------------------------------------------- two passes, fp64 ----------------------------
-
-// Two adjacent words, read and written in one 16-byte access (rows are 8-byte aligned).
-struct __attribute__((aligned(8))) Pair {
-    uint64_t x, y;
-};
-__device__ __forceinline__ Pair ld2(const uint64_t *p) { return *(const Pair *)p; }
 
 // The positions of thread t (of 32) in a row of 256: pairs (j, j + 1) at j = 64 c + 4 (t & 15) + 2 (t >> 4), register
 // e = 2 c + (0 or 1), so a wave's access is whole cache lines.  It is the layout that the transforms end in and inverse
@@ -318,15 +225,6 @@ __device__ __forceinline__ void wsum8(const WsumKind &w, const Ct &ct, const Dim
             use(x1, (k + 1) * PU);
         }
     }
-}
-
-// Block b of a launch over `tiles` tiles (a multiple of 8) of each of n ciphertexts: blocks go to the 8 XCDs in turn, and
-// the ciphertexts of one tile, which share its keys and tables, follow one another on one XCD.
-__device__ __forceinline__ void tile_of(uint32_t n, uint32_t &z, uint32_t &tile)
-{
-    const uint32_t xcd = blockIdx.x & 7u, rest = blockIdx.x >> 3;
-    z = rest % n;
-    tile = (rest / n) * 8 + xcd;
 }
 
 // 1. rows q_l and P (s = 0: q_l, s > 0: p_{s-1}) of u: up[z P + o][k][s], raw doubles below 2q after the row pass.  One
@@ -675,23 +573,20 @@ bool fp64_sums(const ckks_ctx *ctx, uint32_t level)
     return f64_switch(ctx, level) && n_digits(ctx, level) <= 5;
 }
 
-// Words of a batch.  The digits, with the staging rows of the ModUps that take any; then, two passes: the rows q_l and P of
-// u and the converted rows; elsewhere u, the quotient by P, the conversion's rows (before them, the gathered c1) and
-// the rescale's result.
+// Words of a batch: the digits, the staging rows of the ModUps that take any, u (the fp64 kernels: its rows q_l and P)
+// and the converted rows.
 struct Scratch {
-    size_t dig, stage_rows, u, v, work, res, total;
+    size_t dig, stage, u, x, total;
 };
 Scratch scratch_of(const ckks_ctx *ctx, uint32_t L, uint32_t cts, uint32_t pages)
 {
-    const size_t N = ctx->n, K = ctx->n_p, ext = L + K, nd = n_digits(ctx, L - 1), outs = (size_t)cts * pages;
+    const size_t N = ctx->n, ext = L + ctx->n_p, nd = n_digits(ctx, L - 1), outs = (size_t)cts * pages;
     Scratch s{};
-    s.stage_rows = (size_t)cts * std::max<size_t>(ctx->alpha, L);
-    s.dig = cts * nd * ext * N + s.stage_rows * N;
+    s.dig = cts * nd * ext * N;
+    s.stage = (size_t)cts * L * N;
     s.u = outs * 2 * ext * N;
-    s.v = outs * 2 * L * N;
-    s.work = std::max(outs * 2, (size_t)cts) * L * N;
-    s.res = outs * 2 * (L - 1) * N;
-    s.total = s.dig + s.u + s.v + s.work + s.res;
+    s.x = outs * 2 * (L - 1) * N;
+    s.total = s.dig + s.stage + s.u + s.x;
     return s;
 }
 
@@ -700,36 +595,31 @@ Dims dims_of(const ckks_ctx *ctx, uint32_t L)
     return Dims{L, ctx->n_p, L + ctx->n_p, n_digits(ctx, L - 1), ctx->alpha, ctx->n_q, ctx->n_primes(), ctx->log_n};
 }
 
-// the digits of the first n_rot ciphertexts; for the ModUps that take polynomials at one distance only, c1 of ciphertexts
-// that lie elsewhere is gathered to `work` first
-ckks_status modup_cts(ckks_ctx *ctx, uint32_t L, const Args &a, uint32_t n_rot, bool fast, bool rows, uint64_t *dig,
-                      size_t stage_rows, uint64_t *work)
+// The digits of the first n_rot ciphertexts, without their own rows (blk_modup writes those too).  With fp64 primes the
+// ModUps read c1 where it is; else it is gathered to `stage` and taken to coefficient form there.
+ckks_status modup_cts(ckks_ctx *ctx, uint32_t L, const Args &a, uint32_t n_rot, uint64_t *dig, uint64_t *stage)
 {
-    const size_t N = ctx->n;
-    size_t stride = 2 * (size_t)L * N;
-    const uint64_t *c1 = a.ct[0].c + (size_t)L * N;
-    if (fast) {
+    if (f64_switch(ctx, L - 1)) {
         static_assert(kWsumCts <= (uint32_t)kPolyList, "a batch's polynomials fit the list");
         PolySrc src{};
-        for (uint32_t i = 0; i < n_rot; i++) src.list[i] = a.ct[i].c + (size_t)L * N;
-        if (rows)
-            return blk_modup(ctx, src, nullptr, n_rot, L - 1, dig, dig + (size_t)n_rot * n_digits(ctx, L - 1) * (L + ctx->n_p) * N);
-        return up_modup(ctx, src, n_rot, L - 1, dig, false);
+        for (uint32_t i = 0; i < n_rot; i++) src.list[i] = a.ct[i].c + (size_t)L * ctx->n;
+        return blk_switch(ctx, L - 1) ? blk_modup(ctx, src, nullptr, n_rot, L - 1, dig, stage)
+                                      : up_modup(ctx, src, n_rot, L - 1, dig, false);
     }
-    bool even = true;
-    for (uint32_t i = 1; i < n_rot; i++) even = even && a.ct[i].c == a.ct[0].c + i * stride;
-    if (!even) {
-        prof_begin(ctx, K_ELEM, 16.0 * N * L * n_rot);
-        hipLaunchKernelGGL(k_gather_c1, grid_of(ctx, L, n_rot), dim3(kThreads), 0, ctx->stream, work, a, L, ctx->log_n);
-        prof_end(ctx, K_ELEM);
-        HIP_TRY(hipGetLastError());
-        c1 = work;
-        stride = (size_t)L * N;
-    }
-    return ks_modup_batch(ctx, c1, stride, n_rot, L - 1, dig, stage_rows);
+    CK_TRY(wsum_gather_c1(ctx, a, n_rot, L, stage));
+    return ks_modup_staged(ctx, stage, n_rot, L - 1, dig);
 }
 
-#define CK_ND(nd, GO)                                                                                                  do {                                                                                                                   switch (nd) {                                                                                                      case 1: GO(1); break;                                                                                              case 2: GO(2); break;                                                                                              case 3: GO(3); break;                                                                                              case 4: GO(4); break;                                                                                              default: GO(5); break;                                                                                             }                                                                                                              } while (0)
+#define CK_ND(nd, GO)                                                                                              \
+    do {                                                                                                           \
+        switch (nd) {                                                                                              \
+        case 1: GO(1); break;                                                                                      \
+        case 2: GO(2); break;                                                                                      \
+        case 3: GO(3); break;                                                                                      \
+        case 4: GO(4); break;                                                                                      \
+        default: GO(5); break;                                                                                     \
+        }                                                                                                          \
+    } while (0)
 
 // steps 1 to 4 for n ciphertexts whose digits are formed
 ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pages, const Dims &d, uint64_t *up,
@@ -744,7 +634,16 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
     const double prods = 2.0 * 2 * d.nd + 2.0 * 3 * pages;
     const double rows1 = (double)n * (d.K + 1) * N;
     prof_begin(ctx, K_KEYIP, 8.0 * rows1 * (d.nd + 2.0 * pages), rows1 * (prods * 7.0 + 2 * pages * 4 * kOpsButterflyF64));
-#define CK_GO(ND)                                                                                                      do {                                                                                                                   const dim3 grid((d.K + 1) * bpl * n);                                                                              if (pages == 1)                                                                                                        hipLaunchKernelGGL((k_wsum_intt8<ND, 1>), grid, dim3(64), 0, ctx->stream, a, up, d, n, ctx->d_pmodq,                                    ctx->d_mod, ctx->d_itwf);                                                                   else                                                                                                                   hipLaunchKernelGGL((k_wsum_intt8<ND, 2>), grid, dim3(64), 0, ctx->stream, a, up, d, n, ctx->d_pmodq,                                    ctx->d_mod, ctx->d_itwf);                                                               } while (0)
+#define CK_GO(ND)                                                                                                  \
+    do {                                                                                                           \
+        const dim3 grid((d.K + 1) * bpl * n);                                                                      \
+        if (pages == 1)                                                                                            \
+            hipLaunchKernelGGL((k_wsum_intt8<ND, 1>), grid, dim3(64), 0, ctx->stream, a, up, d, n,                 \
+                               ctx->d_pmodq, ctx->d_mod, ctx->d_itwf);                                             \
+        else                                                                                                       \
+            hipLaunchKernelGGL((k_wsum_intt8<ND, 2>), grid, dim3(64), 0, ctx->stream, a, up, d, n,                 \
+                               ctx->d_pmodq, ctx->d_mod, ctx->d_itwf);                                             \
+    } while (0)
     CK_ND(d.nd, CK_GO);
 #undef CK_GO
     prof_end(ctx, K_KEYIP);
@@ -756,10 +655,10 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
     const double rows2 = (double)polys * (d.K + 1) * N;
     if (!cols) {
         prof_begin(ctx, K_NTT_INV_COL, 16.0 * rows2, rows2 * kOpsButterflyF64 * (d.log_n - 8) / 2);
-#define CK_COL(S)                                                                                                      hipLaunchKernelGGL(k_quot_col<S>, dim3(polys * (d.K + 1) * (256 / (4096u >> S))), dim3(256), 0, ctx->stream, up, a,                        d, pages, qt, ctx->d_mod, ctx->d_itwf)
+#define CK_COL(S)                                                                                                  \
+    hipLaunchKernelGGL(k_quot_col<S>, dim3(polys * (d.K + 1) * (256 / (4096u >> S))), dim3(256), 0, ctx->stream, up, \
+                       a, d, pages, qt, ctx->d_mod, ctx->d_itwf)
         switch (d.log_n) {
-        case 12: CK_COL(4); break;
-        case 13: CK_COL(5); break;
         case 14: CK_COL(6); break;
         case 15: CK_COL(7); break;
         default: CK_COL(8); break;
@@ -801,43 +700,19 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
     const double rows4 = (double)n * level * N;
     prof_begin(ctx, K_MODDOWN, 8.0 * rows4 * (d.nd + 2.0 + 4.0 * pages),
                rows4 * (prods * 7.0 + 2 * pages * (4 * kOpsButterflyF64 + 14.0)));
-#define CK_GO(ND)                                                                                                      do {                                                                                                                   const dim3 grid(level * bpl * n);                                                                                  if (pages == 1)                                                                                                        hipLaunchKernelGGL((k_wsum_fin8<ND, 1>), grid, dim3(64), 0, ctx->stream, a, cw, d, n, qt, ctx->d_mod,                                   ctx->d_twf);                                                                                else                                                                                                                   hipLaunchKernelGGL((k_wsum_fin8<ND, 2>), grid, dim3(64), 0, ctx->stream, a, cw, d, n, qt, ctx->d_mod,                                   ctx->d_twf);                                                                            } while (0)
+#define CK_GO(ND)                                                                                                  \
+    do {                                                                                                           \
+        const dim3 grid(level * bpl * n);                                                                          \
+        if (pages == 1)                                                                                            \
+            hipLaunchKernelGGL((k_wsum_fin8<ND, 1>), grid, dim3(64), 0, ctx->stream, a, cw, d, n, qt,              \
+                               ctx->d_mod, ctx->d_twf);                                                            \
+        else                                                                                                       \
+            hipLaunchKernelGGL((k_wsum_fin8<ND, 2>), grid, dim3(64), 0, ctx->stream, a, cw, d, n, qt,              \
+                               ctx->d_mod, ctx->d_twf);                                                            \
+    } while (0)
     CK_ND(d.nd, CK_GO);
 #undef CK_GO
     prof_end(ctx, K_MODDOWN);
-    HIP_TRY(hipGetLastError());
-    return CKKS_OK;
-}
-
-// n ciphertexts, all of rotated kinds or all of unrotated ones, in exact 128-bit sums
-ckks_status exact_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pages, const Dims &d, bool rot, const Scratch &s,
-                       uint64_t *mem)
-{
-    const size_t N = ctx->n;
-    const uint32_t level = d.L - 1, outs = n * pages;
-    uint64_t *u = mem + s.dig, *v = u + s.u, *work = v + s.v, *res = work + s.work;
-    if (rot) {
-        prof_begin(ctx, K_KEYIP, 8.0 * N * d.ext * n * (d.nd + 1.0 + 2.0 * pages));
-        if (pages == 1)
-            hipLaunchKernelGGL(k_wsum<1>, grid_of(ctx, d.ext, n), dim3(kThreads), 0, ctx->stream, a, u, d, ctx->d_pmodq,
-                               ctx->d_mod);
-        else
-            hipLaunchKernelGGL(k_wsum<2>, grid_of(ctx, d.ext, n), dim3(kThreads), 0, ctx->stream, a, u, d, ctx->d_pmodq,
-                               ctx->d_mod);
-        prof_end(ctx, K_KEYIP);
-        HIP_TRY(hipGetLastError());
-        CK_TRY(ks_moddown(ctx, u, 2 * outs, level, nullptr, 1, nullptr, v, work));
-    } else {
-        prof_begin(ctx, K_ELEM, 8.0 * N * d.L * n * (2.0 + 2.0 * pages));
-        hipLaunchKernelGGL(k_wmul, grid_of(ctx, d.L, n), dim3(kThreads), 0, ctx->stream, a, v, d, pages, ctx->d_mod);
-        prof_end(ctx, K_ELEM);
-        HIP_TRY(hipGetLastError());
-    }
-    CK_TRY(rescale_many(ctx, v, outs, level, res, work));
-    prof_begin(ctx, K_ELEM, 8.0 * N * level * outs * 6.0);
-    hipLaunchKernelGGL(k_emit, grid_of(ctx, 2 * level, outs), dim3(kThreads), 0, ctx->stream, a, res, level, pages,
-                       ctx->log_n, ctx->d_mod);
-    prof_end(ctx, K_ELEM);
     HIP_TRY(hipGetLastError());
     return CKKS_OK;
 }
@@ -874,13 +749,14 @@ ckks_status wsum_run(ckks_ctx *ctx, uint32_t L, uint32_t pages, const WsumKind *
             }
         }
         const Scratch s = scratch_of(ctx, L, n, pages);
-        if (n_rot) CK_TRY(modup_cts(ctx, L, a, n_rot, fast, rows, mem, s.stage_rows, mem + s.dig + s.u + s.v));
+        uint64_t *stage = mem + s.dig, *u = stage + s.stage, *x = u + s.u;
+        if (n_rot) CK_TRY(modup_cts(ctx, L, a, n_rot, mem, stage));
         if (rows)
-            CK_TRY(wsum_blk_sums(ctx, a, n, pages, d, mem + s.dig));
+            CK_TRY(wsum_blk_sums(ctx, a, n, pages, d, u));
         else if (fast)
-            CK_TRY(two_pass_sums(ctx, a, n, pages, d, mem + s.dig, mem + s.dig + s.u));
+            CK_TRY(two_pass_sums(ctx, a, n, pages, d, u, x));
         else
-            CK_TRY(exact_sums(ctx, a, n, pages, d, first, s, mem));
+            CK_TRY(wsum_exact_sums(ctx, a, n, pages, d, first, u, x));
         r0 += n;
     }
     return CKKS_OK;
