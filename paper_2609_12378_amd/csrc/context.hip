@@ -268,6 +268,9 @@ static ckks_status make_conv(ckks_ctx *c, const std::vector<uint32_t> &src, cons
     // centred |y_i| < q_t and the sums stay exact)
     out->f64 = true;
     uint64_t max_src = 0, min_dst = ~0ull;
+    out->below60 = src.size() <= 8;
+    for (uint32_t v : src) out->below60 = out->below60 && c->primes[v] >> 60 == 0;
+    for (uint32_t v : dst) out->below60 = out->below60 && c->primes[v] >> 60 == 0;
     for (uint32_t v : src) {
         out->f64 = out->f64 && c->f64_ok[v];
         max_src = std::max(max_src, c->primes[v]);

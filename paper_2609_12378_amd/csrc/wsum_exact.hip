@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "ops.h"
+#include "sum60.h"
 #include "wsum_args.h"
 
 namespace {
@@ -165,6 +166,71 @@ __global__ __launch_bounds__(kThreads) void k_quot(uint64_t *x, const uint64_t *
     }
 }
 
+// The same with at most 8 special primes and every prime below 2^60 (sum60.h).  The constants, 2^64 times theirs, are staged
+// as halves, so the quotient's w takes its own sums (a ninth product would pass 64 bits in mid).
+__global__ __launch_bounds__(kThreads) void k_quot60(uint64_t *x, const uint64_t *in, Dims d, int ns, uint32_t t_per,
+                                                     const ulonglong2 *__restrict__ qhat_inv,
+                                                     const ulonglong2 *__restrict__ qhat_mod,
+                                                     const ulonglong2 *__restrict__ neg_q,
+                                                     const ulonglong2 *__restrict__ pinv,
+                                                     const ulonglong2 *__restrict__ pmodq, const ModQ *__restrict__ mods)
+{
+    // slot s of the constants: target t0 + s, and the last one, t1 - t0, q_l
+    __shared__ uint2 s_mod[8 * kMaxPrimes], s_neg[kMaxPrimes], s_f[kMaxPrimes];
+    __shared__ uint64_t s_negw[kMaxPrimes];
+    __shared__ Mod60 s_tm[kMaxPrimes];
+    const uint32_t l = d.L - 1, t0 = blockIdx.y * t_per, nt = min(l, t0 + t_per) - t0, poly = blockIdx.z;
+    const uint64_t ql = mods[l].q;
+    for (uint32_t k = threadIdx.x; k < (uint32_t)ns * (nt + 1); k += kThreads) {
+        const uint32_t i = k / (nt + 1), s = k % (nt + 1), t = s < nt ? t0 + s : l;
+        s_mod[i * kMaxPrimes + s] = halves(times_2_64(qhat_mod[i * d.L + t].x, mods[t]));
+    }
+    for (uint32_t s = threadIdx.x; s <= nt; s += kThreads) {
+        const uint32_t t = s < nt ? t0 + s : l;
+        const ModQ m = mods[t];
+        const uint64_t f = times_2_64(ns ? pmodq[t].x : 1, m);
+        s_tm[s] = mod60(m.q);
+        s_neg[s] = halves(ns ? times_2_64(neg_q[t].x, m) : 0);
+        s_f[s] = halves(f);
+        s_negw[s] = submod(0, mulmod(f, ql, m), m.q);
+    }
+    __syncthreads();
+    const uint32_t col = blockIdx.x * kThreads + threadIdx.x;
+    if (col >= (1u << d.log_n)) return;
+    const uint64_t *src = in + ((size_t)poly * d.ext << d.log_n) + col;
+    uint2 y[8];
+    uint32_t neg = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        if (i < ns) {
+            const uint64_t q = mods[d.n_q + i].q;
+            const ulonglong2 c = qhat_inv[i];
+            const uint64_t v = shoup(src[(size_t)(i + 1) << d.log_n], c.x, c.y, q);
+            neg += v > (q >> 1);
+            y[i] = halves(v);
+        }
+    const auto sum = [&](uint32_t s) {
+        Sum60 r;
+        r.add(neg, s_neg[s]);
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (i < ns) r.add(y[i], s_mod[i * kMaxPrimes + s]);
+        return r.value();
+    };
+    uint64_t w = src[0];
+    if (ns) w = shoup(submod(w, redc(sum(nt), s_tm[nt]), ql), pinv[l].x, pinv[l].y, ql);
+    const bool negw = w > (ql >> 1);
+    const uint2 wh = halves(w);
+    for (uint32_t s = 0; s < nt; s++) {
+        Sum60 p;
+        p.add(wh, s_f[s]);
+        const acc128 a = sum(s), b = p.value();
+        const unsigned __int128 r = ((unsigned __int128)a.hi << 64 | a.lo) + ((unsigned __int128)b.hi << 64 | b.lo) +
+                                    (negw ? s_negw[s] : 0);
+        x[(((size_t)poly * l + t0 + s) << d.log_n) + col] = redc(acc128{(uint64_t)r, (uint64_t)(r >> 64)}, s_tm[s]);
+    }
+}
+
 // out = (u - x) f (+ prev) for rings below 2^12 points, x transformed
 __global__ __launch_bounds__(kThreads) void k_finish(Args a, const uint64_t *u, const uint64_t *x, Dims d, uint32_t pages,
                                                      const ulonglong2 *__restrict__ f, const ModQ *__restrict__ mods)
@@ -238,17 +304,21 @@ ckks_status wsum_exact_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t p
 
     const ConvDev none{}, *cd = &none;
     if (rot) CK_TRY(ctx_conv(ctx, (int)level, -1, &cd));
+    bool below60 = d.K <= 8;
+    for (uint32_t i = 0; i < m.n; i++) below60 = below60 && ctx->primes[m.prime[i]] >> 60 == 0;
+    for (uint32_t i = 0; i < level; i++) below60 = below60 && ctx->primes[i] >> 60 == 0;
     // groups of targets until the grid has four waves a SIMD
     const uint32_t blocks = grid_of(ctx, 1, 1, 1).x * polys, groups = std::min(level, std::max(1u, 1024u / blocks));
     const uint32_t t_per = (level + groups - 1) / groups;
     const dim3 grid(grid_of(ctx, 1, 1, 1).x, (level + t_per - 1) / t_per, polys);
     prof_begin(ctx, K_CONV, 8.0 * N * polys * (d.K + 1.0 + level));
-#define CK_QUOT(NS)                                                                                                \
-    hipLaunchKernelGGL(k_quot<NS>, grid, dim3(kThreads), 0, ctx->stream, x, top, d, (int)d.K, t_per, cd->d_qhat_inv, \
+#define CK_QUOT(KERN)                                                                                              \
+    hipLaunchKernelGGL(KERN, grid, dim3(kThreads), 0, ctx->stream, x, top, d, (int)d.K, t_per, cd->d_qhat_inv,     \
                        cd->d_qhat_mod, cd->d_neg_q, ctx->d_pinv, ctx->d_pmodq, ctx->d_mod)
-    if (d.K <= 8) CK_QUOT(8);
-    else if (d.K <= 16) CK_QUOT(16);
-    else CK_QUOT(kMaxPrimes);
+    if (below60) CK_QUOT(k_quot60);
+    else if (d.K <= 8) CK_QUOT(k_quot<8>);
+    else if (d.K <= 16) CK_QUOT(k_quot<16>);
+    else CK_QUOT(k_quot<kMaxPrimes>);
 #undef CK_QUOT
     prof_end(ctx, K_CONV);
     HIP_TRY(hipGetLastError());
