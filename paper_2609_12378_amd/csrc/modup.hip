@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "ckks_internal.h"
+#include "conv_col.h"
 #include "ks_args.h"
 #include "ops.h"
 
@@ -271,12 +272,6 @@ __global__ __launch_bounds__(512) void k_conv_col8(uint64_t *out, const uint64_t
 #undef CK_NS
 }
 
-// masks of the forward stages that reduce (ntt.hip: column output below 2 q, or below 4.3 q from k_conv_col8)
-constexpr unsigned up_col_mask(int logs)
-{
-    return logs == 4 ? 0x0c : logs == 5 ? 0x1c : logs == 6 ? 0x34 : logs == 7 ? 0x74 : 0xd4;
-}
-
 // 3b. forward column pass of the converted rows, own rows left alone
 template <int LOGS>
 __global__ __launch_bounds__(256) void k_up_fcol(uint64_t *data, Blocks bl, const ModQ *__restrict__ mods,
@@ -294,7 +289,7 @@ __global__ __launch_bounds__(256) void k_up_fcol(uint64_t *data, Blocks bl, cons
     double x[kE];
 #pragma unroll
     for (int k = 0; k < kE; k++) x[k] = A::from_u64(base[(size_t)(t + TS * k) * 256]);
-    constexpr unsigned kMask = up_col_mask(LOGS);
+    constexpr unsigned kMask = nttc::up_col_mask(LOGS);
     nttc::fwd_top<true, kMask>(x, tw, 1, ar);
     if (LOGS > 4) {
         nttc::transpose<LOGS, true>(x, lds, col, t);
@@ -302,6 +297,29 @@ __global__ __launch_bounds__(256) void k_up_fcol(uint64_t *data, Blocks bl, cons
     }
 #pragma unroll
     for (int k = 0; k < kE; k++) base[(size_t)(LOGS > 4 ? 16 * t + k : k) * 256] = A::to_raw(x[k]);
+}
+
+// 3. the conversion with the forward column pass (conv_col.h), any ring and number of sources: block (target; entry, block
+// and tile of columns)
+template <int LOGS>
+__global__ __launch_bounds__(256) void k_conv_col16(uint64_t *out, const uint64_t *in, Blocks bl, uint32_t tiles,
+                                                    uint32_t max_tgt, const ModQ *__restrict__ mods,
+                                                    const double *__restrict__ twf)
+{
+    using Tile = nttc::ColTile<LOGS>;
+    __shared__ double lds[Tile::kLds];
+    uint32_t tile, tt;
+    nttc::target_of(max_tgt, tile, tt);
+    const uint32_t e = tile / Tile::kTiles, j = e % bl.nd, r = e / bl.nd, lo = bl.lo(j);
+    if (tile >= tiles || tt >= bl.targets(j)) return;
+    const uint32_t row = bl.out_row(j, tt), prime = bl.out_prime(row);
+    const A ar(mods[prime]);
+    const Tile ct(tile % Tile::kTiles);
+    double x[1][kE];
+    ct.sum(x, in + bl.at(r, lo), bl.log_n, bl.hi(j) - lo, {bl.mod[j] + tt}, {bl.targets(j)}, {ar});
+#pragma unroll
+    for (int k = 0; k < kE; k++) x[0][k] = ar.red(x[0][k]);
+    ct.forward(x[0], out + (((size_t)e * bl.out_rows + row) << bl.log_n), twf + ((size_t)prime << bl.log_n), lds, ar);
 }
 
 // 4. forward row pass, canonical out; a digit's own rows take the polynomial's (own_rows) or are left as they are.  Input below 4.3 q: stages 0, 2, 4, 6
@@ -391,6 +409,20 @@ ckks_status launch_blocks_conv(ckks_ctx *ctx, uint64_t *out, const uint64_t *in,
         else if (cols) CK_CC(false, true);
         else CK_CC(false, false);
 #undef CK_CC
+    } else if (conv_col_few(ctx, count * bl.nd, max_src, max_tgt)) {
+        const uint32_t tiles = count * bl.nd << (ctx->log_n - 12);
+        const dim3 grid((tiles + 7) / 8 * 8 * max_tgt);
+#define CK_CC(S)                                                                                                   \
+    hipLaunchKernelGGL(k_conv_col16<S>, grid, dim3(256), 0, ctx->stream, out, in, bl, tiles, max_tgt, ctx->d_mod,    \
+                       ctx->d_twf)
+        switch (ctx->log_n) {
+        case 12: CK_CC(4); break;
+        case 13: CK_CC(5); break;
+        case 14: CK_CC(6); break;
+        case 15: CK_CC(7); break;
+        default: CK_CC(8); break;
+        }
+#undef CK_CC
     } else {
         // groups of targets until the grid has 2048 blocks of four waves (two waves a SIMD)
         for (uint32_t r0 = 0; r0 < count; r0 += 65535u / bl.nd) {
@@ -462,7 +494,7 @@ ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t 
     if (!conv_cols(ctx, max_src, count, bl)) CK_TRY(launch_col_digits(ctx, digits, count, bl));
     CK_TRY(launch_blocks_conv(ctx, digits, digits, count, bl, max_src, max_tgt, exact8));
     const uint32_t rows = count * bl.nd * bl.ext;
-    if (!conv_fused(ctx, max_src)) {
+    if (!conv_fused(ctx, max_src) && !conv_col_few(ctx, count * bl.nd, max_src, max_tgt)) {
         prof_begin(ctx, K_NTT_FWD_COL, 16.0 * rows * ctx->n);
 #define CK_COL(S)                                                                                                  \
     hipLaunchKernelGGL(k_up_fcol<S>, dim3(rows * (256 / (4096u >> S))), dim3(256), 0, ctx->stream, digits, bl,       \
@@ -501,7 +533,7 @@ ckks_status up_moddown(ckks_ctx *ctx, uint64_t *up, uint32_t polys, uint32_t lev
     bl.mod[0] = cd->d_qhat_mod_f;
     if (!conv_cols(ctx, ctx->n_p, polys, bl)) CK_TRY(launch_col_digits(ctx, up, polys, bl));
     CK_TRY(launch_blocks_conv(ctx, cw, up, polys, bl, ctx->n_p, level + 1, ctx->n_p == 8));
-    if (!conv_fused(ctx, ctx->n_p))
+    if (!conv_fused(ctx, ctx->n_p) && !conv_col_few(ctx, polys, ctx->n_p, level + 1))
         CK_TRY(launch_ntt_fwd_first_pass(ctx, cw, polys, level + 1, limb_range(0, level + 1)));
     return CKKS_OK;
 }

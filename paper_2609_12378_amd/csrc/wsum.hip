@@ -21,6 +21,7 @@
 // (wsum_exact.hip).
 #include <algorithm>
 
+#include "conv_col.h"
 #include "ops.h"
 #include "wsum_args.h"
 
@@ -494,6 +495,43 @@ __global__ __launch_bounds__(256) void k_quot_conv(uint64_t *out, const uint64_t
     }
 }
 
+// 3. The conversion with the forward column pass for N < 2^16 or more than 8 special primes (conv_col.h): block (target;
+// polynomial and tile of columns).  Every target forms w again, from the reads of its own sum.
+template <int LOGS>
+__global__ __launch_bounds__(256) void k_quot_col16(uint64_t *out, const uint64_t *up, Args a, Dims d, uint32_t pages,
+                                                    uint32_t tiles, Quot qt, const ModQ *__restrict__ mods,
+                                                    const double *__restrict__ twf)
+{
+    using Tile = nttc::ColTile<LOGS>;
+    __shared__ double lds[Tile::kLds], s_top[kMaxPrimes];
+    const uint32_t nt = d.L - 1;
+    uint32_t tile, tt;
+    nttc::target_of(nt, tile, tt);
+    if (tile >= tiles) return;
+    const uint32_t p = tile / Tile::kTiles;
+    const bool rot = a.kind[a.ct[p / 2 / pages].kind].rotated;
+    const A top(mods[nt]), ar(mods[tt]);
+    const uint64_t *src = up + ((size_t)p * (d.K + 1) << d.log_n), *rows = src + (1u << d.log_n);
+    const Tile ct(tile % Tile::kTiles);
+    double w[kE], x[kE];
+    if (rot) {
+        if (threadIdx.x < d.K) s_top[threadIdx.x] = top_factor(qt, d, (int)threadIdx.x, top);
+        __syncthreads();
+        double s[2][kE];
+        ct.sum(s, rows, d.log_n, d.K, {s_top, qt.qhat_mod + tt}, {1, d.L}, {top, ar});
+        ct.load(w, src);
+        const double pt = (double)qt.pmodq[tt].x;
+#pragma unroll
+        for (int k = 0; k < kE; k++)
+            x[k] = ar.red(s[1][k] + ar.mul(centre(top, w[k] - top.red(s[0][k])), pt));
+    } else {
+        ct.load(x, src);
+#pragma unroll
+        for (int k = 0; k < kE; k++) x[k] = ar.red(x[k]);
+    }
+    ct.forward(x, out + (((size_t)p * nt + tt) << d.log_n), twf + ((size_t)tt << d.log_n), lds, ar);
+}
+
 // 4. out = (u - NTT(x)) (P q_l)^-1 (+ prev) on the rows below q_l: cw[z P + o][k][l] after the column pass.  Magnitudes in
 // units of q: column-pass rows below 4.3, transformed below 2.6, u below 2.6, products below 2.5: all below 8 q = 2^53.
 template <int ND, int NOUT>
@@ -651,7 +689,9 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
 
     const bool fused = d.log_n == 16 && d.K <= 8;
     // with a block for every CU, no block's targets are split and its columns are transformed where they are converted
+    // (both rules of the conversions, us a call with and without: 772 and 819 for 16 ciphertexts; 130 and 108 for one)
     const bool cols = fused && polys * 16 >= 256;
+    const bool col16 = !fused && conv_col_few(ctx, polys, d.K, level);
     const double rows2 = (double)polys * (d.K + 1) * N;
     if (!cols) {
         prof_begin(ctx, K_NTT_INV_COL, 16.0 * rows2, rows2 * kOpsButterflyF64 * (d.log_n - 8) / 2);
@@ -683,6 +723,18 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
         else if (cols) CK_QC(false, true);
         else CK_QC(false, false);
 #undef CK_QC
+    } else if (col16) {
+        const uint32_t tiles = polys << (d.log_n - 12);
+        const dim3 grid((tiles + 7) / 8 * 8 * level);
+#define CK_QC(S)                                                                                                   \
+    hipLaunchKernelGGL(k_quot_col16<S>, grid, dim3(256), 0, ctx->stream, cw, up, a, d, pages, tiles, qt, ctx->d_mod, \
+                       ctx->d_twf)
+        switch (d.log_n) {
+        case 14: CK_QC(6); break;
+        case 15: CK_QC(7); break;
+        default: CK_QC(8); break;
+        }
+#undef CK_QC
     } else {
         // groups of targets until the grid has 2048 blocks of four waves
         const uint32_t blocks = polys * (ctx->n / 256), groups = std::min(level, std::max(1u, 2048u / blocks));
@@ -695,7 +747,7 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
     }
     prof_end(ctx, K_CONV);
     HIP_TRY(hipGetLastError());
-    if (!fused) CK_TRY(launch_ntt_fwd_first_pass(ctx, cw, polys, level, limb_range(0, level)));
+    if (!fused && !col16) CK_TRY(launch_ntt_fwd_first_pass(ctx, cw, polys, level, limb_range(0, level)));
 
     const double rows4 = (double)n * level * N;
     prof_begin(ctx, K_MODDOWN, 8.0 * rows4 * (d.nd + 2.0 + 4.0 * pages),
