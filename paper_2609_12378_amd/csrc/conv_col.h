@@ -17,12 +17,6 @@ inline bool conv_col_few(const ckks_ctx *ctx, uint32_t polys, uint32_t sources, 
 
 namespace nttc {
 
-// masks of the forward stages that reduce (ntt.hip: column output below 2 q, or below 4.3 q from k_conv_col8)
-constexpr unsigned up_col_mask(int logs)
-{
-    return logs == 4 ? 0x0c : logs == 5 ? 0x1c : logs == 6 ? 0x34 : logs == 7 ? 0x74 : 0xd4;
-}
-
 template <int LOGS>
 struct ColTile {
     static constexpr uint32_t TS = (1u << LOGS) / 16, kCols = 4096u >> LOGS, kTiles = 256 / kCols;   // tiles a row
@@ -66,10 +60,10 @@ struct ColTile {
 #pragma unroll
             for (int k = 0; k < kE; k++) x[s][k] = acc[s][k].value(ar[s]);
     }
-    // forward column pass of reduced values, raw doubles out
+    // forward column pass of reduced values, the stages of kMask reducing; raw doubles out
+    template <unsigned kMask>
     __device__ void forward(double (&x)[kE], uint64_t *row, const double *tw, double *lds, const Ar<true> &ar) const
     {
-        constexpr unsigned kMask = up_col_mask(LOGS);
         fwd_top<true, kMask>(x, tw, 1, ar);
         if (LOGS > 4) {
             transpose<LOGS, true>(x, lds, col, t);

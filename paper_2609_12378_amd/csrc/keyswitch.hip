@@ -99,7 +99,8 @@ __global__ __launch_bounds__(kThreads) void k_conv(const uint64_t *in, uint32_t 
 }
 
 // The same conversion of at most 8 sources with every prime below 2^60 (sum60.h), the targets' constants [Qhat_i]_t 2^64
-// and [-Q_I]_t 2^64 as halves: 1190 -> 850 cycles a wave and target at N = 2^16 (two ciphertexts of 37 limbs, a digit 36.6 -> 26.2 us).
+// and [-Q_I]_t 2^64 as halves: a digit of two ciphertexts of 37 limbs at N = 2^16 36.6 -> 26.2 us, 92 instructions a
+// coefficient and target.
 __global__ __launch_bounds__(kThreads) void k_conv60(const uint64_t *in, uint32_t in_stride, uint64_t *out,
                                                      uint32_t out_stride, uint32_t split, uint32_t skip, ConvArgs a,
                                                      const ulonglong2 *__restrict__ qhat_inv,

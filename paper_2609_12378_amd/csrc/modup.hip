@@ -3,11 +3,12 @@
 //
 // A conversion Conv(x)_t = sum_i y_i [Qhat_i]_t starts from the centred digits y_i = [x_i Qhat_i^-1]: the inverse
 // transform writes them itself, the constant folded into its last stage's factor N^-1.  A ModUp of any number of
-// ciphertexts is four launches for all digits together at N = 2^16, five below:
+// ciphertexts is three to five launches for all digits together:
 //   1. row pass of the inverse transform of every limb, from the polynomial into the limb's row of its digit;
-//   2. column pass, leaving the digits y there;
-//   3. conversion of every digit, fused with the forward column pass where columns have 256 points;
-//   4. forward row pass, which in the digits' own rows (no longer needed for y) puts the polynomial itself.
+//   2. column pass, leaving the digits y there (within 3 at N = 2^16 with a block for every CU);
+//   3. conversion of every digit, fused with the forward column pass at N = 2^16 and where its reads are few;
+//   4. forward row pass, which in the digits' own rows (no longer needed for y) puts the polynomial itself, unless the
+//      caller reads those from the polynomial.
 // One launch per digit and step and copies of the limbs in and out were 6 nd + 2 launches: an evaluation step with two
 // key switches at N = 2^16 (13 limbs, two digits) took 378 us with those and 316 us so, 32 rotations sharing a ModUp
 // (24 limbs, three digits) 1640 and 1536 us.
@@ -155,7 +156,8 @@ struct ConvLds {
     nttc::InvConst src[8];
 };
 // COLS: `in` holds the sources after the row pass of their inverse transform, and each source's column pass is run here
-// as well, its row asked for while the one before is transformed.
+// as well, its row asked for while the one before is transformed: the ModDown of 32 rotations 107 us of column pass and
+// 403 us become 11 (one ciphertext's ModUp) and 453, two passes over the rows fewer; 4096 waves at 62% of the issue slots.
 template <int NS, bool COLS>
 __device__ __forceinline__ void conv_col8(uint64_t *out, const uint64_t *in, const Blocks &bl, uint32_t t_per,
                                           const ModQ *__restrict__ mods, const double *__restrict__ twf,
@@ -272,6 +274,12 @@ __global__ __launch_bounds__(512) void k_conv_col8(uint64_t *out, const uint64_t
 #undef CK_NS
 }
 
+// masks of the forward stages that reduce (ntt.hip: column output below 2 q, or below 4.3 q from k_conv_col8)
+constexpr unsigned up_col_mask(int logs)
+{
+    return logs == 4 ? 0x0c : logs == 5 ? 0x1c : logs == 6 ? 0x34 : logs == 7 ? 0x74 : 0xd4;
+}
+
 // 3b. forward column pass of the converted rows, own rows left alone
 template <int LOGS>
 __global__ __launch_bounds__(256) void k_up_fcol(uint64_t *data, Blocks bl, const ModQ *__restrict__ mods,
@@ -289,7 +297,7 @@ __global__ __launch_bounds__(256) void k_up_fcol(uint64_t *data, Blocks bl, cons
     double x[kE];
 #pragma unroll
     for (int k = 0; k < kE; k++) x[k] = A::from_u64(base[(size_t)(t + TS * k) * 256]);
-    constexpr unsigned kMask = nttc::up_col_mask(LOGS);
+    constexpr unsigned kMask = up_col_mask(LOGS);
     nttc::fwd_top<true, kMask>(x, tw, 1, ar);
     if (LOGS > 4) {
         nttc::transpose<LOGS, true>(x, lds, col, t);
@@ -319,11 +327,11 @@ __global__ __launch_bounds__(256) void k_conv_col16(uint64_t *out, const uint64_
     ct.sum(x, in + bl.at(r, lo), bl.log_n, bl.hi(j) - lo, {bl.mod[j] + tt}, {bl.targets(j)}, {ar});
 #pragma unroll
     for (int k = 0; k < kE; k++) x[0][k] = ar.red(x[0][k]);
-    ct.forward(x[0], out + (((size_t)e * bl.out_rows + row) << bl.log_n), twf + ((size_t)prime << bl.log_n), lds, ar);
+    ct.template forward<up_col_mask(LOGS)>(x[0], out + (((size_t)e * bl.out_rows + row) << bl.log_n), twf + ((size_t)prime << bl.log_n), lds, ar);
 }
 
-// 4. forward row pass, canonical out; a digit's own rows take the polynomial's (own_rows) or are left as they are.  Input below 4.3 q: stages 0, 2, 4, 6
-// reducing keep every value below 7 q.
+// 4. forward row pass, canonical out; a digit's own rows take the polynomial's (own_rows) or are left as they are.
+// Input below 4.3 q: stages 0, 2, 4, 6 reducing keep every value below 7 q.
 constexpr unsigned kUpRowMask = 0x55;
 __global__ __launch_bounds__(128) void k_up_frow(uint64_t *data, PolySrc c1, Blocks bl, bool own_rows,
                                                  const ModQ *__restrict__ mods, const double *__restrict__ twf)

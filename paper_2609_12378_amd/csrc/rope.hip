@@ -16,6 +16,8 @@
 namespace {
 
 constexpr int kThreads = 256;
+// Tables are made once for a position and serve every layer and head, so they are plain element-wise kernels around the
+// encoder's transforms.
 // cos and sin of positions[i] * inv_freq[k], times factor.  The product is taken with its rounding error e (an FMA) and
 // the angles added, so a far position's angle is as exact as a near one's.
 __global__ __launch_bounds__(kThreads) void k_cos_sin(const int64_t *positions, const double *inv_freq, uint32_t half,

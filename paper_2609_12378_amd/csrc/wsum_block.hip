@@ -4,8 +4,9 @@
 //   2. k_blk_wtop   the rows q_l and P to coefficients: U P^-1 and the centred digits y_i;
 //   3. k_blk_wfin   a block forms its row of the conversion, x_t = sum_i y_i [P / p_i]_t + P w with w the centred top
 //      coefficient of the quotient by P, transforms it and writes (u - NTT(x)) (P q_l)^-1 (+ prev).
-// With the two launches of the ModUp that is five; through the ModDown, the rescale and the additions it was eight.  A call
-// of a few ciphertexts here is bounded by its launches, 4-5 us each.
+// With the two launches of the ModUp that is five; through the ModDown, the rescale and the additions it was eight.  Few
+// ciphertexts are bounded by one row's latency a launch: one of 4 limbs at N = 2^12 takes 4, 7 and 11 us in the three (35 us
+// a call, as long as the host takes to issue it), three of 6 limbs at 2^13 8, 10 and 17 (56 us a call).
 #include "ntt_block.h"
 #include "ops.h"
 #include "wsum_args.h"

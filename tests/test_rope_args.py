@@ -160,3 +160,20 @@ def test_the_transposed_rotation_is_the_gradient(pairing):
         d[i] = 1.0
         diff = np.sum(w * (plain_rope(x + d, np.cos(a), np.sin(a), pairing) - plain_rope(x, np.cos(a), np.sin(a), pairing)))
         assert abs(diff - grad[i]) < 1e-12
+
+
+@pytest.mark.parametrize("logs", [6, 7, 8])
+def test_the_sums_column_pass_stays_in_its_bounds(logs):
+    """In units of q: a reducing stage maps a bound b to 1 + 0.375 b, a lazy one to 0.5 + 1.375 b; the converted values are
+    at most q / 2, every value stays below 8 q and the rows that the row pass takes below its 4.3 q."""
+    import os
+    import re
+    path = os.path.join(os.path.dirname(__file__), "..", "paper_2609_12378_amd", "csrc", "wsum.hip")
+    body = re.search(r"constexpr unsigned quot_col_mask\(int logs\)\s*\{\s*return (.*?);", open(path).read(), re.S).group(1)
+    masks = {int(k): int(v, 16) for k, v in re.findall(r"== (\d) \? (0x[0-9a-f]+)", body)}
+    mask = masks.get(logs, int(re.search(r"(0x[0-9a-f]+)\s*$", body).group(1), 16))
+    b = peak = 0.5
+    for s in range(logs):
+        b = (1 + 0.375 * b if (mask >> s) & 1 else 1.375 * b + 0.5) * (1 + 2.0 ** -40)
+        peak = max(peak, b)
+    assert peak < 8 and b < 2
