@@ -125,3 +125,71 @@ def test_two_contexts_at_once():
         for i in range(2):
             for g, w in zip(run[i], want[i]):
                 assert np.array_equal(to_host(g.data), w)
+
+
+@pytest.mark.parametrize("chain,T,hd,limbs", [((12, 4, 2, 2, 36), 16, 64, 4), ((14, 6, 2, 3, 50), 64, 128, 5),
+                                              ((16, 4, 2, 2, 59), 128, 128, 3)], ids=lambda c: "n%d" % c[0]
+                         if isinstance(c, tuple) else str(c))
+def test_a_ciphertext_given_twice(chain, T, hd, limbs):
+    """Inputs may repeat: two outputs of one ciphertext, and one ciphertext as the key and the value of two heads."""
+    from paper_2609_12378_amd import Buf
+    ctx, ck = ring(*chain)
+    steps, moved = term_steps(ck.n, T, hd, "tm", "half"), term_steps(ck.n, T, hd, "tm", "half", 2)
+    keys = random_keys(ck, steps + moved, 51)
+    dk = dev_keys(keys)
+    cos, sin = (to_dev(x) for x in angles(T, hd // 2, 52))
+    x = random_cts(ck, limbs, 1, 53)[0]
+    b = Buf(to_dev(x), 2.0 ** 40)
+    tables = ctx.rope_tables(cos, sin, T, hd, hd, limbs)
+    want = weighted(ck, x, steps, keys, to_host(tables))
+    for out in ctx.rope([b, b], tables, T, hd, hd, dk):
+        same(out.data, want, "rope")
+    ct = ctx.cache_tables(cos[:3].contiguous(), sin[:3].contiguous(), T, hd, hd, 2, 3, limbs)
+    old = random_cts(ck, limbs - 1, 4, 54)
+    pools = [[Buf(to_dev(a), 2.0 ** 40) for a in old] for _ in range(2)]
+    ctx.cache_append([b, b], [b, b], ct, T, hd, hd, 2, 3, dk, *pools, [[1], [3]], fork=[0, 0])
+    tab = to_host(ct)[0]
+    for i, (st, t) in enumerate([(moved, tab[:3]), (moved[:1], tab[3:])]):
+        want = ck.ct_add(weighted(ck, x, st, keys, t), old[0])
+        for p in (1, 3):
+            same(pools[i][p].data, want, "page %d" % p)
+        for p in (0, 2):
+            same(pools[i][p].data, old[p], "page %d" % p)
+
+
+@pytest.mark.parametrize("chain,T,limbs,count", [((16, 4, 2, 2, 50), 128, 4, 9), ((16, 4, 3, 2, 59), 128, 3, 2),
+                                                 ((15, 6, 2, 3, 50), 128, 5, 2)], ids=lambda c: "n%d-b%d" % (c[0], c[4])
+                         if isinstance(c, tuple) else str(c))
+def test_large_rings_captured(chain, T, limbs, count):
+    import torch
+    from paper_2609_12378_amd import Buf, Context
+    eager, ck = ring(*chain)
+    hd = 128
+    stream = torch.cuda.Stream()
+    ctx = Context(ck.log_n, ck.n_q, ck.n_p, ck.dnum, q=eager.q, p=eager.p, stream=stream)
+    keys = dev_keys(random_keys(ck, term_steps(ck.n, T, hd, "tm", "half"), 61))
+    cos, sin = (to_dev(x) for x in angles(T, hd // 2, 62))
+    tables = eager.rope_tables(cos, sin, T, hd, hd, limbs)
+    x = [Buf(torch.zeros((2, limbs, ck.n), dtype=torch.uint64, device="cuda"), 1.0) for _ in range(count)]
+    ws = torch.empty(ctx.workspace_bytes(ctx.OP_ROPE, (limbs, count)) // 8, dtype=torch.uint64, device="cuda")
+    ctx.set_workspace(ws)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        ctx.rope(x, tables, T, hd, hd, keys)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out = ctx.rope(x, tables, T, hd, hd, keys)
+    torch.cuda.synchronize()
+    for r in range(3):
+        for b, a in zip(x, random_cts(ck, limbs, count, 63 + r)):
+            b.data.copy_(to_dev(a))
+        want = eager.rope(x, tables, T, hd, hd, keys)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for o, w in zip(out, want):
+            same(o.data, to_host(w.data), "replay %d" % r)
+        junk = torch.randn(1 << 22, device="cuda").sum()
+        del junk
+    del graph
