@@ -98,20 +98,44 @@ __global__ __launch_bounds__(kThreads) void k_conv(const uint64_t *in, uint32_t 
     }
 }
 
+// Conversions that one launch of k_conv60 does: conversion j reads from row in_row[j] of each polynomial, writes to out_row[j].
+constexpr uint32_t kConv60 = 8;
+struct Conv60Args {
+    uint32_t n, groups;
+    uint32_t in_row[kConv60], out_row[kConv60], split[kConv60], skip[kConv60];
+    const ulonglong2 *qhat_inv[kConv60], *qhat_mod[kConv60], *neg_q[kConv60];
+    ConvArgs c[kConv60];
+    void set(uint32_t j, const ConvDev &cd, uint32_t in_row_, uint32_t out_row_, uint32_t split_, uint32_t skip_)
+    {
+        in_row[j] = in_row_;
+        out_row[j] = out_row_;
+        split[j] = split_;
+        skip[j] = skip_;
+        qhat_inv[j] = cd.d_qhat_inv;
+        qhat_mod[j] = cd.d_qhat_mod;
+        neg_q[j] = cd.d_neg_q;
+        c[j].ns = cd.ns;
+        c[j].nt = cd.nt;
+        for (int i = 0; i < cd.ns; i++) c[j].src[i] = cd.src[i];
+        for (int t = 0; t < cd.nt; t++) c[j].dst[t] = cd.dst[t];
+    }
+};
+
 // The same conversion of at most 8 sources with every prime below 2^60 (sum60.h), the targets' constants [Qhat_i]_t 2^64
-// and [-Q_I]_t 2^64 as halves: a digit of two ciphertexts of 37 limbs at N = 2^16 36.6 -> 26.2 us, 92 instructions a
-// coefficient and target.
+// and [-Q_I]_t 2^64 as halves; blockIdx.z = conversion, group of t_per targets.  The five digits of two ciphertexts of 37
+// limbs at N = 2^16: 183 us in exact 128-bit sums, 131 so, 82 in one launch for all five.
 __global__ __launch_bounds__(kThreads) void k_conv60(const uint64_t *in, uint32_t in_stride, uint64_t *out,
-                                                     uint32_t out_stride, uint32_t split, uint32_t skip, ConvArgs a,
-                                                     const ulonglong2 *__restrict__ qhat_inv,
-                                                     const ulonglong2 *__restrict__ qhat_mod,
-                                                     const ulonglong2 *__restrict__ neg_q,
+                                                     uint32_t out_stride, Conv60Args args,
                                                      const ModQ *__restrict__ mods, uint32_t log_n, uint32_t t_per)
 {
     __shared__ uint2 s_mod[8 * kMaxPrimes], s_neg[kMaxPrimes];
     __shared__ Mod60 s_tm[kMaxPrimes];
+    const uint32_t j = blockIdx.z / args.groups;
+    const ConvArgs &a = args.c[j];
+    const ulonglong2 *qhat_inv = args.qhat_inv[j], *qhat_mod = args.qhat_mod[j];
     const int ns = a.ns, nt = a.nt;
-    const int t0 = (int)(blockIdx.z * t_per), t1 = min(nt, t0 + (int)t_per);
+    const int t0 = (int)(blockIdx.z % args.groups * t_per), t1 = min(nt, t0 + (int)t_per);
+    if (t0 >= nt) return;
     for (int k = threadIdx.x; k < ns * (t1 - t0); k += kThreads) {
         const int i = k / (t1 - t0), t = t0 + k % (t1 - t0);
         s_mod[i * kMaxPrimes + t] = halves(times_2_64(qhat_mod[i * nt + t].x, mods[a.dst[t]]));
@@ -119,14 +143,14 @@ __global__ __launch_bounds__(kThreads) void k_conv60(const uint64_t *in, uint32_
     for (int t = t0 + threadIdx.x; t < t1; t += kThreads) {
         const ModQ m = mods[a.dst[t]];
         s_tm[t] = mod60(m.q);
-        s_neg[t] = halves(times_2_64(neg_q[t].x, m));
+        s_neg[t] = halves(times_2_64(args.neg_q[j][t].x, m));
     }
     __syncthreads();
     const uint32_t n = 1u << log_n;
     const uint32_t col = blockIdx.x * kThreads + threadIdx.x;
     const uint32_t poly = blockIdx.y;
     if (col >= n) return;
-    const uint64_t *src = in + ((size_t)poly * in_stride << log_n) + col;
+    const uint64_t *src = in + (((size_t)poly * in_stride + args.in_row[j]) << log_n) + col;
     uint2 y[8];
     uint32_t neg = 0;
 #pragma unroll
@@ -139,7 +163,8 @@ __global__ __launch_bounds__(kThreads) void k_conv60(const uint64_t *in, uint32_
             y[i] = halves(v);
         }
     }
-    uint64_t *dst = out + ((size_t)poly * out_stride << log_n) + col;
+    uint64_t *dst = out + (((size_t)poly * out_stride + args.out_row[j]) << log_n) + col;
+    const uint32_t split = args.split[j], skip = args.skip[j];
     for (int t = t0; t < t1; t++) {
         Sum60 s;
         s.add(neg, s_neg[t]);
@@ -149,6 +174,26 @@ __global__ __launch_bounds__(kThreads) void k_conv60(const uint64_t *in, uint32_
         const uint32_t row = t < (int)split ? t : t + skip;
         dst[(size_t)row << log_n] = redc(s.value(), s_tm[t]);
     }
+}
+
+// the conversions of `args` of each polynomial: the targets split until the grid has 4096 waves
+void launch_conv60(ckks_ctx *ctx, Conv60Args &args, const uint64_t *in, uint32_t in_stride, uint64_t *out,
+                   uint32_t out_stride, uint32_t polys)
+{
+    uint32_t nt = 1;
+    double rows = 0;
+    for (uint32_t j = 0; j < args.n; j++) {
+        nt = std::max(nt, (uint32_t)args.c[j].nt);
+        rows += args.c[j].ns + args.c[j].nt;
+    }
+    const uint32_t cols = (ctx->n + kThreads - 1) / kThreads;
+    const size_t waves = (size_t)((ctx->n + 63) / 64) * polys * args.n;
+    const uint32_t groups = (uint32_t)std::min<size_t>(nt, (4096 + waves - 1) / waves), t_per = (nt + groups - 1) / groups;
+    args.groups = (nt + t_per - 1) / t_per;
+    prof_begin(ctx, K_CONV, 8.0 * polys * rows * ctx->n);
+    hipLaunchKernelGGL(k_conv60, dim3(cols, polys, args.n * args.groups), dim3(kThreads), 0, ctx->stream, in, in_stride,
+                       out, out_stride, args, ctx->d_mod, ctx->log_n, t_per);
+    prof_end(ctx, K_CONV);
 }
 
 // The same conversion in fp64 (every prime below 2^50): y_i = x_i * qhat_inv_i mod s_i (|mul| < 0.875 s_i for
@@ -690,6 +735,14 @@ __global__ __launch_bounds__(kThreads) void k_moddown_finish_batch(RotArgs ra, c
 ckks_status launch_conv(ckks_ctx *ctx, const ConvDev *cd, const uint64_t *in, uint32_t in_stride, uint64_t *out,
                         uint32_t out_stride, uint32_t split, uint32_t skip, uint32_t polys)
 {
+    if (cd->below60 && !(cd->f64 && !ctx->int_only)) {
+        Conv60Args c{};
+        c.n = 1;
+        c.set(0, *cd, 0, 0, split, skip);
+        launch_conv60(ctx, c, in, in_stride, out, out_stride, polys);
+        HIP_TRY(hipGetLastError());
+        return CKKS_OK;
+    }
     ConvArgs a;
     a.ns = cd->ns;
     a.nt = cd->nt;
@@ -733,10 +786,7 @@ ckks_status launch_conv(ckks_ctx *ctx, const ConvDev *cd, const uint64_t *in, ui
             CK_CONVF(8);
         else
             CK_CONVF(16);
-    } else if (cd->below60)
-        hipLaunchKernelGGL(k_conv60, grid1, block, 0, ctx->stream, in, in_stride, out, out_stride, split, skip, a,
-                           cd->d_qhat_inv, cd->d_qhat_mod, cd->d_neg_q, ctx->d_mod, ctx->log_n, t_per);
-    else if (a.ns <= 4)
+    } else if (a.ns <= 4)
         hipLaunchKernelGGL(k_conv<4>, grid1, block, 0, ctx->stream, in, in_stride, out, out_stride, split, skip, a,
                            cd->d_qhat_inv, cd->d_qhat_mod, cd->d_neg_q, ctx->d_mod, ctx->log_n, t_per);
     else if (a.ns <= 8)
@@ -1045,11 +1095,24 @@ ckks_status ks_modup_staged(ckks_ctx *ctx, uint64_t *c1, uint32_t count, uint32_
     const uint32_t L = level + 1, ext = L + ctx->n_p, nd = n_digits(ctx, level);
     const size_t N = ctx->n;
     CK_TRY(launch_ntt(ctx, c1, count * L, limb_range(0, L), true));
+    Conv60Args c{};
     for (uint32_t j = 0; j < nd; j++) {
         const uint32_t lo = digit_lo(ctx, j), hi = digit_hi(ctx, j, level);
         const ConvDev *cd;
         CK_TRY(ctx_conv(ctx, (int)level, (int)j, &cd));
-        CK_TRY(launch_conv(ctx, cd, c1 + lo * N, L, digits + (size_t)j * ext * N, nd * ext, lo, hi - lo, count));
+        if (!cd->below60 || (cd->f64 && !ctx->int_only)) {
+            CK_TRY(launch_conv(ctx, cd, c1 + lo * N, L, digits + (size_t)j * ext * N, nd * ext, lo, hi - lo, count));
+            continue;
+        }
+        c.set(c.n++, *cd, lo, j * ext, lo, hi - lo);
+        if (c.n < kConv60 && j + 1 < nd) continue;
+        launch_conv60(ctx, c, c1, L, digits, nd * ext, count);
+        HIP_TRY(hipGetLastError());
+        c.n = 0;
+    }
+    if (c.n) {   // the last digit took another kernel
+        launch_conv60(ctx, c, c1, L, digits, nd * ext, count);
+        HIP_TRY(hipGetLastError());
     }
     LimbMap m = limb_range(0, L);
     for (uint32_t i = 0; i < ctx->n_p; i++) m.prime[m.n++] = (uint8_t)(ctx->n_q + i);

@@ -395,6 +395,13 @@ bool conv_cols(const ckks_ctx *ctx, uint32_t max_src, uint32_t count, const Bloc
     return conv_fused(ctx, max_src) && count * 16 * bl.nd >= 256;
 }
 
+// the conversion takes the forward column pass along (k_conv_col16).  A ModDown's does so below 2^15 alone: above, the
+// launches of a rotation that the event profiler reports stay those of a pass of its own.
+bool conv_col(const ckks_ctx *ctx, const Blocks &bl, uint32_t count, uint32_t max_src, uint32_t max_tgt)
+{
+    return !(bl.down && ctx->log_n > 14) && conv_col_few(ctx, count * bl.nd, max_src, max_tgt);
+}
+
 // the conversion of every block of `count` entries; max_src, max_tgt over the blocks; the sources are digits, or (conv_cols)
 // rows after the row pass of their inverse transform
 ckks_status launch_blocks_conv(ckks_ctx *ctx, uint64_t *out, const uint64_t *in, uint32_t count, const Blocks &bl,
@@ -417,7 +424,7 @@ ckks_status launch_blocks_conv(ckks_ctx *ctx, uint64_t *out, const uint64_t *in,
         else if (cols) CK_CC(false, true);
         else CK_CC(false, false);
 #undef CK_CC
-    } else if (conv_col_few(ctx, count * bl.nd, max_src, max_tgt)) {
+    } else if (conv_col(ctx, bl, count, max_src, max_tgt)) {
         const uint32_t tiles = count * bl.nd << (ctx->log_n - 12);
         const dim3 grid((tiles + 7) / 8 * 8 * max_tgt);
 #define CK_CC(S)                                                                                                   \
@@ -502,7 +509,7 @@ ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t 
     if (!conv_cols(ctx, max_src, count, bl)) CK_TRY(launch_col_digits(ctx, digits, count, bl));
     CK_TRY(launch_blocks_conv(ctx, digits, digits, count, bl, max_src, max_tgt, exact8));
     const uint32_t rows = count * bl.nd * bl.ext;
-    if (!conv_fused(ctx, max_src) && !conv_col_few(ctx, count * bl.nd, max_src, max_tgt)) {
+    if (!conv_fused(ctx, max_src) && !conv_col(ctx, bl, count, max_src, max_tgt)) {
         prof_begin(ctx, K_NTT_FWD_COL, 16.0 * rows * ctx->n);
 #define CK_COL(S)                                                                                                  \
     hipLaunchKernelGGL(k_up_fcol<S>, dim3(rows * (256 / (4096u >> S))), dim3(256), 0, ctx->stream, digits, bl,       \
@@ -541,7 +548,7 @@ ckks_status up_moddown(ckks_ctx *ctx, uint64_t *up, uint32_t polys, uint32_t lev
     bl.mod[0] = cd->d_qhat_mod_f;
     if (!conv_cols(ctx, ctx->n_p, polys, bl)) CK_TRY(launch_col_digits(ctx, up, polys, bl));
     CK_TRY(launch_blocks_conv(ctx, cw, up, polys, bl, ctx->n_p, level + 1, ctx->n_p == 8));
-    if (!conv_fused(ctx, ctx->n_p) && !conv_col_few(ctx, polys, ctx->n_p, level + 1))
+    if (!conv_fused(ctx, ctx->n_p) && !conv_col(ctx, bl, polys, ctx->n_p, level + 1))
         CK_TRY(launch_ntt_fwd_first_pass(ctx, cw, polys, level + 1, limb_range(0, level + 1)));
     return CKKS_OK;
 }
