@@ -309,8 +309,9 @@ ckks_status wsum_exact_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t p
     bool below60 = d.K <= 8;
     for (uint32_t i = 0; i < m.n; i++) below60 = below60 && ctx->primes[m.prime[i]] >> 60 == 0;
     for (uint32_t i = 0; i < level; i++) below60 = below60 && ctx->primes[i] >> 60 == 0;
-    // groups of targets until the grid has four waves a SIMD
-    const uint32_t blocks = grid_of(ctx, 1, 1, 1).x * polys, groups = std::min(level, std::max(1u, 1024u / blocks));
+    // groups of targets until the grid has eight waves a SIMD (four polynomials of 36 targets: 53 us undivided, 48 in two
+    // groups, 55 in four, each of which forms the digits and w again)
+    const uint32_t blocks = grid_of(ctx, 1, 1, 1).x * polys, groups = std::min(level, std::max(1u, 2048u / blocks));
     const uint32_t t_per = (level + groups - 1) / groups;
     const dim3 grid(grid_of(ctx, 1, 1, 1).x, (level + t_per - 1) / t_per, polys);
     prof_begin(ctx, K_CONV, 8.0 * N * polys * (d.K + 1.0 + level));
