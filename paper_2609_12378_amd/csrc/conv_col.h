@@ -1,15 +1,16 @@
-// A basis conversion with the forward column pass of its target, 16 points of a 2^LOGS-point column a thread (256 threads,
-// 4096 / 2^LOGS columns).  Each target reads its tile of the sources again, which no registers hold, so ring and number of
-// sources are free; with the targets of a tile one after the other on one XCD those reads meet its L2.
+// A basis conversion with the forward column pass of its target, 16 points of a 2^LOGS-point column a thread (256
+// threads, 4096 / 2^LOGS columns).  Each target reads its tile of the sources again, which no registers hold, so ring
+// and number of sources are free; with the targets of a tile one after the other on one XCD those reads meet its L2.
 #pragma once
 #include "ckks_internal.h"
 #include "ntt_core.h"
 
-// Worth it while the reads, tiles of 4096 coefficients times targets times sources, are few.  Calls of hoisted rotations,
-// us in one launch and in two: 59 and 67 (one rotation at N = 2^14, 11 limbs in digits of 4), 215 and 231 (32 of them,
-// 11264 reads), 194 and 196 (8 at N = 2^15, 16 limbs, 8 special primes: 16384), 260 and 251 (8 at N = 2^16, 10 limbs, 10
-// special primes: 25600), 1990 and 1771 (32 at N = 2^16, 24 limbs, 12 special primes: 294912).  The weighted sums' quotient
-// (five ciphertexts at N = 2^14, 9 limbs, 4 special primes): 15.8 us in place of 10.7 and 7.8.
+// Worth it while the reads, tiles of 4096 coefficients times targets times sources, are few.  Calls of hoisted
+// rotations, us in one launch and in two: 59 and 67 (one rotation at N = 2^14, 11 limbs in digits of 4), 215 and 231
+// (32 of them, 11264 reads), 194 and 196 (8 at N = 2^15, 16 limbs, 8 special primes: 16384), 260 and 251 (8 at N =
+// 2^16, 10 limbs, 10 special primes: 25600), 1990 and 1771 (32 at N = 2^16, 24 limbs, 12 special primes: 294912).  The
+// weighted sums' quotient (five ciphertexts at N = 2^14, 9 limbs, 4 special primes): 15.8 us in place of 10.7 and 7.8.
+// (Rotations: ModUps and ModDowns both.)
 inline bool conv_col_few(const ckks_ctx *ctx, uint32_t polys, uint32_t sources, uint32_t targets)
 {
     return ((size_t)polys << (ctx->log_n - 12)) * targets * sources <= 16384;
@@ -31,8 +32,8 @@ struct ColTile {
 #pragma unroll
         for (int k = 0; k < kE; k++) x[k] = Ar<true>::from_raw(row[at + (size_t)(t + TS * k) * 256]);
     }
-    // S sums x[s] = sum_i (row src + i N) m[s][i stride[s]] modulo ar[s], i < ns, lazily reduced (GridSum::value); the next
-    // row is asked for ahead
+    // S sums x[s] = sum_i (row src + i N) m[s][i stride[s]] modulo ar[s], i < ns, lazily reduced (GridSum::value); the
+    // next row is asked for ahead
     template <int S>
     __device__ void sum(double (&x)[S][kE], const uint64_t *src, uint32_t log_n, uint32_t ns,
                         const double *const (&m)[S], const uint32_t (&stride)[S], const Ar<true> (&ar)[S]) const

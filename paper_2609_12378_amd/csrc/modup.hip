@@ -95,9 +95,9 @@ __global__ __launch_bounds__(256) void k_up_col(uint64_t *data, Blocks bl, const
     for (int k = 0; k < kE; k++) base[(size_t)(t + TS * k) * 256] = A::to_raw(ar.red(x[k]));
 }
 
-// 3. conversion alone (N1 < 256, or more than 8 sources): thread = one coefficient, blockIdx.y a group of t_per targets,
-// blockIdx.z (entry, block); canonical residues out.  All loads issue before the first is used: short blocks repeat
-// their last source.
+// 3. conversion alone (N1 < 256, or more than 8 sources): thread = one coefficient, blockIdx.y a group of t_per
+// targets, blockIdx.z (entry, block); canonical residues out.  All loads issue before the first is used: short blocks
+// repeat their last source.
 template <int NS>
 __global__ __launch_bounds__(256) void k_up_conv(uint64_t *out, const uint64_t *in, Blocks bl, uint32_t t_per,
                                                  const ModQ *__restrict__ mods)
@@ -157,7 +157,8 @@ struct ConvLds {
 };
 // COLS: `in` holds the sources after the row pass of their inverse transform, and each source's column pass is run here
 // as well, its row asked for while the one before is transformed: the ModDown of 32 rotations 107 us of column pass and
-// 403 us become 11 (one ciphertext's ModUp) and 453, two passes over the rows fewer; 4096 waves at 62% of the issue slots.
+// 403 us become 11 (one ciphertext's ModUp) and 453, two passes over the rows fewer; 4096 waves at 62% of the issue
+// slots.
 template <int NS, bool COLS>
 __device__ __forceinline__ void conv_col8(uint64_t *out, const uint64_t *in, const Blocks &bl, uint32_t t_per,
                                           const ModQ *__restrict__ mods, const double *__restrict__ twf,
@@ -307,8 +308,8 @@ __global__ __launch_bounds__(256) void k_up_fcol(uint64_t *data, Blocks bl, cons
     for (int k = 0; k < kE; k++) base[(size_t)(LOGS > 4 ? 16 * t + k : k) * 256] = A::to_raw(x[k]);
 }
 
-// 3. the conversion with the forward column pass (conv_col.h), any ring and number of sources: block (target; entry, block
-// and tile of columns)
+// 3. the conversion with the forward column pass (conv_col.h), any ring and number of sources: block (target; entry,
+// block and tile of columns)
 template <int LOGS>
 __global__ __launch_bounds__(256) void k_conv_col16(uint64_t *out, const uint64_t *in, Blocks bl, uint32_t tiles,
                                                     uint32_t max_tgt, const ModQ *__restrict__ mods,
@@ -402,8 +403,8 @@ bool conv_col(const ckks_ctx *ctx, const Blocks &bl, uint32_t count, uint32_t ma
     return !(bl.down && ctx->log_n > 14) && conv_col_few(ctx, count * bl.nd, max_src, max_tgt);
 }
 
-// the conversion of every block of `count` entries; max_src, max_tgt over the blocks; the sources are digits, or (conv_cols)
-// rows after the row pass of their inverse transform
+// the conversion of every block of `count` entries; max_src, max_tgt over the blocks; the sources are digits, or
+// (conv_cols) rows after the row pass of their inverse transform
 ckks_status launch_blocks_conv(ckks_ctx *ctx, uint64_t *out, const uint64_t *in, uint32_t count, const Blocks &bl,
                                uint32_t max_src, uint32_t max_tgt, bool exact8)
 {

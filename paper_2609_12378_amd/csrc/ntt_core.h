@@ -513,8 +513,8 @@ __device__ __forceinline__ void inv8_256(double (&x)[kE8], const double *itws, d
     inv8_stage<0, 0>(x, itws, t, ar);
 }
 
-// Constants of a limb that a block staged in LDS (a loop over limbs would wait for scalar loads of them at its first LDS
-// access), read back as scalars.
+// Constants of a limb that a block staged in LDS (a loop over limbs would wait for scalar loads of them at its first
+// LDS access), read back as scalars.
 __device__ __forceinline__ double uniform(double v)
 {
     const uint64_t b = (uint64_t)__double_as_longlong(v);

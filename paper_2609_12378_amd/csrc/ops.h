@@ -50,8 +50,8 @@ inline size_t ks_stage_rows(const ckks_ctx *ctx, uint32_t level, uint32_t batch,
 // where the ring has them
 ckks_status ks_modup_batch(ckks_ctx *ctx, const uint64_t *c1, size_t in_stride, uint32_t count, uint32_t level,
                            uint64_t *digits, size_t stage_rows);
-// The same in the general arithmetic from c1 [count][level+1][N], which is left in coefficient form; the digits' own rows
-// are not written.  Every transform is one launch over all digits.
+// The same in the general arithmetic from c1 [count][level+1][N], which is left in coefficient form; the digits' own
+// rows are not written.  Every transform is one launch over all digits.
 ckks_status ks_modup_staged(ckks_ctx *ctx, uint64_t *c1, uint32_t count, uint32_t level, uint64_t *digits);
 // out_k = (u_k - Conv(INTT([u_k]_P))) P^-1 (+ add_k), k < polys; u ([polys][level+1+K][N]) is clobbered.
 // add0/add1: [level+1][N] or null, add0 read through the automorphism add0_g (1 = none);
@@ -88,8 +88,8 @@ bool fused_rows_ok(const ckks_ctx *ctx);
 // ciphertexts into outs[r] ([2][l][N]); work: polys (1 + l) N words
 ckks_status fused_rescale(ckks_ctx *ctx, const uint64_t *c, uint32_t polys, uint32_t l, uint64_t *out,
                           uint64_t *const *outs, uint64_t *work);
-// out = (u - cw) w (+ addend): u [count][2][u_rows][N], cw [count][2][limbs][N] after the column pass, w [limbs] (the last
-// step of a rotation batch in the integer arithmetic with P^-1, of a weighted sum with (P q_l)^-1)
+// out = (u - cw) w (+ addend): u [count][2][u_rows][N], cw [count][2][limbs][N] after the column pass, w [limbs] (the
+// last step of a rotation batch in the integer arithmetic with P^-1, of a weighted sum with (P q_l)^-1)
 struct RotArgs;
 ckks_status fused_quotient(ckks_ctx *ctx, uint32_t limbs, uint32_t u_rows, const RotArgs &ra, const uint64_t *u,
                            const uint64_t *cw, const ulonglong2 *w);

@@ -1,10 +1,11 @@
 // Sums of products of residues below 2^60, one reduction a sum: what the basis conversions of the integer arithmetic
 // spend their time on.
 //
-// Both factors split into halves of 30 bits, so the four partial products, below 2^60 each, add up in three 64-bit words
-// without carries: ll and hh of up to 15 products and mid, two a product, of up to 8.  A product is four 32-bit
-// multiply-adds and nothing else, where an exact 128-bit sum adds more carries and moves than that.  The sum S, at most 2^64 q, is divided by 2^64 modulo q (Montgomery 1985: one low and one high product, seven
-// multiplies where reduce128 takes twenty), so the constants carry a factor 2^64 from where they are staged.
+// Both factors split into halves of 30 bits, so the four partial products, below 2^60 each, add up in three 64-bit
+// words without carries: ll and hh of up to 15 products and mid, two a product, of up to 8.  A product is four 32-bit
+// multiply-adds and nothing else, where an exact 128-bit sum adds more carries and moves than that.  The sum S, at most
+// 2^64 q, is divided by 2^64 modulo q (Montgomery 1985: one low and one high product, seven multiplies where reduce128
+// takes twenty), so the constants carry a factor 2^64 from where they are staged.
 #pragma once
 #include "modarith.h"
 

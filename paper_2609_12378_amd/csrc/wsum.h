@@ -19,8 +19,8 @@ struct WsumKind {
     const uint64_t *key[kWsumTerms];
     const uint64_t *tab[kWsumPages][kWsumTerms];
 };
-// A ciphertext c ([2][level+1][N]) and its outputs out[o] ([2][level][N]), prev[o] ([2][level][N]; null: nothing) added;
-// prev[o] may be out[o], no output overlaps another or a ciphertext.
+// A ciphertext c ([2][level+1][N]) and its outputs out[o] ([2][level][N]), prev[o] ([2][level][N]; null: nothing)
+// added; prev[o] may be out[o], no output overlaps another or a ciphertext.
 struct WsumCt {
     const uint64_t *c;
     uint32_t kind;

@@ -13,12 +13,12 @@
 //   1. k_wsum_intt8   u on the rows modulo q_l and P, with the row pass of their inverse transform;
 //   2. k_quot_col     its column pass: centred digits y_i of the P rows, U P^-1 of the q_l row;
 //   3. k_quot_col8    x_t = sum_i y_i [P / p_i]_t + P w for every target q_t, t < l, with the forward column pass
-//      (elsewhere k_quot_col16, or for many reads k_quot_conv and a column pass), w the centred top coefficient of the quotient by P:
-//      w = [(U - sum_i y_i [P / p_i]) P^-1]_{q_l}.  ModDown and rescale subtract Conv(y) P^-1 and then w, so
-//      out = (u - NTT(x)) (P q_l)^-1 holds for both together and the q_l row never leaves the coefficient domain;
+//      (elsewhere k_quot_col16, or for many reads k_quot_conv and a column pass), w the centred top coefficient of the
+//      quotient by P: w = [(U - sum_i y_i [P / p_i]) P^-1]_{q_l}.  ModDown and rescale subtract Conv(y) P^-1 and then
+//      w, so out = (u - NTT(x)) (P q_l)^-1 holds for both together and the q_l row never leaves the coefficient domain;
 //   4. k_wsum_fin8    the forward row pass, u on the rows below q_l (in registers, never in HBM), the quotient, prev.
-// Rings of 2^12 and 2^13 points do the same in whole rows (wsum_block.hip), other primes and rings in exact 128-bit sums
-// (wsum_exact.hip).
+// Rings of 2^12 and 2^13 points do the same in whole rows (wsum_block.hip), other primes and rings in exact 128-bit
+// sums (wsum_exact.hip).
 #include <algorithm>
 
 #include "conv_col.h"
@@ -39,9 +39,10 @@ using nttc::kE8;
 // ones start from (nttc::u8<2>, four adjacent positions a thread) with position bits 1 and 6 exchanged, which is one
 // swap of lane rows a register (swap_1_6).
 // sigma_g reads position j at j' with 2 brev(j') + 1 = (2 brev(j) + 1) g mod 2N.  Bit 0 of j is the top bit of
-// 2 brev(j) + 1 modulo 2N, which an odd g leaves in place up to a carry from below: the partner j + 1 of an even j is read
-// at j' ^ 1; likewise the sources of 64 aligned positions are 64 aligned positions.  So gathers are pairs and whole lines
-// as well.  (8-byte accesses, or 16-byte ones at a stride of 32, cost twice the requests to L2, which bound the kernels.)
+// 2 brev(j) + 1 modulo 2N, which an odd g leaves in place up to a carry from below: the partner j + 1 of an even j is
+// read at j' ^ 1; likewise the sources of 64 aligned positions are 64 aligned positions.  So gathers are pairs and
+// whole lines as well.  (8-byte accesses, or 16-byte ones at a stride of 32, cost twice the requests to L2, which bound
+// the kernels.)
 struct Positions {
     uint32_t at, log_n;
     __device__ Positions(uint32_t h, uint32_t t, uint32_t log_n_)
@@ -77,29 +78,23 @@ __device__ __forceinline__ Pair ld2_auto(const uint64_t *p, uint32_t src)
     return src & 1u ? Pair{v.y, v.x} : v;
 }
 
-// The words that one term takes at PU pairs of positions: c0 (and, unrotated, c1 in place of the first digit), the digits,
-// the key's two halves, the tables.  A unit's loads are issued together, and the next unit's before its own sums: what
-// bounds these kernels otherwise is the wait on one row after another with two or three waves a SIMD.
+// The words that one term takes at PU pairs of positions: c0 (and, unrotated, c1 in place of the first digit), the
+// digits, the key's two halves, the tables.  A unit's loads are issued together, and the next unit's before its own
+// sums: what bounds these kernels otherwise is the wait on one row after another with two or three waves a SIMD.
 template <int ND, int PU, int NOUT>
 struct Unit {
     Pair c[PU], dig[ND][PU], b[ND][PU], a[ND][PU], tab[NOUT][PU];
     uint32_t flip[PU];
 };
-constexpr int unit_pairs(int) { return 1; }
 
-struct NoTail {
-    __device__ void operator()() const {}
-};
-
-// u of output o at the 8 positions of a thread, both components, as doubles: |u| <= 2.6 q (a term of at most 0.7 q after
-// the reduction of t, or 0.83 q unrotated).  Unrotated kinds: pt c without the factor P.  A digit's own rows are the
-// ciphertext's (the ModUp leaves them out).  Q: the row is one of the q limbs (the P rows have no c terms).  tail() is
-// called when the last loads here are out.
-template <int ND, int NOUT, bool Q, typename Tail>
+// u of output o at the 8 positions of a thread, both components, as doubles: |u| <= 2.6 q (a term of at most 0.7 q
+// after the reduction of t, or 0.83 q unrotated).  Unrotated kinds: pt c without the factor P.  A digit's own rows are
+// the ciphertext's (the ModUp leaves them out).  Q: the row is one of the q limbs (the P rows have no c terms).
+template <int ND, int NOUT, bool Q>
 __device__ __forceinline__ void wsum8(const WsumKind &w, const Ct &ct, const Dims &d, uint32_t row, double pq, const A &ar,
-                                      const Positions &ps, double (&u)[NOUT][2][kE8], Tail tail)
+                                      const Positions &ps, double (&u)[NOUT][2][kE8])
 {
-    constexpr int PU = unit_pairs(ND), kUnits = 4 / PU;
+    constexpr int PU = 1, kUnits = 4 / PU;   // two pairs a unit hold more words than the registers
     using U = Unit<ND, PU, NOUT>;
     const size_t rw = (size_t)row << d.log_n, half = (size_t)d.L << d.log_n;
     const size_t kstride = (size_t)d.key_rows << d.log_n, dstride = (size_t)d.ext << d.log_n;
@@ -139,8 +134,8 @@ __device__ __forceinline__ void wsum8(const WsumKind &w, const Ct &ct, const Dim
         u[o][0][e + 1] += ar.mul(s0, p1);
         u[o][1][e + 1] += ar.mul(s1, p1);
     };
-    // keeps the sums of one unit ahead of the next unit's loads: the compiler would gather them all behind the last load,
-    // with every unit's words in registers
+    // keeps the sums of one unit ahead of the next unit's loads: the compiler would gather them all behind the last
+    // load, with every unit's words in registers
     auto done = [&] {
 #pragma unroll
         for (int o = 0; o < NOUT; o++)
@@ -197,7 +192,6 @@ __device__ __forceinline__ void wsum8(const WsumKind &w, const Ct &ct, const Dim
 #pragma unroll
                 for (int o = 0; o < NOUT; o++) tab[o][e] = ld2(w.tab[o][0] + rw + at);
             }
-            if (p0 && first >= n) tail();
 #pragma unroll
             for (int e = 0; e < 2; e++) {
                 double t0 = A::from_u64(v0[e].x), t1 = A::from_u64(v1[e].x), t2 = A::from_u64(v0[e].y),
@@ -215,14 +209,13 @@ __device__ __forceinline__ void wsum8(const WsumKind &w, const Ct &ct, const Dim
         }
     }
     for (uint32_t j = first; j < n; j++) {
-        // two register sets in turn; the last unit's successor is the term after it, or the tail
+        // two register sets in turn; the last unit's successor is the term after it
 #pragma unroll
         for (int k = 0; k < kUnits; k += 2) {
             load(x1, j, (k + 1) * PU);
             use(x0, k * PU);
             if (k + 2 < kUnits) load(x0, j, (k + 2) * PU);
             else if (j + 1 < n) load(x0, j + 1, 0);
-            else tail();
             use(x1, (k + 1) * PU);
         }
     }
@@ -250,8 +243,8 @@ __global__ __launch_bounds__(64) void k_wsum_intt8(Args a, uint64_t *up, Dims d,
     nttc::stage_twiddles8(tws[sub], itwf + ((size_t)prime << d.log_n), (1u << (d.log_n - 8)) + h, t, 32);
     const Positions ps(h, t, d.log_n);
     double u[NOUT][2][kE8];
-    if (s) wsum8<ND, NOUT, false>(w, ct, d, row, 0.0, ar, ps, u, NoTail());
-    else wsum8<ND, NOUT, true>(w, ct, d, row, (double)pmodq[row].x, ar, ps, u, NoTail());
+    if (s) wsum8<ND, NOUT, false>(w, ct, d, row, 0.0, ar, ps, u);
+    else wsum8<ND, NOUT, true>(w, ct, d, row, (double)pmodq[row].x, ar, ps, u);
     __syncthreads();
 #pragma unroll
     for (int o = 0; o < NOUT; o++)
@@ -298,12 +291,12 @@ __global__ __launch_bounds__(256) void k_quot_col(uint64_t *up, Args a, Dims d, 
     for (int k = 0; k < kE; k++) base[(size_t)(t + TS * k) * 256] = A::to_raw(centre(ar, x[k]));
 }
 
-// 3. The conversion fused with the forward column pass, N = 2^16 and at most 8 special primes (k_conv_col8's shape: block
-// (poly; 16 adjacent columns; group of t_per targets), 512 threads, 8 points of a 256-point column each, the digits of
-// the block's 4096 coefficients and w in registers for every target).  EXACT: K = 8.  COLS: `up` holds the rows after the
-// row pass of their inverse transforms, whose column passes run here as well (step 2 is not a launch of its own).
-// 32 polynomials, 8 special primes, 12 targets: 181 us, 63% of the issue slots with the two waves a SIMD that the digits'
-// registers allow.
+// 3. The conversion fused with the forward column pass, N = 2^16 and at most 8 special primes (k_conv_col8's shape:
+// block (poly; 16 adjacent columns; group of t_per targets), 512 threads, 8 points of a 256-point column each, the
+// digits of the block's 4096 coefficients and w in registers for every target).  EXACT: K = 8.  COLS: `up` holds the
+// rows after the row pass of their inverse transforms, whose column passes run here as well (step 2 is not a launch of
+// its own). 32 polynomials, 8 special primes, 12 targets: 181 us, 63% of the issue slots with the two waves a SIMD that
+// the digits' registers allow.
 template <bool EXACT, bool COLS>
 __global__ __launch_bounds__(512) void k_quot_col8(uint64_t *out, const uint64_t *up, Args a, Dims d, uint32_t pages,
                                                    uint32_t t_per, Quot qt, const ModQ *__restrict__ mods,
@@ -436,8 +429,8 @@ __global__ __launch_bounds__(512) void k_quot_col8(uint64_t *out, const uint64_t
     }
 }
 
-// 3. The conversion alone (N < 2^16, or more than 8 special primes): thread = one coefficient, blockIdx.y a group of t_per
-// targets, blockIdx.z the polynomial; canonical residues out.
+// 3. The conversion alone (N < 2^16, or more than 8 special primes): thread = one coefficient, blockIdx.y a group of
+// t_per targets, blockIdx.z the polynomial; canonical residues out.
 template <int NS>
 __global__ __launch_bounds__(256) void k_quot_conv(uint64_t *out, const uint64_t *up, Args a, Dims d, uint32_t pages,
                                                    uint32_t t_per, Quot qt, const ModQ *__restrict__ mods)
@@ -504,8 +497,8 @@ constexpr unsigned quot_col_mask(int logs)
     return logs == 6 ? 0x34 : logs == 7 ? 0x74 : 0xd4;
 }
 
-// 3. The conversion with the forward column pass for N < 2^16 or more than 8 special primes (conv_col.h): block (target;
-// polynomial and tile of columns).  Every target forms w again, from the reads of its own sum.
+// 3. The conversion with the forward column pass for N < 2^16 or more than 8 special primes (conv_col.h): block
+// (target; polynomial and tile of columns).  Every target forms w again, from the reads of its own sum.
 template <int LOGS>
 __global__ __launch_bounds__(256) void k_quot_col16(uint64_t *out, const uint64_t *up, Args a, Dims d, uint32_t pages,
                                                     uint32_t tiles, Quot qt, const ModQ *__restrict__ mods,
@@ -541,10 +534,10 @@ __global__ __launch_bounds__(256) void k_quot_col16(uint64_t *out, const uint64_
     ct.template forward<quot_col_mask(LOGS)>(x, out + (((size_t)p * nt + tt) << d.log_n), twf + ((size_t)tt << d.log_n), lds, ar);
 }
 
-// 4. out = (u - NTT(x)) (P q_l)^-1 (+ prev) on the rows below q_l: cw[z P + o][k][l] after the column pass.  Magnitudes in
-// units of q: column-pass rows below 4.3, transformed below 2.6, u below 2.6, products below 2.5: all below 8 q = 2^53.
-// 16 ciphertexts of 13 limbs: 211 us, 64% of the issue slots, 0.53 GB at 2.5 TB/s; 8 rotated and 8 unrotated added to
-// their pages: 201 us, 51%, 0.61 GB at 3.1 TB/s.
+// 4. out = (u - NTT(x)) (P q_l)^-1 (+ prev) on the rows below q_l: cw[z P + o][k][l] after the column pass.  Magnitudes
+// in units of q: column-pass rows below 4.3, transformed below 2.6, u below 2.6, products below 2.5: all below 8 q =
+// 2^53. 16 ciphertexts of 13 limbs: 211 us, 64% of the issue slots, 0.53 GB at 2.5 TB/s; 8 rotated and 8 unrotated
+// added to their pages: 201 us, 51%, 0.61 GB at 3.1 TB/s.
 template <int ND, int NOUT>
 __global__ __launch_bounds__(64) void k_wsum_fin8(Args a, const uint64_t *__restrict__ cw, Dims d, uint32_t n, Quot qt,
                                                   const ModQ *__restrict__ mods, const double *__restrict__ twf)
@@ -575,7 +568,7 @@ __global__ __launch_bounds__(64) void k_wsum_fin8(Args a, const uint64_t *__rest
         __builtin_amdgcn_sched_barrier(0);
     };
     double u[NOUT][2][kE8];
-    wsum8<ND, NOUT, true>(w, ct, d, row, (double)qt.pmodq[row].x, ar, ps, u, NoTail());
+    wsum8<ND, NOUT, true>(w, ct, d, row, (double)qt.pmodq[row].x, ar, ps, u);
     // (P q_l)^-1, or q_l^-1 where u has no factor P, canonical
     double f = (double)qt.qlinv[row].x;
     if (w.rotated) {

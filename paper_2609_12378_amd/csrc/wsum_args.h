@@ -30,8 +30,8 @@ struct __attribute__((aligned(8))) Pair {
 };
 __device__ __forceinline__ Pair ld2(const uint64_t *p) { return *(const Pair *)p; }
 
-// Block b of a launch over `tiles` tiles (a multiple of 8) of each of n ciphertexts: blocks go to the 8 XCDs in turn, and
-// the ciphertexts of one tile, which share its keys and tables, follow one another on one XCD.
+// Block b of a launch over `tiles` tiles (a multiple of 8) of each of n ciphertexts: blocks go to the 8 XCDs in turn,
+// and the ciphertexts of one tile, which share its keys and tables, follow one another on one XCD.
 __device__ __forceinline__ void tile_of(uint32_t n, uint32_t &z, uint32_t &tile)
 {
     const uint32_t xcd = blockIdx.x & 7u, rest = blockIdx.x >> 3;
@@ -39,8 +39,8 @@ __device__ __forceinline__ void tile_of(uint32_t n, uint32_t &z, uint32_t &tile)
     tile = (rest / n) * 8 + xcd;
 }
 
-// sum_i a_i w_i mod q of at most 4 products of canonical residues under one quotient (nttc::GridSum with twice its grid:
-// u = 2^51, so |sum| < 4 2^100 = 2^51 u, and lo is at most 4 2^50 = 2^52).  value(): |x| <= q/2 + 1.
+// sum_i a_i w_i mod q of at most 4 products of canonical residues under one quotient (nttc::GridSum with twice its
+// grid: u = 2^51, so |sum| < 4 2^100 = 2^51 u, and lo is at most 4 2^50 = 2^52).  value(): |x| <= q/2 + 1.
 struct ProductSum {
     static constexpr double kGrid = 0x1.8p+103;   // 1.5 2^52 u
     double hi, lo;
@@ -103,9 +103,9 @@ __device__ __forceinline__ double top_factor(const Quot &qt, const Dims &d, int 
 // u: 2 n pages (level+1+n_p) N words
 ckks_status wsum_blk_sums(ckks_ctx *ctx, const wsum::Args &a, uint32_t n, uint32_t pages, const wsum::Dims &d, uint64_t *u);
 
-// Any ring and any primes (wsum_exact.hip): the same in exact 128-bit sums, of ciphertexts that are all of rotated kinds
-// (rot) or all of unrotated ones; a.ct[z].dig's own rows are not read.  u: 2 n pages (level+1+n_p) N words, x: 2 n pages
-// level N
+// Any ring and any primes (wsum_exact.hip): the same in exact 128-bit sums, of ciphertexts that are all of rotated
+// kinds (rot) or all of unrotated ones; a.ct[z].dig's own rows are not read.  u: 2 n pages (level+1+n_p) N words, x: 2
+// n pages level N
 ckks_status wsum_exact_sums(ckks_ctx *ctx, const wsum::Args &a, uint32_t n, uint32_t pages, const wsum::Dims &d, bool rot,
                             uint64_t *u, uint64_t *x);
 // c1 of the first n ciphertexts to out[n][L][N]

@@ -1,12 +1,12 @@
-// Weighted sums of rotations (wsum.hip) in the rings of 2^12 and 2^13 points with fp64 arithmetic, whole rows in a block
-// (ntt_block.h).  After the ModUp:
+// Weighted sums of rotations (wsum.hip) in the rings of 2^12 and 2^13 points with fp64 arithmetic, whole rows in a
+// block (ntt_block.h).  After the ModUp:
 //   1. k_blk_wsum   u on every row, element-wise;
 //   2. k_blk_wtop   the rows q_l and P to coefficients: U P^-1 and the centred digits y_i;
 //   3. k_blk_wfin   a block forms its row of the conversion, x_t = sum_i y_i [P / p_i]_t + P w with w the centred top
 //      coefficient of the quotient by P, transforms it and writes (u - NTT(x)) (P q_l)^-1 (+ prev).
-// With the two launches of the ModUp that is five; through the ModDown, the rescale and the additions it was eight.  Few
-// ciphertexts are bounded by one row's latency a launch: one of 4 limbs at N = 2^12 takes 4, 7 and 11 us in the three (35 us
-// a call, as long as the host takes to issue it), three of 6 limbs at 2^13 8, 10 and 17 (56 us a call).
+// With the two launches of the ModUp that is five; through the ModDown, the rescale and the additions it was eight. 
+// Few ciphertexts are bounded by one row's latency a launch: one of 4 limbs at N = 2^12 takes 4, 7 and 11 us in the
+// three (35 us a call, as long as the host takes to issue it), three of 6 limbs at 2^13 8, 10 and 17 (56 us a call).
 #include "ntt_block.h"
 #include "ops.h"
 #include "wsum_args.h"
@@ -22,8 +22,8 @@ struct Tab {
     const double *twf, *itwf;
 };
 
-// u[z P + o][k][row][n] as doubles of at most q/2 + 1: one position a thread, every load issued before the first product.
-// Unrotated kinds: pt c, on the q rows alone.
+// u[z P + o][k][row][n] as doubles of at most q/2 + 1: one position a thread, every load issued before the first
+// product. Unrotated kinds: pt c, on the q rows alone.
 template <int ND, int P>
 __global__ __launch_bounds__(256) void k_blk_wsum(Args a, uint64_t *u, Dims d, const ulonglong2 *__restrict__ pmodq,
                                                   const ModQ *__restrict__ mods)
@@ -102,8 +102,8 @@ __global__ __launch_bounds__(256) void k_blk_wsum(Args a, uint64_t *u, Dims d, c
     }
 }
 
-// rows q_l (blockIdx.x = 0) and P of each polynomial to centred coefficients times their factor, in place (a thread's words
-// are in registers before the first block barrier and written after the last); grid (K + 1, polys)
+// rows q_l (blockIdx.x = 0) and P of each polynomial to centred coefficients times their factor, in place (a thread's
+// words are in registers before the first block barrier and written after the last); grid (K + 1, polys)
 template <int LOGN>
 __global__ __launch_bounds__(blk::Shape<LOGN>::NT) void k_blk_wtop(uint64_t *u, Args a, Dims d, uint32_t pages, Quot qt,
                                                                    Tab tb)
@@ -182,7 +182,8 @@ __global__ __launch_bounds__(blk::Shape<LOGN>::NT) void k_blk_wfin(Args a, const
         const double pq = (double)qt.pmodq[i].x;
         f = centre(ar, ar.mul(f, (double)qt.pinv[i].x));
         f = f < 0.0 ? f + ar.q : f;
-        // the sums modulo q_l first, then those modulo q_i, eight points at a time: both at once would not fit the registers
+        // the sums modulo q_l first, then those modulo q_i, eight points at a time: both at once would not fit the
+        // registers
         double v[kE];
         digit_sums<LOGN>(v, yr, d, top, [&](int s) { return top_factor(qt, d, s, top); });
 #pragma unroll
