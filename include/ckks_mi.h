@@ -458,7 +458,9 @@ ckks_status ckks_rope(ckks_ctx *ctx, const ckks_buf *in, uint32_t count, const c
  * position, as a ciphertext with one limb fewer than the new tokens' (the
  * attention calls' key or value ciphertext).  k_pages, v_pages: n_pages
  * descriptors each; table (host, [n_heads][n_blocks]): the page of tokens
- * b T .. b T + T - 1 of head h, the same in both pools. */
+ * b T .. b T + T - 1 of head h, the same in both pools.  A call looks at the
+ * descriptors and table entries of the pages that it writes or continues alone:
+ * the others may be anything. */
 typedef struct {
     ckks_buf *k_pages, *v_pages;
     uint32_t n_pages;

@@ -735,7 +735,8 @@ class Context:
                      pairing: str = "half", fork: Optional[Sequence[int]] = None) -> None:
         """Append tokens src .. src + count - 1 of each head's key (rotated by the tables) and value ciphertext to a
         paged cache of `length` tokens: block_table[h][b] is the page of head h's tokens b * tokens and on, in both
-        pools; fork[h] the page that head h's started page continues, if not itself."""
+        pools; fork[h] the page that head h's started page continues, if not itself.  Of pools and table only the pages
+        written and continued are looked at (the others may be None), so a call costs the same however long the cache."""
         shape = self._rope_shape(tokens, head_dim, rot_dim, "tm", pairing)
         heads = len(k_cts)
         if len(v_cts) != heads or len(block_table) != heads or (fork is not None and len(fork) != heads):
@@ -749,24 +750,42 @@ class Context:
         if not heads or not count:
             return
         n_blocks = min(len(row) for row in block_table)
-        index = [int(p) for row in block_table for p in row[:n_blocks]]
-        if any(not 0 <= p < 1 << 32 for p in index + list(fork or ())):
+        first = length // tokens
+        if any(not 0 <= p < 1 << 32 for row in block_table for p in row[first:first + blocks]) or \
+                any(not 0 <= p < 1 << 32 for p in fork or ()):
             raise CkksError("cache_append: a page index is not a 32-bit count")
         pt = _arg(tables, "tables", torch.uint64,
                   shape=(blocks, 4 if rot_dim else 1, k_cts[0].n_limbs + self.n_p, self.n))
         kb, vb = ((_Buf * heads)(*[c.c(self.n) for c in x]) for x in (k_cts, v_cts))
+        # descriptors and table entries of the pages written and continued alone (the rest stays zero): the library reads
+        # no others.  Their number grows with the context (a call's host side with every page described: 0.4 ms at 64
+        # pages a pool, 22 ms at 4096; so, 0.11 ms at either), and a page that is not written is not this call's to change
         n_pages = len(k_pages)
-        kp_, vp_ = ((_Buf * max(1, n_pages))(*[c.c(self.n) for c in x]) for x in (k_pages, v_pages))
-        tab = (_U32 * max(1, len(index)))(*index)
+        tab = (_U32 * max(1, heads * n_blocks))()
+        written, seen = set(), set()
+        for h, row in enumerate(block_table):
+            for b in range(first, min(first + blocks, n_blocks)):
+                tab[h * n_blocks + b] = int(row[b])
+                written.add(int(row[b]))
+        seen.update(written, (int(p) for p in fork or () if length % tokens))
+        kp_, vp_ = ((_Buf * max(1, n_pages))() for _ in range(2))
+        for what, bufs, pages in (("key", kp_, k_pages), ("value", vp_, v_pages)):
+            for p in seen:
+                if p >= n_pages:
+                    continue   # the library names the head and the block
+                if pages[p] is None:
+                    raise CkksError("cache_append: %s page %d is not there" % (what, p))
+                bufs[p] = pages[p].c(self.n)
         cache = _Cache(kp_, vp_, n_pages, tab, n_blocks)
         fk = None if fork is None else (_U32 * heads)(*fork)
         ks, kp, nk = self._keys_of(keys)
-        self._used(tables, *[c.data for x in (k_cts, v_cts, k_pages, v_pages) for c in x], *keys.values())
+        self._used(tables, *[c.data for x in (k_cts, v_cts) for c in x],
+                   *[x[p].data for x in (k_pages, v_pages) for p in seen if p < n_pages], *keys.values())
         _check(self.lib.ckks_cache_append(self.h, kb, vb, heads, ctypes.byref(shape), src, length, count, pt, ks, kp,
                                           nk, ctypes.byref(cache), fk), "ckks_cache_append")
         for bufs, pages in ((kp_, k_pages), (vp_, v_pages)):
-            for b, p in zip(bufs, pages):
-                p.scale = b.scale
+            for p in written:
+                pages[p].scale = bufs[p].scale
 
     @staticmethod
     def rope_steps(slots: int, tokens: int, rot_dim: int, layout: str = "tm", pairing: str = "half") -> List[int]:
