@@ -100,6 +100,7 @@ __global__ __launch_bounds__(blk::Shape<LOGN>::NT) void k_blk_ntt(uint64_t *dst,
 {
     __shared__ double lds[blk::Shape<LOGN>::kLds];
     const uint32_t b = blockIdx.x / map.n, limb = blockIdx.x % map.n, prime = map.prime[limb], t = threadIdx.x;
+    if (map.skips(b, limb)) return;
     const A ar(tb.mods[prime]);
     const double *tw = table<LOGN>(INV ? tb.itwf : tb.twf, prime);
     const blk::ColTw<LOGN> cw(tw);
