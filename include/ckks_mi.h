@@ -155,7 +155,7 @@ typedef enum {
     CKKS_OP_ATTN_APPLY = 14,    /* shape = {limbs of the scores, limbs of the values, tokens, head_dim} */
     CKKS_OP_ROPE_TABLES = 15,   /* rope_tables and cache_tables; shape unused */
     CKKS_OP_ROPE = 16,          /* shape = {limbs of the inputs, ciphertexts of one call} */
-    CKKS_OP_CACHE_APPEND = 17   /* shape = {limbs of the inputs, heads of one call} */
+    CKKS_OP_CACHE_APPEND = 17   /* shape = {limbs of the inputs, heads of one call}: any src, length and count */
 } ckks_op;
 size_t ckks_workspace_bytes(const ckks_ctx *ctx, int op, const uint32_t *shape);
 ckks_status ckks_set_workspace(ckks_ctx *ctx, void *dev, size_t bytes);
@@ -406,7 +406,8 @@ ckks_status ckks_attention_apply(ckks_ctx *ctx, const ckks_buf *p, uint32_t n_p,
  * D the ModUp digits of c1 and g the Galois element of term j (t_j = P (c0, c1)
  * where the rotation is by nothing), exactly: the stages are ckks_modup's,
  * ckks_moddown's and ckks_rescale's.  Needs special primes; any primes the
- * context takes.
+ * context takes, where the attention calls take primes below 2^50 alone
+ * (CKKS_EUNSUPPORTED): pages over larger ones are for the caller's own products.
  *
  * Shape.  `tokens` tokens a ciphertext (T, a power of two up to N/2; D = N/2/T
  * features), heads of `head_dim` features (any size up to D; features after the
@@ -481,15 +482,21 @@ ckks_status ckks_cache_tables(ckks_ctx *ctx, const ckks_rope_shape *shape, uint3
  * src + i of k[h] (rotated by the tables) and of v[h] becomes token length + i of
  * head h.  k, v: one head a ciphertext, repeated in every head position; n_limbs =
  * level + 1 >= 2, equal; equal scales within each.  The slots of their other
- * tokens are not read into the cache.  The pages' slots before the new tokens stay, slots after them become
- * zero where a page is begun (length a multiple of T, or the second page) and
- * stay (zero, as it was begun) otherwise; no other page is touched.  A begun page's old
- * contents do not matter; a started one must have the new tokens' scale.
+ * tokens are not read into the cache.  The pages' slots before the new tokens
+ * stay, slots after them become zero where a page is begun (length a multiple of
+ * T, or the second page) and stay (zero, as it was begun) otherwise; no other page
+ * is touched.  A begun page's old contents do not matter; a started one must have
+ * the new tokens' scale.
+ * Noise: an append adds that of its key switch and rescale to every slot of the
+ * pages it writes, so a page of n appends holds the sum of n of them, about
+ * sqrt(n) times one's and at most n times (N = 2^13, scale 2^50: slots off by
+ * 8e-12 after one append, 9.4e-11 after 128 single tokens).
  * fork (host, [n_heads], or NULL): the page that head h's started page continues,
- * if not itself - its contents are taken over, and it stays as it is (sequences that share
- * a prefix).  The pages written must be distinct, and none may be an input or
- * another head's forked page (CKKS_EINVAL).  Keys: the left rotations by -m and, with rot_dim > 0, h - m and
- * -h - m (as ckks_rope's h), m = D ((length - src) mod T); a token placed in its
+ * if not itself - its contents are taken over, and it stays as it is (sequences
+ * that share a prefix).  The pages written must be distinct, and none may be an
+ * input or another head's forked page (CKKS_EINVAL).  Keys: the left rotations by
+ * -m and, with rot_dim > 0, h - m and -h - m (as ckks_rope's h),
+ * m = D ((length - src) mod T); a token placed in its
  * own slot by the encryptor (src = length mod T) needs +-h alone, and its values
  * no key.  Scratch: CKKS_OP_CACHE_APPEND.  Errors as ckks_rope's, CKKS_EINVAL also
  * for a page index out of range or a table too short, CKKS_ESCALE. */

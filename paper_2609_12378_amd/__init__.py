@@ -736,7 +736,7 @@ class Context:
         """Append tokens src .. src + count - 1 of each head's key (rotated by the tables) and value ciphertext to a
         paged cache of `length` tokens: block_table[h][b] is the page of head h's tokens b * tokens and on, in both
         pools; fork[h] the page that head h's started page continues, if not itself.  Of pools and table only the pages
-        written and continued are looked at (the others may be None), so a call costs the same however long the cache."""
+        written and continued are looked at (the others may be None): a call costs the same however long the cache."""
         shape = self._rope_shape(tokens, head_dim, rot_dim, "tm", pairing)
         heads = len(k_cts)
         if len(v_cts) != heads or len(block_table) != heads or (fork is not None and len(fork) != heads):
@@ -757,9 +757,9 @@ class Context:
         pt = _arg(tables, "tables", torch.uint64,
                   shape=(blocks, 4 if rot_dim else 1, k_cts[0].n_limbs + self.n_p, self.n))
         kb, vb = ((_Buf * heads)(*[c.c(self.n) for c in x]) for x in (k_cts, v_cts))
-        # descriptors and table entries of the pages written and continued alone (the rest stays zero): the library reads
-        # no others.  Their number grows with the context (a call's host side with every page described: 0.4 ms at 64
-        # pages a pool, 22 ms at 4096; so, 0.11 ms at either), and a page that is not written is not this call's to change
+        # descriptors and table entries of the pages written and continued alone (the rest stays zero): the library
+        # reads no others.  Their number grows with the context (a call's host side with every page described: 0.4 ms at
+        # 64 pages a pool, 22 ms at 4096; so, 0.11 ms at either), and a page not written is not this call's to change
         n_pages = len(k_pages)
         tab = (_U32 * max(1, heads * n_blocks))()
         written, seen = set(), set()

@@ -615,8 +615,12 @@ bool fp64_sums(const ckks_ctx *ctx, uint32_t level)
     return f64_switch(ctx, level) && n_digits(ctx, level) <= 5;
 }
 
-// Words of a batch: the digits, the staging rows of the ModUps that take any, u (the fp64 kernels: its rows q_l and P)
-// and the converted rows.
+// Words of a batch: the digits, the staging rows of the ModUps that take any, u and the converted rows.  The figure is
+// what the sums in integers write; the fp64 kernels leave a part of it alone (u's rows below q_l and the staging rows
+// in two passes, the converted rows in whole ones: 16 ciphertexts of 13 + 8 limbs at N = 2^16 touch 0.70 GB of 1.02).
+// It is one figure for both arithmetics, since a workspace of it has to serve after ckks_ctx_set_ntt_arith as well, and
+// one for all calls of as many ciphertexts, so that no later one - a moved token, a page border - makes the arena grow
+// inside a graph.
 struct Scratch {
     size_t dig, stage, u, x, total;
 };
