@@ -5,15 +5,18 @@
 #include "ckks_internal.h"
 #include "ntt_core.h"
 
-// Worth it while the reads, tiles of 4096 coefficients times targets times sources, are few.  Calls of hoisted
-// rotations, us in one launch and in two: 59 and 67 (one rotation at N = 2^14, 11 limbs in digits of 4), 215 and 231
-// (32 of them, 11264 reads), 194 and 196 (8 at N = 2^15, 16 limbs, 8 special primes: 16384), 260 and 251 (8 at N =
-// 2^16, 10 limbs, 10 special primes: 25600), 1990 and 1771 (32 at N = 2^16, 24 limbs, 12 special primes: 294912).  The
-// weighted sums' quotient (five ciphertexts at N = 2^14, 9 limbs, 4 special primes): 15.8 us in place of 10.7 and 7.8.
-// (Rotations: ModUps and ModDowns both.)
-inline bool conv_col_few(const ckks_ctx *ctx, uint32_t polys, uint32_t sources, uint32_t targets)
+// Worth it while the reads, tiles of 4096 coefficients times targets times sources, are few: `most`.  us a call in two
+// launches and in one, rotary positions of 1 to 16 ciphertexts for the ModUps, hoisted rotations for the ModDowns:
+//   ModUps    2^14, 9 limbs in digits of 4: 101 and 95 (2880 reads); 2^15, 6 limbs of 2: 242 and 221 (5376), 16 limbs of 8:
+//             176 and 174 (11776), 318 and 312 (23552); 2^16, 10 limbs of 10: 357 and 354 (12800), 642 and 641 (25600);
+//             2^14, 24 limbs of 8: 464 and 465 (47616)
+//   ModDowns  2^14, 11 limbs and 4 special primes: 96 and 88 (2816), 221 and 205 (11264); 24 and 8: 161 and 157 (12288),
+//             259 and 258 (24576), 440 and 445 (49152)
+constexpr size_t kConvColReads = 16384;
+inline bool conv_col_few(const ckks_ctx *ctx, uint32_t polys, uint32_t sources, uint32_t targets,
+                         size_t most = kConvColReads)
 {
-    return ((size_t)polys << (ctx->log_n - 12)) * targets * sources <= 16384;
+    return ((size_t)polys << (ctx->log_n - 12)) * targets * sources <= most;
 }
 
 namespace nttc {

@@ -699,7 +699,11 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
     // with a block for every CU, no block's targets are split and its columns are transformed where they are converted
     // (both rules of the conversions, us a call with and without: 772 and 819 for 16 ciphertexts; 130 and 108 for one)
     const bool cols = fused && polys * 16 >= 256;
-    const bool col16 = !fused && conv_col_few(ctx, polys, d.K, level);
+    // k_quot_col16 forms w for every target, a second sum over its reads: worth it for a quarter of what the other
+    // conversions take (us a call in two launches and in one: 2^14, 5 ciphertexts of 9 limbs 97.2 and 94.5, 1280 reads;
+    // 16 of them 189 and 186, 4096; 2^15, 8 of 6 limbs 137 and 132, 1280; 4 of 16 limbs 172.5 and 174.3, 7680; 8 of
+    // them 293 and 311, 15360; 2^16, 4 of 10 limbs and 10 special primes 211 and 221, 11520)
+    const bool col16 = !fused && conv_col_few(ctx, polys, d.K, level, kConvColReads / 4);
     const double rows2 = (double)polys * (d.K + 1) * N;
     if (!cols) {
         prof_begin(ctx, K_NTT_INV_COL, 16.0 * rows2, rows2 * kOpsButterflyF64 * (d.log_n - 8) / 2);
