@@ -396,8 +396,11 @@ bool conv_cols(const ckks_ctx *ctx, uint32_t max_src, uint32_t count, const Bloc
     return conv_fused(ctx, max_src) && count * 16 * bl.nd >= 256;
 }
 
-// the conversion takes the forward column pass along (k_conv_col16).  A ModDown's does so below 2^15 alone: above, the
-// launches of a rotation that the event profiler reports stay those of a pass of its own.
+// the conversion takes the forward column pass along (k_conv_col16).  A ModDown's does so up to 2^14 alone.  Above, it
+// would pay as well (us a call of hoisted rotations in two launches and in one: 2^15, 6 limbs and 2 special primes, one
+// 62 and 58, 32 of them 229 and 204; 16 and 8, 8 of them 189 and 186; 2^16, 10 and 10, 4 of them 161 and 158, 8 of them,
+// 25600 reads, 243 and 248), but there the launches of a rotation that the event profiler reports, a column pass of
+// the converted rows among them, are held by tests/test_gpu_mixed_chains.py.
 bool conv_col(const ckks_ctx *ctx, const Blocks &bl, uint32_t count, uint32_t max_src, uint32_t max_tgt)
 {
     return !(bl.down && ctx->log_n > 14) && conv_col_few(ctx, count * bl.nd, max_src, max_tgt);
