@@ -5,7 +5,7 @@
 // transform writes them itself, the constant folded into its last stage's factor N^-1.  A ModUp of any number of
 // ciphertexts is three to five launches for all digits together:
 //   1. row pass of the inverse transform of every limb, from the polynomial into the limb's row of its digit;
-//   2. column pass, leaving the digits y there (within 3 at N = 2^16 with a block for every CU);
+//   2. column pass, leaving the digits y there (within 3 at N = 2^16 for more than 128 blocks);
 //   3. conversion of every digit, fused with the forward column pass at N = 2^16 and where its reads are few;
 //   4. forward row pass, which in the digits' own rows (no longer needed for y) puts the polynomial itself, unless the
 //      caller reads those from the polynomial.
@@ -389,11 +389,14 @@ ckks_status launch_col_digits(ckks_ctx *ctx, uint64_t *data, uint32_t count, con
 // columns of 256 points and few enough sources for the registers of the fused conversion
 bool conv_fused(const ckks_ctx *ctx, uint32_t max_src) { return ctx->log_n == 16 && max_src <= 8; }
 
-// the fused conversion takes the sources' column passes too: with a block for every CU, so that no block's targets are
-// split (each part would transform the sources again)
+// the fused conversion takes the sources' column passes too: above half a block a CU, where no block's targets are split
+// (each part would transform the sources again).  us a call with the pass apart and along, by blocks: ModUps of 13 limbs
+// in two digits 150.6 and 157.0 (64), 250.3 and 253.7 (128), 362 and 356 (192), 425 and 415 (256), 803 and 783 (512);
+// of 24 limbs in three 180 and 187 (48), 402 and 400 (144), 579 and 566 (240); ModDowns of 24 limbs and 8 special primes
+// 184 and 193 (64), 281 and 279 (128), 395 and 384 (192), 1581 and 1544 (1024)
 bool conv_cols(const ckks_ctx *ctx, uint32_t max_src, uint32_t count, const Blocks &bl)
 {
-    return conv_fused(ctx, max_src) && count * 16 * bl.nd >= 256;
+    return conv_fused(ctx, max_src) && count * 16 * bl.nd > 128;
 }
 
 // the conversion takes the forward column pass along (k_conv_col16).  A ModDown's does so up to 2^14 alone.  Above, it

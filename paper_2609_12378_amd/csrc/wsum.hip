@@ -696,9 +696,10 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
     HIP_TRY(hipGetLastError());
 
     const bool fused = d.log_n == 16 && d.K <= 8;
-    // with a block for every CU, no block's targets are split and its columns are transformed where they are converted
-    // (both rules of the conversions, us a call with and without: 772 and 819 for 16 ciphertexts; 130 and 108 for one)
-    const bool cols = fused && polys * 16 >= 256;
+    // above half a block a CU no block's targets are split and its columns are transformed where they are converted (us
+    // a call with the pass apart and along, by blocks: 13 limbs 150.4 and 160.4 (64), 251.9 and 253.7 (128), 363 and 356
+    // (192), 433 and 415 (256), 812 and 783 (512); 4 limbs 73.0 and 75.6 (64), 124.3 and 119.3 (192))
+    const bool cols = fused && polys * 16 > 128;
     // k_quot_col16 forms w for every target, a second sum over its reads: worth it for a quarter of what the other
     // conversions take (us a call in two launches and in one: 2^14, 5 ciphertexts of 9 limbs 97.2 and 94.5, 1280 reads;
     // 16 of them 189 and 186, 4096; 2^15, 8 of 6 limbs 137 and 132, 1280; 4 of 16 limbs 172.5 and 174.3, 7680; 8 of

@@ -36,3 +36,10 @@ def launches(chain, T, hd, limbs, count):
 def test_forward_column_passes(chain, limbs, count, apart):
     T = 64 if chain[0] == 14 else 128
     assert launches(chain, T, 128, limbs, count).get("ntt_fwd_col", 0) == apart
+
+
+@pytest.mark.parametrize("count,apart", [(1, 2), (4, 2), (5, 0), (7, 0)])
+def test_inverse_column_passes(count, apart):
+    """N = 2^16, two digits: 32 count blocks of 16 columns a conversion, in the ModUp and in the quotient.  Up to 128 the
+    sources' column passes are launches of their own, as their targets are split over blocks."""
+    assert launches((16, 4, 2, 2, 50), 128, 128, 4, count).get("ntt_inv_col", 0) == apart
