@@ -123,7 +123,7 @@ struct Conv60Args {
 
 // The same conversion of at most 8 sources with every prime below 2^60 (sum60.h), the targets' constants [Qhat_i]_t 2^64
 // and [-Q_I]_t 2^64 as halves; blockIdx.z = conversion, group of t_per targets.  The five digits of two ciphertexts of 37
-// limbs at N = 2^16: 183 us in exact 128-bit sums, 131 so, 82 in one launch for all five.
+// limbs at N = 2^16: 183 us in exact 128-bit sums, 131 so, 82 in one launch for all five (70 in a long run).
 __global__ __launch_bounds__(kThreads) void k_conv60(const uint64_t *in, uint32_t in_stride, uint64_t *out,
                                                      uint32_t out_stride, Conv60Args args,
                                                      const ModQ *__restrict__ mods, uint32_t log_n, uint32_t t_per)

@@ -222,8 +222,8 @@ __device__ __forceinline__ void wsum8(const WsumKind &w, const Ct &ct, const Dim
 }
 
 // 1. rows q_l and P (s = 0: q_l, s > 0: p_{s-1}) of u: up[z P + o][k][s], raw doubles below 2q after the row pass.  One
-// wave, two rows of 256 points, 8 positions a thread.  16 ciphertexts of 13 limbs in two digits, three terms: 129 us,
-// 63% of the issue slots, 0.26 GB at 2.0 TB/s: the products, their conversions from words and the transform.
+// wave, two rows of 256 points, 8 positions a thread.  16 ciphertexts of 13 limbs in two digits, three terms: 122 us,
+// 63% of the issue slots, 0.26 GB at 2.2 TB/s: the products, their conversions from words and the transform.
 template <int ND, int NOUT>
 __global__ __launch_bounds__(64) void k_wsum_intt8(Args a, uint64_t *up, Dims d, uint32_t n,
                                                    const ulonglong2 *__restrict__ pmodq, const ModQ *__restrict__ mods,
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(256) void k_quot_col(uint64_t *up, Args a, Dims d, 
 // block (poly; 16 adjacent columns; group of t_per targets), 512 threads, 8 points of a 256-point column each, the
 // digits of the block's 4096 coefficients and w in registers for every target).  EXACT: K = 8.  COLS: `up` holds the
 // rows after the row pass of their inverse transforms, whose column passes run here as well (step 2 is not a launch of
-// its own). 32 polynomials, 8 special primes, 12 targets: 181 us, 63% of the issue slots with the two waves a SIMD that
+// its own). 32 polynomials, 8 special primes, 12 targets: 152 us, 63% of the issue slots with the two waves a SIMD that
 // the digits' registers allow.
 template <bool EXACT, bool COLS>
 __global__ __launch_bounds__(512) void k_quot_col8(uint64_t *out, const uint64_t *up, Args a, Dims d, uint32_t pages,
@@ -536,8 +536,8 @@ __global__ __launch_bounds__(256) void k_quot_col16(uint64_t *out, const uint64_
 
 // 4. out = (u - NTT(x)) (P q_l)^-1 (+ prev) on the rows below q_l: cw[z P + o][k][l] after the column pass.  Magnitudes
 // in units of q: column-pass rows below 4.3, transformed below 2.6, u below 2.6, products below 2.5: all below 8 q =
-// 2^53. 16 ciphertexts of 13 limbs: 211 us, 64% of the issue slots, 0.53 GB at 2.5 TB/s; 8 rotated and 8 unrotated
-// added to their pages: 201 us, 51%, 0.61 GB at 3.1 TB/s.
+// 2^53. 16 ciphertexts of 13 limbs: 198 us, 64% of the issue slots, 0.53 GB at 2.7 TB/s; 8 rotated and 8 unrotated
+// added to their pages: 194 us, 51%, 0.61 GB at 3.2 TB/s.
 template <int ND, int NOUT>
 __global__ __launch_bounds__(64) void k_wsum_fin8(Args a, const uint64_t *__restrict__ cw, Dims d, uint32_t n, Quot qt,
                                                   const ModQ *__restrict__ mods, const double *__restrict__ twf)

@@ -31,7 +31,9 @@ struct __attribute__((aligned(8))) Pair {
 __device__ __forceinline__ Pair ld2(const uint64_t *p) { return *(const Pair *)p; }
 
 // Block b of a launch over `tiles` tiles (a multiple of 8) of each of n ciphertexts: blocks go to the 8 XCDs in turn,
-// and the ciphertexts of one tile, which share its keys and tables, follow one another on one XCD.
+// and the ciphertexts of one tile, which share its keys and tables, follow one another on one XCD (16 of 13 limbs:
+// k_wsum_intt8 122 us against 178 with one ciphertext after the other, k_wsum_fin8 198 against 312; two of 37 limbs in
+// integers: k_wsum 195 against 284).
 __device__ __forceinline__ void tile_of(uint32_t n, uint32_t &z, uint32_t &tile)
 {
     const uint32_t xcd = blockIdx.x & 7u, rest = blockIdx.x >> 3;

@@ -6,7 +6,8 @@
 //      coefficient of the quotient by P, transforms it and writes (u - NTT(x)) (P q_l)^-1 (+ prev).
 // With the two launches of the ModUp that is five; through the ModDown, the rescale and the additions it was eight. 
 // Few ciphertexts are bounded by one row's latency a launch: one of 4 limbs at N = 2^12 takes 4, 7 and 11 us in the
-// three (35 us a call, as long as the host takes to issue it), three of 6 limbs at 2^13 8, 10 and 17 (56 us a call).
+// three (35 us a call, as long as the host takes to issue it), three of 6 limbs at 2^13 7, 11 and 17 (58 us a call).  The
+// sums of 1 could be formed where 2 and 3 read them, a row a block, in one launch fewer; that is not tried.
 #include "ntt_block.h"
 #include "ops.h"
 #include "wsum_args.h"

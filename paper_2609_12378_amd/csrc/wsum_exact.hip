@@ -17,9 +17,10 @@ constexpr int kThreads = 256;
 using namespace wsum;
 
 // u[z P + o][k][row][n] of ciphertext z, output o of P.  Two positions a thread: sigma_g reads the pair (j, j + 1) at
-// (j', j' ^ 1).  A digit's own rows are c1's.  Two ciphertexts of 37 limbs in five digits: 203 us (288 with a ciphertext
-// after the other, so that each read the keys from HBM, one position a thread and a product of seven multiplies), 0.67 GB at 3.3 TB/s, 79% of the issue
-// slots.  Sums of 30-bit halves (sum60.h) measured 197 us here and loads a digit ahead 211: neither is used.
+// (j', j' ^ 1).  A digit's own rows are c1's.  Two ciphertexts of 37 limbs in five digits: 195 us, 0.67 GB at 3.4 TB/s,
+// 79% of the issue slots, about 40% of the instructions in reduce128 (284 us with a ciphertext after the other, so that
+// each reads the keys from HBM).  In the first passes of a process, where it takes 203 us, sums of 30-bit halves (sum60.h)
+// measured 197 and loads a digit ahead 211: neither is used.
 template <int P>
 __global__ __launch_bounds__(kThreads) void k_wsum(Args a, uint64_t *u, Dims d, uint32_t n, uint32_t per_row,
                                                    const ulonglong2 *__restrict__ pmodq, const ModQ *__restrict__ mods)
@@ -309,8 +310,10 @@ ckks_status wsum_exact_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t p
     bool below60 = d.K <= 8;
     for (uint32_t i = 0; i < m.n; i++) below60 = below60 && ctx->primes[m.prime[i]] >> 60 == 0;
     for (uint32_t i = 0; i < level; i++) below60 = below60 && ctx->primes[i] >> 60 == 0;
-    // groups of targets until the grid has eight waves a SIMD (four polynomials of 36 targets: 53 us undivided, 48 in two
-    // groups, 55 in four, each of which forms the digits and w again)
+    // groups of targets until the grid has eight waves a SIMD: 2048 blocks (four polynomials of 36 targets: 53 us undivided,
+    // 48 in two groups, 55 in four, each of which forms the digits and w again).  us a call with none, groups to 1024, 2048,
+    // 4096 and 8192 blocks: one ciphertext of 37 limbs at N = 2^16 488, 479, 478, 483, 490; four 1364, 1361, 1364, 1366,
+    // 1380; one of 10 limbs 166, 164, 163, 167, 173; four at 2^14 154, 153, 153, 156, 159; one at 2^12 82, 78, 78, 78, 79
     const uint32_t blocks = grid_of(ctx, 1, 1, 1).x * polys, groups = std::min(level, std::max(1u, 2048u / blocks));
     const uint32_t t_per = (level + groups - 1) / groups;
     const dim3 grid(grid_of(ctx, 1, 1, 1).x, (level + t_per - 1) / t_per, polys);
