@@ -155,7 +155,11 @@ typedef enum {
     CKKS_OP_ATTN_APPLY = 14,    /* shape = {limbs of the scores, limbs of the values, tokens, head_dim} */
     CKKS_OP_ROPE_TABLES = 15,   /* rope_tables and cache_tables; shape unused */
     CKKS_OP_ROPE = 16,          /* shape = {limbs of the inputs, ciphertexts of one call} */
-    CKKS_OP_CACHE_APPEND = 17   /* shape = {limbs of the inputs, heads of one call}: any src, length and count */
+    CKKS_OP_CACHE_APPEND = 17,  /* shape = {limbs of the inputs, heads of one call}: any src, length and count */
+    CKKS_OP_POLY_EVAL = 18,     /* shape = {limbs of the inputs, ciphertexts, degree} */
+    CKKS_OP_RMS_NORM = 19,      /* shape = {limbs of the inputs, ciphertexts, tokens, layout, degree, newton} */
+    CKKS_OP_PROJECT_EPILOGUE = 20 /* shape = {limbs of the inputs, tokens, d_in, d_out, n1, layout, degree of the
+                                     activation (0: none), gate (0 or 1)} */
 } ckks_op;
 size_t ckks_workspace_bytes(const ckks_ctx *ctx, int op, const uint32_t *shape);
 ckks_status ckks_set_workspace(ckks_ctx *ctx, void *dev, size_t bytes);
@@ -504,6 +508,117 @@ ckks_status ckks_cache_append(ckks_ctx *ctx, const ckks_buf *k, const ckks_buf *
                               const ckks_rope_shape *shape, uint32_t src, uint32_t length, uint32_t count,
                               const uint64_t *dev_tables, const int32_t *key_steps, const uint64_t *const *dev_keys,
                               uint32_t n_keys, const ckks_cache *cache, const uint32_t *fork);
+
+/* ---- polynomials, norms and the projection's epilogue ----------------------- */
+
+/* What a transformer block does between its projections (the paper's SiLU(g) *
+ * u, norms and residual additions; its polynomials are not described).  The
+ * calls below are made of steps at level l, of ciphertexts a, b, z and integers:
+ *   (d0, d1, d2) = m (a0 b0, a0 b1 + a1 b0, a1 b1) + sum_i k_i (z0, z1, 0)_i
+ *   out          = Rescale((d0, d1) + ModDown(sum_j ModUp(d2)_j rlk_j)) + c
+ * (b a plaintext: no d2; operands with more limbs: the first l + 1; the stages
+ * are ckks_modup's, ckks_moddown's and ckks_rescale's), bit for bit.  k and c
+ * are the integers nearest to the products of values and scales that are given
+ * below, evaluated in double from left to right (ties to even); from 2^120 on
+ * the call is refused (CKKS_ESCALE).  q(L) is the top prime of L limbs.  A value
+ * keeps about log2 scale - 12 bits; scales near the primes keep the most.
+ * Needs special primes; any primes and rings the context takes.  Outputs may
+ * overlap neither inputs nor each other (CKKS_EINVAL); operands may be one
+ * another.  All checks are before the first launch. */
+
+/* sum_{i <= degree} coefs[i] T_i(t), T_i the Chebyshev polynomials, of t = (2 x -
+ * lo - hi) / (hi - lo): what a smooth function on [lo, hi] is replaced by (its
+ * interpolation at the degree + 1 Chebyshev nodes, for one).  Slots outside
+ * [lo, hi] give what the polynomial gives there: for degrees beyond a few, huge
+ * values.  coefs: host, finite; degree 1 to 127. */
+typedef struct {
+    const double *coefs;
+    uint32_t degree;
+    double lo, hi;
+} ckks_poly;
+
+/* The polynomial of `count` ciphertexts, equal n_limbs = L and scales S; with D
+ * the bits of `degree` (2^(D-1) <= degree < 2^D), out[r]: L - 1 - D limbs, scale
+ * S.  T_1 is a step of x with k = (2 / (hi - lo) s1) (q(L) / S), s1 = q(L - 1);
+ * T_i = 2 T_(i - i/2) T_(i/2) - T_(i mod 2), i > 1, ceil(log2 i) levels below it.
+ * A sum c of degree d wanted at depth e below T_1, scale s, is one step (from L'
+ * = L - e limbs) of the terms k_i T_i, k_i = c_i ((s q(L')) / scale(T_i)), if d <
+ * 2^b, b = min(3, max(1, D - 2)), and all T_i are there; else c = q T_m + r, m
+ * the largest power of two up to d: a step of the product of q's sum (depth e -
+ * 1, scale (s q(L')) / scale(T_m)) and T_m (q constant: a term of T_m) and of
+ * r's terms (m <= 2^b), or of r's sum (depth e - 1, scale s) times q_(L'-1).
+ * Scratch: CKKS_OP_POLY_EVAL.  Other errors: CKKS_EINVAL (polynomial,
+ * descriptors), CKKS_ELEVEL, CKKS_ESCALE, CKKS_EUNSUPPORTED. */
+ckks_status ckks_poly_eval(ckks_ctx *ctx, const ckks_buf *in, uint32_t count, const ckks_poly *poly,
+                           const uint64_t *dev_rlk, ckks_buf *out);
+
+/* A norm over the features of each token: `tokens` tokens a ciphertext (T, a power
+ * of two; D = N/2/T features), `features` of count D in all (the rest, if any,
+ * holds zeros), layout CKKS_TOKEN_MAJOR or CKKS_FEATURE_MAJOR.  newton: steps y <-
+ * y (3 - (mean + eps) y^2) / 2 after the polynomial (at most 4); without one eps
+ * is not used. */
+typedef struct {
+    uint32_t tokens, features, layout, newton;
+    double eps;
+} ckks_norm_shape;
+
+/* out = w x f(mean) + residual_scale residual, mean = sum x^2 / features of a token,
+ * f = inv_root (about (mean + eps)^-1/2 on its interval) refined by the Newton
+ * steps.  in: `count` ciphertexts, n_limbs = L, equal scales S.  weights: null,
+ * `count` plaintexts (norm weights, a gate or residual scale folded in by their
+ * encoder) or `count` ciphertexts (a gate computed from data); residual: null or
+ * `count` ciphertexts (the stream that the block's output joins; it may be `in`).
+ * mask: the plaintext of 1 at the first feature of every token and 0 elsewhere,
+ * token-major alone.  Each of these has one scale and the limbs that it is used at,
+ * or more.
+ *
+ * With D' the bits of the degree and Lv = L - 1, token-major L - 2:
+ *   v    the step of sum_r x_r x_r; then, per round of radix R (at most 16, log2 of
+ *        the product D's, as even as they go, larger first), v += ModDown(sum_{0<k<R}
+ *        key switch and P sigma(c0) of the left rotations by k times the stride),
+ *        stride T (token-major 1) times the earlier radixes; token-major then a
+ *        step of v mask and the rounds again with strides -1
+ *   y    the polynomial of v / features, as in ckks_poly_eval; Lv - 1 - D' limbs
+ *   step y' = -(n y)(y y) + 3 y, n = v / features + eps a step from Lv limbs, at the
+ *        scale that makes y' land on its own
+ *   out  the step of y, m limbs, with (w x), the step of x and w from m + 1 limbs,
+ *        and the residual: m - 1 limbs, scale S
+ * so m = Lv - 1 - D' - 2 newton >= 2; L = 4 + D' + 2 newton (+ 1) at least.  Keys
+ * (Galois; steps modulo N/2): the rounds' rotations, both signs token-major; a round
+ * of 16 reads 15 keys for one ModUp and one ModDown.
+ * Scratch: CKKS_OP_RMS_NORM.  Other errors as ckks_poly_eval's, CKKS_ENOKEY. */
+ckks_status ckks_rms_norm(ckks_ctx *ctx, const ckks_buf *in, uint32_t count, const ckks_norm_shape *shape,
+                          const ckks_poly *inv_root, const ckks_buf *weights, const ckks_buf *mask,
+                          const ckks_buf *residual, double residual_scale, const uint64_t *dev_rlk,
+                          const int32_t *key_steps, const uint64_t *const *dev_keys, uint32_t n_keys, ckks_buf *out);
+
+/* What follows a projection, each null if it does not: bias (d_out / D plaintexts),
+ * act, gate and residual (d_out / D ciphertexts), of one scale each.  dev_rlk: for
+ * act and gate.  Host memory but for the buffers' data and the key. */
+typedef struct {
+    const ckks_buf *bias;
+    const ckks_poly *act;
+    const ckks_buf *gate, *residual;
+    double residual_scale;
+    const uint64_t *dev_rlk;
+} ckks_epilogue;
+
+/* out_j = gate_j act((X W)_j + bias_j) + residual_scale residual_j: ckks_linear_project
+ * (layout CKKS_FEATURE_MAJOR) or ckks_linear_project_tm with another end.  Their
+ * sums before the rescale, from weights encoded at scale q(L) (s / S), take k bias
+ * and, if nothing else follows, k residual, and are rescaled: to T_1 of the
+ * activation (s = 2 / (hi - lo) q(L - 1), so its interval costs no level), to what
+ * the gate multiplies (s = S q(L - 1) / scale(gate)), or to the output (s = S).
+ * The activation's sum follows as in ckks_poly_eval (with its residual in the last
+ * step if there is no gate, at scale S q(m) / scale(gate) if there is), then the
+ * gate's step from m limbs.  out[j]: L - 1 limbs less the activation's D and one
+ * for a gate; scale S.  The weights' scale is at most 2^62 (CKKS_ESCALE; and see
+ * ckks_linear_project for the bound of weights times scale).  Other arguments and
+ * errors as of the projections and ckks_poly_eval; scratch: CKKS_OP_PROJECT_EPILOGUE. */
+ckks_status ckks_linear_project_epilogue(ckks_ctx *ctx, const ckks_buf *in, const double *dev_W,
+                                         const ckks_proj_shape *shape, uint32_t layout, const ckks_epilogue *epilogue,
+                                         const int32_t *key_steps, const uint64_t *const *dev_keys, uint32_t n_keys,
+                                         ckks_buf *out);
 
 /* ---- measurement helpers ------------------------------------------------- */
 

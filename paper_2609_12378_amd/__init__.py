@@ -12,14 +12,14 @@ import ctypes
 import math
 import os
 from dataclasses import dataclass
-from typing import Dict, List, Optional, Sequence
+from typing import Callable, Dict, List, Optional, Sequence
 
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libckks_mi.so")
 
-__all__ = ["Context", "Buf", "CkksError", "load_library", "rope_inv_freq", "LIB_PATH"]
+__all__ = ["Context", "Buf", "Poly", "Epilogue", "CkksError", "load_library", "rope_inv_freq", "LIB_PATH"]
 
 
 class CkksError(RuntimeError):
@@ -53,6 +53,20 @@ class _RopeShape(ctypes.Structure):
 class _Cache(ctypes.Structure):
     _fields_ = [("k_pages", ctypes.POINTER(_Buf)), ("v_pages", ctypes.POINTER(_Buf)), ("n_pages", ctypes.c_uint32),
                 ("table", ctypes.POINTER(ctypes.c_uint32)), ("n_blocks", ctypes.c_uint32)]
+
+
+class _Poly(ctypes.Structure):
+    _fields_ = [("coefs", ctypes.POINTER(ctypes.c_double)), ("degree", ctypes.c_uint32), ("lo", ctypes.c_double),
+                ("hi", ctypes.c_double)]
+
+
+class _NormShape(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_uint32) for f in ("tokens", "features", "layout", "newton")] + [("eps", ctypes.c_double)]
+
+
+class _Epilogue(ctypes.Structure):
+    _fields_ = [("bias", ctypes.POINTER(_Buf)), ("act", ctypes.POINTER(_Poly)), ("gate", ctypes.POINTER(_Buf)),
+                ("residual", ctypes.POINTER(_Buf)), ("residual_scale", ctypes.c_double), ("rlk", ctypes.c_void_p)]
 
 
 _LIB = None
@@ -106,6 +120,11 @@ _SIGS = {
     "ckks_cache_tables": (ctypes.c_int, [_VP, ctypes.POINTER(_RopeShape), _U32, _U32, _VP, _VP, _U32, _VP]),
     "ckks_cache_append": (ctypes.c_int, [_VP, _BP, _BP, _U32, ctypes.POINTER(_RopeShape), _U32, _U32, _U32, _VP, _VP,
                                          _VP, _U32, ctypes.POINTER(_Cache), _VP]),
+    "ckks_poly_eval": (ctypes.c_int, [_VP, _BP, _U32, ctypes.POINTER(_Poly), _VP, _BP]),
+    "ckks_rms_norm": (ctypes.c_int, [_VP, _BP, _U32, ctypes.POINTER(_NormShape), ctypes.POINTER(_Poly), _BP, _BP, _BP,
+                                     _DBL, _VP, _VP, _VP, _U32, _BP]),
+    "ckks_linear_project_epilogue": (ctypes.c_int, [_VP, _BP, _VP, ctypes.POINTER(_ProjShape), _U32,
+                                                    ctypes.POINTER(_Epilogue), _VP, _VP, _U32, _BP]),
     "ckks_profile_enable": (ctypes.c_int, [_VP, ctypes.c_int]),
     "ckks_profile_read": (ctypes.c_int, [_VP, ctypes.c_char_p, ctypes.POINTER(_DBL), ctypes.POINTER(_U64),
                                          ctypes.POINTER(_DBL), ctypes.POINTER(_DBL)]),
@@ -230,6 +249,58 @@ class Buf:
         return _Buf(_ptr(d), d.shape[0], d.shape[1], float(self.scale))
 
 
+@dataclass(frozen=True)
+class Poly:
+    """sum_i coefs[i] T_i(t), t = (2 x - lo - hi) / (hi - lo): a function on [lo, hi] by Chebyshev polynomials."""
+    coefs: Sequence[float]
+    lo: float
+    hi: float
+
+    @classmethod
+    def fit(cls, fn: Callable[[float], float], degree: int, lo: float, hi: float) -> "Poly":
+        """fn interpolated at the degree + 1 Chebyshev nodes of [lo, hi]."""
+        if degree < 1 or not lo < hi:
+            raise CkksError("Poly.fit: degree %r on [%r, %r]" % (degree, lo, hi))
+        n = degree + 1
+        at = [math.cos(math.pi * (k + 0.5) / n) for k in range(n)]
+        f = [float(fn((hi - lo) / 2 * x + (hi + lo) / 2)) for x in at]
+        c = [2.0 / n * sum(f[k] * math.cos(math.pi * j * (k + 0.5) / n) for k in range(n)) for j in range(n)]
+        return cls((c[0] / 2, *c[1:]), float(lo), float(hi))
+
+    @property
+    def degree(self) -> int:
+        return len(self.coefs) - 1
+
+    @property
+    def depth(self) -> int:
+        """Levels of the sum below T_1's, which takes one itself."""
+        return max(0, self.degree).bit_length()
+
+    def __call__(self, x: float) -> float:
+        """Its value in plain arithmetic (Clenshaw's recurrence)."""
+        t, b1, b2 = (2 * x - self.lo - self.hi) / (self.hi - self.lo), 0.0, 0.0
+        for c in reversed(self.coefs[1:]):
+            b1, b2 = 2 * t * b1 - b2 + c, b1
+        return t * b1 - b2 + self.coefs[0]
+
+    def c(self) -> _Poly:
+        if len(self.coefs) < 1:
+            raise CkksError("a polynomial without coefficients")
+        return _Poly((ctypes.c_double * len(self.coefs))(*self.coefs), self.degree, self.lo, self.hi)
+
+
+@dataclass
+class Epilogue:
+    """What follows a projection's sums: gate act(X W + bias) + residual_scale residual, each part optional.  bias: a
+    plaintext an output; gate and residual: a ciphertext an output; rlk: the relinearisation key of act and gate."""
+    bias: Optional[Sequence[Buf]] = None
+    act: Optional[Poly] = None
+    gate: Optional[Sequence[Buf]] = None
+    residual: Optional[Sequence[Buf]] = None
+    residual_scale: float = 1.0
+    rlk: Optional[torch.Tensor] = None
+
+
 class Context:
     """A libckks_mi context on the current HIP device and stream."""
 
@@ -285,7 +356,7 @@ class Context:
     # workspace op codes (ckks_op)
     OP_ENCODE, OP_DECODE, OP_ENCRYPT, OP_DECRYPT, OP_KEYGEN, OP_RESCALE, OP_ROTATE, OP_MUL_RELIN, OP_MODUP, \
         OP_MODDOWN, OP_LINEAR_PROJECT, OP_LINEAR_PROJECT_TM, OP_ATTN_SCORES, OP_ATTN_APPLY, OP_ROPE_TABLES, OP_ROPE, \
-        OP_CACHE_APPEND = range(1, 18)
+        OP_CACHE_APPEND, OP_POLY_EVAL, OP_RMS_NORM, OP_PROJECT_EPILOGUE = range(1, 21)
 
     def workspace_bytes(self, op: int, shape=()) -> int:
         """Device bytes one call of `op` takes from the arena or workspace, for the given shape."""
@@ -531,8 +602,9 @@ class Context:
 
     def linear_project(self, cts: Sequence[Buf], W: torch.Tensor, tokens: int, n1: int,
                        keys: Dict[int, torch.Tensor], outs: Optional[Sequence[Buf]] = None,
-                       layout: str = "fm") -> List[Buf]:
-        """Y = X W on packed ciphertexts; layout "fm" (slot f*tokens + t) or "tm" (slot t*D + f)."""
+                       layout: str = "fm", epilogue: Optional[Epilogue] = None) -> List[Buf]:
+        """Y = X W on packed ciphertexts; layout "fm" (slot f*tokens + t) or "tm" (slot t*D + f).  With an epilogue: gate
+        act(Y + bias) + residual_scale residual, fewer limbs by the activation's depth and one for a gate."""
         if not isinstance(W, torch.Tensor) or W.dim() != 2:
             raise CkksError("linear_project: W must be a 2-d (d_in, d_out) tensor")
         d_in, d_out = W.shape
@@ -540,8 +612,10 @@ class Context:
         D = (self.n // 2) // tokens
         n_out = d_out // D
         level = cts[0].level
+        if epilogue is not None:
+            level -= (epilogue.act.depth if epilogue.act else 0) + (epilogue.gate is not None)
         if outs is None:
-            outs = [Buf(self._empty(cts[0].data, 2, level), cts[0].scale) for _ in range(n_out)]
+            outs = [Buf(self._empty(cts[0].data, 2, max(1, level)), cts[0].scale) for _ in range(n_out)]
         # the library reads d_in/D input and d_out/D output descriptors: never hand it shorter arrays
         if D > 0 and d_in % D == 0 and d_out % D == 0 and (len(cts) < d_in // D or len(outs) < n_out):
             raise ValueError("linear_project: %d inputs and %d outputs given, the shape needs %d and %d"
@@ -554,11 +628,100 @@ class Context:
         shape = _ProjShape(tokens, d_in, d_out, n1)
         if layout not in ("fm", "tm"):
             raise ValueError("layout must be 'fm' or 'tm'")
-        fn = "ckks_linear_project" if layout == "fm" else "ckks_linear_project_tm"
-        _check(getattr(self.lib, fn)(self.h, inb, pw, ctypes.byref(shape), ks, kp, len(steps), ob), fn)
+        if epilogue is None:
+            fn = "ckks_linear_project" if layout == "fm" else "ckks_linear_project_tm"
+            _check(getattr(self.lib, fn)(self.h, inb, pw, ctypes.byref(shape), ks, kp, len(steps), ob), fn)
+        else:
+            e = epilogue
+            lists = [None if x is None else self._bufs(x, n_out, name)
+                     for x, name in ((e.bias, "bias"), (e.gate, "gate"), (e.residual, "residual"))]
+            pk = None if e.rlk is None else self._key(e.rlk, "relinearisation key")
+            act = None if e.act is None else ctypes.pointer(e.act.c())
+            ce = _Epilogue(lists[0], act, lists[1], lists[2], float(e.residual_scale), pk)
+            self._used(W, e.rlk, *keys.values(), *[b.data for x in (cts, outs, e.bias, e.gate, e.residual) for b in x or ()])
+            _check(self.lib.ckks_linear_project_epilogue(self.h, inb, pw, ctypes.byref(shape), self._LAYOUTS[layout],
+                                                         ctypes.byref(ce), ks, kp, len(steps), ob),
+                   "ckks_linear_project_epilogue")
         for o, b in zip(outs, ob):
             o.scale = b.scale
         return list(outs)
+
+    # ---------------- polynomials and norms ----------------
+    def _bufs(self, x: Sequence[Buf], count: int, what: str):
+        """Descriptors of a list that the library reads `count` of."""
+        if len(x) < count:
+            raise CkksError("%s: %d buffers, %d needed" % (what, len(x), count))
+        return (_Buf * max(1, count))(*[b.c(self.n) for b in x[:count]])
+
+    def _outs(self, outs: Optional[Sequence[Buf]], cts: Sequence[Buf], limbs: int, what: str) -> List[Buf]:
+        if outs is None:
+            outs = [Buf(self._empty(c.data, 2, max(1, limbs)), c.scale) for c in cts]
+        if len(outs) < len(cts):
+            raise CkksError("%s: %d outputs for %d inputs" % (what, len(outs), len(cts)))
+        return list(outs[:len(cts)])
+
+    def poly_eval(self, cts: Sequence[Buf], poly: Poly, rlk: torch.Tensor, outs: Optional[Sequence[Buf]] = None) -> List[Buf]:
+        """The polynomial of every ciphertext's slots: 1 + poly.depth limbs fewer, the same scale."""
+        if not cts:
+            return []
+        outs = self._outs(outs, cts, cts[0].n_limbs - 1 - poly.depth, "poly_eval")
+        ib, ob = self._bufs(cts, len(cts), "poly_eval"), self._bufs(outs, len(cts), "poly_eval")
+        cp, pk = poly.c(), self._key(rlk, "relinearisation key")
+        self._used(rlk, *[b.data for x in (cts, outs) for b in x])
+        _check(self.lib.ckks_poly_eval(self.h, ib, len(cts), ctypes.byref(cp), pk, ob), "ckks_poly_eval")
+        for o, b in zip(outs, ob):
+            o.scale = b.scale
+        return outs
+
+    def rms_norm(self, cts: Sequence[Buf], tokens: int, features: int, inv_root: Poly, rlk: torch.Tensor,
+                 keys: Dict[int, torch.Tensor], layout: str = "fm", weights: Optional[Sequence[Buf]] = None,
+                 mask: Optional[Buf] = None, newton: int = 0, eps: float = 0.0,
+                 residual: Optional[Sequence[Buf]] = None, residual_scale: float = 1.0,
+                 outs: Optional[Sequence[Buf]] = None) -> List[Buf]:
+        """weights x inv_root(mean of x^2 over a token's features) + residual_scale residual; `newton` steps refine the
+        inverse root of mean + eps.  weights: plaintexts or ciphertexts; mask: norm_mask(), token-major alone."""
+        if layout not in self._LAYOUTS:
+            raise CkksError("layout must be 'fm' or 'tm'")
+        for name, v in (("tokens", tokens), ("features", features), ("newton", newton)):
+            if not isinstance(v, int) or not 0 <= v < 1 << 32:
+                raise CkksError("%s: %r is not a 32-bit count" % (name, v))
+        if not cts:
+            return []
+        n, limbs = len(cts), cts[0].n_limbs
+        outs = self._outs(outs, cts, limbs - 3 - (layout == "tm") - inv_root.depth - 2 * newton, "rms_norm")
+        ib, ob = self._bufs(cts, n, "rms_norm"), self._bufs(outs, n, "rms_norm")
+        wb = None if weights is None else self._bufs(weights, n, "weights")
+        rb = None if residual is None else self._bufs(residual, n, "residual")
+        mb = None if mask is None else self._bufs([mask], 1, "mask")
+        shape = _NormShape(tokens, features, self._LAYOUTS[layout], newton, float(eps))
+        cp, pk = inv_root.c(), self._key(rlk, "relinearisation key")
+        ks, kp, nk = self._keys_of(keys)
+        self._used(rlk, *keys.values(), *[b.data for x in (cts, outs, weights, residual, [mask] if mask else None)
+                                          for b in x or ()])
+        _check(self.lib.ckks_rms_norm(self.h, ib, n, ctypes.byref(shape), ctypes.byref(cp), wb, mb, rb,
+                                      float(residual_scale), pk, ks, kp, nk, ob), "ckks_rms_norm")
+        for o, b in zip(outs, ob):
+            o.scale = b.scale
+        return outs
+
+    def norm_mask(self, tokens: int, n_limbs: int, scale: float) -> Buf:
+        """The plaintext that rms_norm() needs in the token-major layout: 1 at every token's first feature."""
+        if not 1 <= tokens <= self.n // 2 or (self.n // 2) % tokens:
+            raise CkksError("norm_mask: %d tokens do not divide %d slots" % (tokens, self.n // 2))
+        with torch.cuda.stream(self._stream):
+            z = torch.zeros((tokens, self.n // 2 // tokens), dtype=torch.float64, device=torch.device("cuda", self.device))
+            z[:, 0] = 1.0
+            return self.encode(z.reshape(-1), None, scale, n_limbs)
+
+    @staticmethod
+    def norm_steps(slots: int, tokens: int, layout: str = "fm") -> List[int]:
+        """The rotation steps rms_norm() needs keys for."""
+        bits, unit, steps = (slots // tokens).bit_length() - 1, tokens if layout == "fm" else 1, set()
+        for left in range(-(-bits // 4), 0, -1):
+            b = -(-bits // left)
+            steps |= {sign * k * unit % slots for k in range(1, 1 << b) for sign in ((1, -1) if layout == "tm" else (1,))}
+            bits, unit = bits - b, unit << b
+        return sorted(steps)
 
     def _attention(self, fn: str, a_cts: Sequence[Buf], b_cts: Sequence[Buf], b_of_a: Sequence[int], tokens: int,
                    head_dim: int, rlk: torch.Tensor, keys: Dict[int, torch.Tensor], outs: Optional[Sequence[Buf]]):

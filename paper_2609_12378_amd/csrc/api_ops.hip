@@ -82,6 +82,15 @@ size_t op_workspace_bytes(const ckks_ctx *ctx, int op, const uint32_t *shape)
     case CKKS_OP_CACHE_APPEND:
         if (!shape) return SIZE_MAX;
         return append_workspace_bytes(ctx, shape[0], shape[1]);
+    case CKKS_OP_POLY_EVAL:
+        if (!shape) return SIZE_MAX;
+        return poly_workspace_bytes(ctx, shape[0], shape[1], shape[2]);
+    case CKKS_OP_RMS_NORM:
+        if (!shape) return SIZE_MAX;
+        return norm_workspace_bytes(ctx, shape[0], shape[1], shape[2], shape[3], shape[4], shape[5]);
+    case CKKS_OP_PROJECT_EPILOGUE:
+        if (!shape) return SIZE_MAX;
+        return epilogue_workspace_bytes(ctx, shape);
     default: return SIZE_MAX;
     }
 }

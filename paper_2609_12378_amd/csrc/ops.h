@@ -2,6 +2,8 @@
 // projection kernels (definitions in ops.hip, keyswitch.hip, encode.hip,
 // project.hip).
 #pragma once
+#include <functional>
+
 #include "ckks_internal.h"
 
 enum { EW_ADD = 0, EW_SUB = 1, EW_MUL = 2 };
@@ -201,6 +203,28 @@ size_t proj_tm_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t tokens,
                                uint32_t n1);
 size_t attn_scores_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t tokens, uint32_t head_dim);
 size_t attn_apply_workspace_bytes(const ckks_ctx *ctx, uint32_t Lp, uint32_t Lv, uint32_t tokens, uint32_t head_dim);
+
+// A projection that ends otherwise than in its rescale (epilogue.hip): the weights' scale, bytes kept for the hook before
+// the projection's scratch, the least that the arena has to hold in all, and what becomes of the sums tot
+// ([jc][2][L][N]) of outputs j0 .. j0 + jc - 1.  mem: the arena's start, set before the first launch.
+struct ProjHook {
+    double w_scale;
+    size_t kept, least;
+    void *mem;
+    std::function<ckks_status(const uint64_t *tot, uint32_t j0, uint32_t jc)> finish;
+};
+ckks_status project_fm(ckks_ctx *ctx, const ckks_buf *in, const double *W, const ckks_proj_shape *shape,
+                       const int32_t *key_steps, const uint64_t *const *keys, uint32_t n_keys, ckks_buf *out,
+                       ProjHook *hook);
+ckks_status project_tm(ckks_ctx *ctx, const ckks_buf *in, const double *W, const ckks_proj_shape *shape,
+                       const int32_t *key_steps, const uint64_t *const *keys, uint32_t n_keys, ckks_buf *out,
+                       ProjHook *hook);
+
+// polynomials, norms and the projection's epilogue (nonlinear.hip, epilogue.hip)
+size_t poly_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t count, uint32_t degree);
+size_t norm_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t count, uint32_t tokens, uint32_t layout,
+                            uint32_t degree, uint32_t newton);
+size_t epilogue_workspace_bytes(const ckks_ctx *ctx, const uint32_t *shape);
 
 // rotary positions and the cache (rope.hip)
 size_t rope_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t count);

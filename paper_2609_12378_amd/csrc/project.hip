@@ -424,12 +424,11 @@ size_t proj_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t tokens, ui
     return proj_scratch(ctx, L, D, d_in, d_out, n1).total * 8;
 }
 
-extern "C" ckks_status ckks_linear_project(ckks_ctx *ctx, const ckks_buf *in, const double *W,
-                                           const ckks_proj_shape *shape, const int32_t *key_steps,
-                                           const uint64_t *const *keys, uint32_t n_keys, ckks_buf *out)
+ckks_status project_fm(ckks_ctx *ctx, const ckks_buf *in, const double *W, const ckks_proj_shape *shape,
+                       const int32_t *key_steps, const uint64_t *const *keys, uint32_t n_keys, ckks_buf *out,
+                       ProjHook *hook)
 {
-    clear_error();
-    CK_REQUIRE(ctx && in && W && shape && out, CKKS_EINVAL, "linear_project: null argument");
+    CK_REQUIRE(ctx && in && W && shape, CKKS_EINVAL, "linear_project: null argument");
     CK_REQUIRE(ctx->n_p > 0, CKKS_EUNSUPPORTED, "linear_project: the context has no special primes");
     const uint32_t T = shape->tokens, slots = ctx->n / 2;
     CK_REQUIRE(T >= 1 && slots % T == 0, CKKS_EINVAL, "linear_project: %u tokens do not divide %u slots", T, slots);
@@ -448,7 +447,7 @@ extern "C" ckks_status ckks_linear_project(ckks_ctx *ctx, const ckks_buf *in, co
                    in[i].n_limbs, L);
         CK_REQUIRE(in[i].scale == in[0].scale, CKKS_ESCALE, "linear_project: input scales differ");
     }
-    for (uint32_t j = 0; j < n_out; j++) {
+    for (uint32_t j = 0; !hook && j < n_out; j++) {
         CK_REQUIRE(out[j].data && out[j].n_polys == 2 && out[j].n_limbs == level, CKKS_EINVAL,
                    "linear_project: output %u must be a ciphertext with %u limbs", j, level);
     }
@@ -479,8 +478,10 @@ extern "C" ckks_status ckks_linear_project(ckks_ctx *ctx, const ckks_buf *in, co
     const size_t m_w = ps.m_w, fft_w = ps.fft_w, ks_w = ps.ks_w, wd_w = ps.wd_w, total = ps.total;
     const bool diag = ps.diag;
     void *w;
-    CK_TRY(ctx_scratch(ctx, total * 8, &w));
-    uint64_t *xrot = (uint64_t *)w;
+    const size_t kept = hook ? hook->kept : 0;
+    CK_TRY(ctx_scratch(ctx, std::max(kept + total * 8, hook ? hook->least : 0), &w));
+    if (hook) hook->mem = w;
+    uint64_t *xrot = (uint64_t *)((char *)w + kept);
     uint64_t *acc = xrot + xrot_w;
     uint64_t *tot = acc + acc_w;
     uint64_t *rot = tot + tot_w;
@@ -514,7 +515,7 @@ extern "C" ckks_status ckks_linear_project(ckks_ctx *ctx, const ckks_buf *in, co
     if (fused) CK_TRY(launch_to_f64(ctx, xrot, xrot_w));
 
     // ---- 2./3. tiles of output blocks
-    const double delta_w = (double)ctx->primes[level];
+    const double delta_w = hook ? hook->w_scale : (double)ctx->primes[level];
     for (uint32_t j0 = 0; j0 < n_out; j0 += Jt) {
         const uint32_t jc = std::min<uint32_t>(Jt, n_out - j0);
         // with few outputs several giant steps share the launches (kernels and key switching alike): as many as fill the
@@ -568,10 +569,23 @@ extern "C" ckks_status ckks_linear_project(ckks_ctx *ctx, const ckks_buf *in, co
             CK_TRY(ks_moddown(ctx, uacc, 2 * jc, level, nullptr, 1, nullptr, rot, ksw));
             CK_TRY(launch_binary(ctx, tot, tot, rot, jc * 2 * L, limb_range(0, L), EW_ADD));
         }
+        if (hook) {
+            CK_TRY(hook->finish(tot, j0, jc));
+            continue;
+        }
         std::vector<uint64_t *> outs(jc);
         for (uint32_t jj = 0; jj < jc; jj++) outs[jj] = out[j0 + jj].data;
         CK_TRY(rescale_each(ctx, tot, jc, level, outs.data(), rot));
         for (uint32_t jj = 0; jj < jc; jj++) out[j0 + jj].scale = in[0].scale;
     }
     return CKKS_OK;
+}
+
+extern "C" ckks_status ckks_linear_project(ckks_ctx *ctx, const ckks_buf *in, const double *W,
+                                           const ckks_proj_shape *shape, const int32_t *key_steps,
+                                           const uint64_t *const *keys, uint32_t n_keys, ckks_buf *out)
+{
+    clear_error();
+    CK_REQUIRE(out, CKKS_EINVAL, "linear_project: null argument");
+    return project_fm(ctx, in, W, shape, key_steps, keys, n_keys, out, nullptr);
 }

@@ -687,12 +687,11 @@ size_t proj_tm_workspace_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t tokens,
     return tm_scratch(ctx, L, D, d_in, d_out, n1).total * 8;
 }
 
-extern "C" ckks_status ckks_linear_project_tm(ckks_ctx *ctx, const ckks_buf *in, const double *W,
-                                              const ckks_proj_shape *shape, const int32_t *key_steps,
-                                              const uint64_t *const *keys, uint32_t n_keys, ckks_buf *out)
+ckks_status project_tm(ckks_ctx *ctx, const ckks_buf *in, const double *W, const ckks_proj_shape *shape,
+                       const int32_t *key_steps, const uint64_t *const *keys, uint32_t n_keys, ckks_buf *out,
+                       ProjHook *hook)
 {
-    clear_error();
-    CK_REQUIRE(ctx && in && W && shape && out, CKKS_EINVAL, "linear_project_tm: null argument");
+    CK_REQUIRE(ctx && in && W && shape, CKKS_EINVAL, "linear_project_tm: null argument");
     CK_REQUIRE(ctx->n_p > 0, CKKS_EUNSUPPORTED, "linear_project_tm: the context has no special primes");
     const uint32_t T = shape->tokens, n1 = shape->n1;
     const uint32_t L = in[0].n_limbs, level = L - 1;
@@ -706,7 +705,7 @@ extern "C" ckks_status ckks_linear_project_tm(ckks_ctx *ctx, const ckks_buf *in,
                    in[i].n_limbs, L);
         CK_REQUIRE(in[i].scale == in[0].scale, CKKS_ESCALE, "linear_project_tm: input scales differ");
     }
-    for (uint32_t j = 0; j < n_out; j++)
+    for (uint32_t j = 0; !hook && j < n_out; j++)
         CK_REQUIRE(out[j].data && out[j].n_polys == 2 && out[j].n_limbs == level, CKKS_EINVAL,
                    "linear_project_tm: output %u must be a ciphertext with %u limbs", j, level);
     auto find_key = [&](int32_t st) -> const uint64_t * {
@@ -734,10 +733,13 @@ extern "C" ckks_status ckks_linear_project_tm(ckks_ctx *ctx, const ckks_buf *in,
     TmScratch ts = tm_scratch(ctx, L, D, shape->d_in, shape->d_out, n1);
     void *w;
     ckks_status st = CKKS_OK;
+    const size_t kept = hook ? hook->kept : 0;
     // a workspace or a card without the room for several giant steps per launch: fewer of them, down to one
     const uint32_t G = most_groups(
         ctx->arena, ts.G,
-        [&](uint32_t g) { return tm_scratch(ctx, L, D, shape->d_in, shape->d_out, n1, g).total * 8; },
+        [&](uint32_t g) {
+            return std::max(kept + tm_scratch(ctx, L, D, shape->d_in, shape->d_out, n1, g).total * 8, hook ? hook->least : 0);
+        },
         [&](size_t bytes) {
             if (st == CKKS_ENOMEM) {   // the runtime's and the library's record of the larger request
                 (void)hipGetLastError();
@@ -748,7 +750,8 @@ extern "C" ckks_status ckks_linear_project_tm(ckks_ctx *ctx, const ckks_buf *in,
         });
     CK_TRY(st);
     ts = tm_scratch(ctx, L, D, shape->d_in, shape->d_out, n1, G);
-    uint64_t *x2 = (uint64_t *)w;  // [n_in][n1][xr, xw][2][L][N]
+    if (hook) hook->mem = w;
+    uint64_t *x2 = (uint64_t *)((char *)w + kept);  // [n_in][n1][xr, xw][2][L][N]
     uint64_t *acc = x2 + ts.x2_w;
     uint64_t *tot = acc + ts.acc_w;
     uint64_t *rot = tot + ts.tot_w;
@@ -776,7 +779,7 @@ extern "C" ckks_status ckks_linear_project_tm(ckks_ctx *ctx, const ckks_buf *in,
         CK_TRY(launch_to_f64(ctx, x2, ts.x2_w));
 
     // 2./3. tiles of output ciphertexts, giant steps, sub-batches of pairs
-    const double delta_w = (double)ctx->primes[level];
+    const double delta_w = hook ? hook->w_scale : (double)ctx->primes[level];
     uint32_t logT = 0;
     while ((1u << logT) < T) logT++;
     uint32_t logD = 0;
@@ -817,10 +820,23 @@ extern "C" ckks_status ckks_linear_project_tm(ckks_ctx *ctx, const ckks_buf *in,
             CK_TRY(ks_moddown(ctx, uacc, 2 * jc, level, nullptr, 1, nullptr, rot, ksw));
             CK_TRY(launch_binary(ctx, tot, tot, rot, jc * 2 * L, limb_range(0, L), EW_ADD));
         }
+        if (hook) {
+            CK_TRY(hook->finish(tot, j0, jc));
+            continue;
+        }
         std::vector<uint64_t *> outs(jc);
         for (uint32_t jj = 0; jj < jc; jj++) outs[jj] = out[j0 + jj].data;
         CK_TRY(rescale_each(ctx, tot, jc, level, outs.data(), rot));
         for (uint32_t jj = 0; jj < jc; jj++) out[j0 + jj].scale = in[0].scale;
     }
     return CKKS_OK;
+}
+
+extern "C" ckks_status ckks_linear_project_tm(ckks_ctx *ctx, const ckks_buf *in, const double *W,
+                                              const ckks_proj_shape *shape, const int32_t *key_steps,
+                                              const uint64_t *const *keys, uint32_t n_keys, ckks_buf *out)
+{
+    clear_error();
+    CK_REQUIRE(out, CKKS_EINVAL, "linear_project_tm: null argument");
+    return project_tm(ctx, in, W, shape, key_steps, keys, n_keys, out, nullptr);
 }

@@ -5,9 +5,9 @@
 //            outside the new tokens' slots of the page; values take one term with a 0/1 weight.
 #include <algorithm>
 #include <cmath>
-#include <new>
 #include <vector>
 
+#include "api_args.h"
 #include "ckks_internal.h"
 #include "ntt_core.h"
 #include "ops.h"
@@ -105,41 +105,6 @@ ckks_status check_shape(const ckks_ctx *ctx, const ckks_rope_shape *s, const cha
 // left rotation of the pair above, in slots
 int64_t pair_step(const Shape &s) { return (int64_t)(s.interleaved ? 1 : s.rot_dim / 2) * (s.fm ? s.tokens : 1); }
 
-ckks_status check_cts(const ckks_buf *b, uint32_t n, uint32_t L, const char *what, const char *name)
-{
-    for (uint32_t i = 0; i < n; i++) {
-        CK_REQUIRE(b[i].data && b[i].n_polys == 2, CKKS_EINVAL, "%s: %s %u is not a ciphertext", what, name, i);
-        CK_REQUIRE(b[i].n_limbs == L, CKKS_ELEVEL, "%s: %s %u has %u limbs, expected %u", what, name, i, b[i].n_limbs, L);
-    }
-    return CKKS_OK;
-}
-ckks_status check_scales(const ckks_buf *b, uint32_t n, const char *what, const char *name)
-{
-    for (uint32_t i = 0; i < n; i++)
-        CK_REQUIRE(b[i].scale == b[0].scale, CKKS_ESCALE, "%s: %s scales differ", what, name);
-    return CKKS_OK;
-}
-
-struct Range {
-    const uint64_t *p;
-    size_t n;
-};
-// outs overlap neither one another nor any of ins
-ckks_status check_overlap(std::vector<Range> outs, const std::vector<Range> &ins, const char *what)
-{
-    std::sort(outs.begin(), outs.end(), [](const Range &a, const Range &b) { return a.p < b.p; });
-    for (size_t i = 1; i < outs.size(); i++)
-        CK_REQUIRE(outs[i - 1].p + outs[i - 1].n <= outs[i].p, CKKS_EINVAL, "%s: two outputs overlap", what);
-    for (const Range &r : ins) {
-        auto it = std::upper_bound(outs.begin(), outs.end(), r.p + (r.n - 1),
-                                   [](const uint64_t *p, const Range &b) { return p < b.p; });
-        if (it == outs.begin()) continue;
-        --it;
-        CK_REQUIRE(it->p + it->n <= r.p, CKKS_EINVAL, "%s: an output overlaps an input", what);
-    }
-    return CKKS_OK;
-}
-
 // the terms' automorphisms and keys: left rotations by base, base + h, base - h
 ckks_status find_keys(const ckks_ctx *ctx, WsumKind *w, uint32_t n, int64_t base, int64_t h, const int32_t *key_steps,
                       const uint64_t *const *keys, uint32_t n_keys, const char *what)
@@ -186,33 +151,6 @@ size_t tables_bytes(const ckks_ctx *ctx, uint32_t nb)
 {
     return (size_t)nb * ctx->n / 2 * sizeof(double) + enc_work_bytes(ctx, nb) + (size_t)nb * ctx->n * sizeof(int64_t);
 }
-
-// no C++ exception crosses the C boundary: the argument lists are the only host memory a call takes
-template <typename Body>
-ckks_status guarded(const char *what, Body body)
-{
-    try {
-        return body();
-    } catch (const std::bad_alloc &) {
-        return set_error(CKKS_ENOMEM, "%s: out of host memory", what);
-    } catch (...) {
-        return set_error(CKKS_ENOMEM, "%s: argument lists too long", what);
-    }
-}
-
-// launches go to the context's stream, on its device whichever is current
-struct DeviceScope {
-    int before = -1;
-    explicit DeviceScope(const ckks_ctx *ctx)
-    {
-        int d;
-        if (ctx && hipGetDevice(&d) == hipSuccess && d != ctx->device && hipSetDevice(ctx->device) == hipSuccess) before = d;
-    }
-    ~DeviceScope()
-    {
-        if (before >= 0) (void)hipSetDevice(before);
-    }
-};
 
 }  // namespace
 

@@ -1,0 +1,566 @@
+"""Polynomials, norms and the projection's epilogue on the GPU.
+
+Outputs agree bit for bit with the same steps put together from the oracle's stages, in every kind of ring, either
+arithmetic and both layouts; decrypted results agree with plain evaluation within the bounds of their steps' noise; a run
+of them as a block uses them (norm, gated projections, a projection onto the residual stream) agrees with the plain
+block.  Refused calls leave their outputs as they were.
+"""
+import math
+
+import numpy as np
+import pytest
+
+import nonlinear_common as nc
+from gpu_common import say, to_dev, to_host
+from rope_common import random_cts, random_keys
+from test_gpu_rope import SLOT_BOUND, Party, bufs, dev_keys, ring, same
+from workloads import rng, uniform_residues
+
+pytestmark = pytest.mark.gpu
+
+
+def silu(x):
+    return x / (1 + math.exp(-x))
+
+
+def some_poly(degree, seed, lo=-3.0, hi=5.0):
+    from paper_2609_12378_amd import Poly
+    c = rng(seed, 2).normal(0, 1, degree + 1)
+    c[rng(seed, 2, 1).integers(0, degree + 1)] = 0.0
+    return Poly(tuple(c), lo, hi)
+
+
+def rlk_of(ck, seed):
+    return uniform_residues(rng(seed, 5, 1), ck.primes, ck.n, lead=(ck.dnum, 2))
+
+
+def plaintexts(ck, limbs, count, seed):
+    return [uniform_residues(rng(seed, 2, 2), ck.q[:limbs], ck.n)[None] for _ in range(count)]
+
+
+SCALE = 1.01 * 2.0 ** 49
+
+
+# ---- polynomials ------------------------------------------------------------------------------------------------
+
+POLY = [((8, 9, 3, 3, 50), 9, d, 1) for d in (1, 2, 3, 4, 5, 7, 8, 9, 13, 15, 16, 17, 23, 31, 32, 63, 64, 127)] + [
+    ((4, 5, 2, 2, 45), 5, 5, 2), ((8, 9, 3, 3, 50), 7, 15, 18), ((10, 8, 3, 3, 59), 8, 12, 2), ((11, 6, 6, 1, 50), 5, 7, 1),
+    ((11, 6, 1, 6, 50), 6, 6, 3), ((12, 6, 2, 3, 50), 4, 3, 1), ((12, 7, 2, 7, 36), 7, 15, 17), ((13, 8, 3, 3, 50), 7, 15, 3),
+    ((12, 6, 2, 3, 59), 6, 12, 2), ((13, 6, 2, 2, 0), 6, 9, 2), ((14, 6, 2, 3, 50), 6, 12, 2), ((14, 5, 2, 2, 59), 4, 3, 1),
+    ((15, 5, 2, 2, 50), 4, 3, 3), ((16, 6, 2, 3, 50), 5, 5, 1), ((16, 5, 9, 1, 50), 4, 2, 1), ((14, 5, 2, 2, 0), 4, 3, 2)]
+
+
+def poly_parity(case, arith=0):
+    ring_args, limbs, degree, count = case
+    ctx, ck = ring(*ring_args)
+    poly, rlk = some_poly(degree, degree), rlk_of(ck, 11)
+    xs = random_cts(ck, limbs, count, 100 + degree)
+    ctx.set_ntt_arith(arith)
+    try:
+        got = ctx.poly_eval(bufs(xs, SCALE), poly, to_dev(rlk))
+    finally:
+        ctx.set_ntt_arith(0)
+    assert len(got) == count
+    for r, (g, x) in enumerate(zip(got, xs)):
+        if r not in (0, count - 1):
+            continue
+        assert g.scale == SCALE
+        same(g.data, nc.poly_eval(ck, x, SCALE, poly, rlk), "%s: ciphertext %d" % (case, r))
+
+
+@pytest.mark.parametrize("case", POLY, ids=str)
+def test_poly_matches_the_oracle(case):
+    poly_parity(case)
+
+
+@pytest.mark.parametrize("case", [((8, 9, 3, 3, 50), 6, 9, 2), ((12, 6, 2, 3, 50), 5, 7, 1), ((14, 5, 2, 2, 50), 4, 3, 2)],
+                         ids=str)
+def test_poly_in_integer_arithmetic(case):
+    poly_parity(case, 1)
+
+
+def test_scales_far_from_the_primes():
+    """Factors beyond 64 bits under 59-bit primes: an interval 2^-20 wide takes 2^(139 - log2 scale), refused from 2^120."""
+    from paper_2609_12378_amd import CkksError
+    ctx, ck = ring(10, 8, 3, 3, 59)
+    poly, rlk = some_poly(3, 5, 1.0, 1.0 + 2.0 ** -20), rlk_of(ck, 11)
+    x = random_cts(ck, 4, 1, 105)
+    with pytest.raises(CkksError, match="2.120"):
+        ctx.poly_eval(bufs(x, 2.0 ** 12), poly, to_dev(rlk))
+    for scale in (2.0 ** 20, 2.0 ** 100):
+        got = ctx.poly_eval(bufs(x, scale), poly, to_dev(rlk))[0]
+        same(got.data, nc.poly_eval(ck, x[0], scale, poly, rlk), "scale %g" % scale)
+
+
+# ---- norms ------------------------------------------------------------------------------------------------------
+
+# ring, limbs, tokens, layout, count, degree, newton, weights, residual
+NORM = [((8, 14, 4, 4, 50), L, T, lay, count, deg, nw, w, res) for L, T, lay, count, deg, nw, w, res in (
+    (14, 4, "fm", 1, 3, 0, None, None), (14, 4, "tm", 3, 7, 1, "plain", "other"), (13, 1, "fm", 2, 5, 2, "cipher", "in"),
+    (12, 128, "fm", 2, 1, 1, "plain", None), (12, 128, "tm", 1, 2, 0, "cipher", "in"), (14, 1, "tm", 1, 3, 1, None, "other"),
+    (14, 2, "fm", 17, 8, 1, "plain", "in"), (14, 8, "tm", 1, 4, 2, "plain", None), (14, 16, "fm", 1, 1, 4, None, None),
+    (5, 4, "fm", 1, 1, 0, "cipher", None))] + [
+    ((10, 8, 3, 3, 59), 8, 8, "tm", 2, 3, 0, "plain", "in"), ((12, 7, 2, 4, 50), 7, 16, "fm", 1, 3, 0, None, "other"),
+    ((13, 10, 4, 3, 50), 9, 16, "tm", 3, 3, 1, "cipher", "in"), ((14, 8, 3, 3, 50), 7, 64, "fm", 2, 1, 0, "plain", "in"),
+    ((13, 9, 3, 3, 0), 8, 32, "fm", 1, 2, 1, "plain", None), ((14, 7, 2, 4, 59), 6, 128, "fm", 1, 1, 0, "cipher", None)]
+
+
+def norm_inputs(ck, limbs, tokens, layout, count, weights, residual, seed):
+    st = dict(xs=random_cts(ck, limbs, count, seed), rlk=rlk_of(ck, seed), ws=None, mask=None, res=None)
+    if weights == "plain":
+        st["ws"] = plaintexts(ck, limbs, count, seed)
+    elif weights == "cipher":
+        st["ws"] = random_cts(ck, limbs - 1, count, seed + 1)
+    if layout == "tm":
+        st["mask"] = plaintexts(ck, limbs - 1, 1, seed + 2)[0]
+    if residual:
+        st["res"] = st["xs"] if residual == "in" else random_cts(ck, limbs - 2, count, seed + 3)
+    D, unit, steps = ck.n // 2 // tokens, tokens if layout == "fm" else 1, set()
+    for radix in nc.radixes(D):
+        steps |= {sign * k * unit for k in range(1, radix) for sign in ((1, -1) if layout == "tm" else (1,))}
+        unit *= radix
+    st["keys"] = random_keys(ck, steps, seed)
+    return st
+
+
+@pytest.mark.parametrize("case", NORM, ids=str)
+def test_norm_matches_the_oracle(case):
+    from paper_2609_12378_amd import Buf, Context
+    ring_args, limbs, tokens, layout, count, degree, newton, weights, residual = case
+    ctx, ck = ring(*ring_args)
+    st = norm_inputs(ck, limbs, tokens, layout, count, weights, residual, 200 + degree)
+    D = ck.n // 2 // tokens
+    features = count * D - (1 if D > 2 else 0)
+    poly = some_poly(degree, degree, 0.5, 3.0)
+    assert sorted(st["keys"]) == Context.norm_steps(ck.n // 2, tokens, layout)
+    xs = bufs(st["xs"], SCALE)
+    r_scale = SCALE if residual == "in" else 0.5 * SCALE
+    got = ctx.rms_norm(xs, tokens, features, poly, to_dev(st["rlk"]), dev_keys(st["keys"]), layout=layout,
+                       weights=None if st["ws"] is None else bufs(st["ws"], 0.9 * 2.0 ** 49),
+                       mask=None if st["mask"] is None else Buf(to_dev(st["mask"]), 1.1 * 2.0 ** 49), newton=newton, eps=1e-3,
+                       residual=None if st["res"] is None else xs if residual == "in" else bufs(st["res"], r_scale),
+                       residual_scale=-0.5)
+    pick = sorted({0, count - 1})
+    want = nc.rms_norm(ck, st["xs"], SCALE, tokens, features, poly, st["rlk"], st["keys"], layout, st["ws"], 0.9 * 2.0 ** 49,
+                       st["mask"], 1.1 * 2.0 ** 49, newton, 1e-3, st["res"], r_scale, -0.5)
+    for r in pick:
+        assert got[r].scale == SCALE
+        same(got[r].data, want[r], "ciphertext %d" % r)
+
+
+# ---- the projection's epilogue ----------------------------------------------------------------------------------
+
+# ring, limbs, tokens, layout, d_in and d_out in ciphertexts, n1, bias, degree, gate, residual
+PROJ = [((8, 7, 3, 3, 50), 7, 8, lay, 2, 3, 5, b, deg, g, r) for lay in ("fm", "tm") for b, deg, g, r in (
+    (1, 0, 0, 0), (0, 0, 0, 1), (1, 0, 1, 1), (0, 5, 0, 1), (1, 9, 1, 0), (1, 7, 1, 1), (0, 1, 0, 0))] + [
+    ((8, 7, 3, 3, 50), 2, 8, "fm", 1, 1, 16, 1, 0, 0, 1), ((8, 7, 3, 3, 50), 7, 32, "tm", 1, 17, 4, 1, 3, 1, 1),
+    ((9, 6, 2, 3, 59), 5, 16, "fm", 1, 2, 16, 1, 3, 1, 1), ((12, 4, 2, 2, 36), 4, 64, "fm", 1, 2, 8, 1, 1, 1, 1),
+    ((12, 6, 2, 3, 50), 6, 64, "tm", 2, 2, 16, 1, 7, 1, 1), ((14, 4, 2, 2, 50), 4, 256, "fm", 1, 2, 8, 1, 2, 0, 1),
+    ((13, 5, 2, 2, 0), 4, 128, "fm", 1, 1, 8, 1, 1, 1, 0)]
+
+
+def proj_keys(ck, tokens, layout, n1):
+    D, unit = ck.n // 2 // tokens, tokens if layout == "fm" else 1
+    steps = [unit * b for b in range(1, n1)] + [unit * n1 * g for g in range(1, -(-D // n1))]
+    if layout == "tm":
+        steps += [b - D for b in range(n1)]
+    g = rng(301, 5)
+    return {s: uniform_residues(g, ck.primes, ck.n, lead=(ck.dnum, 2)) for s in sorted(set(steps))}
+
+
+@pytest.mark.parametrize("lazy", [False, True])
+@pytest.mark.parametrize("case", PROJ, ids=str)
+def test_epilogue_matches_the_oracle(case, lazy):
+    from paper_2609_12378_amd import Epilogue
+    ring_args, limbs, tokens, layout, n_in, n_out, n1, bias, degree, gate, residual = case
+    if lazy and ring_args[0] != 8:
+        pytest.skip("the sums' mode is the projection's own, tested there")
+    ctx, ck = ring(*ring_args)
+    D = ck.n // 2 // tokens
+    xs, rlk, keys = random_cts(ck, limbs, n_in, 300), rlk_of(ck, 301), proj_keys(ck, tokens, layout, n1)
+    W = rng(302, 2).normal(0, 0.02, (n_in * D, n_out * D))
+    act = some_poly(degree, degree) if degree else None
+    bs = plaintexts(ck, limbs, n_out, 303) if bias else None
+    gs = random_cts(ck, limbs - 1, n_out, 304) if gate else None
+    rs = random_cts(ck, limbs, n_out, 305) if residual else None
+    near = 2.0 ** ((ring_args[4] or 50) - 50)                # scales near the primes: the weights' is bounded
+    scales = dict(b=0.7 * 2.0 ** 49 * near, g=0.8 * 2.0 ** 49 * near, r=0.9 * 2.0 ** 49 * near)
+    scale = SCALE * near
+    ctx.set_lazy_moddown(lazy)
+    try:
+        got = ctx.linear_project(bufs(xs, scale), to_dev(W), tokens, n1, dev_keys(keys), layout=layout, epilogue=Epilogue(
+            bias=bufs(bs, scales["b"]) if bias else None, act=act, gate=bufs(gs, scales["g"]) if gate else None,
+            residual=bufs(rs, scales["r"]) if residual else None, residual_scale=0.5,
+            rlk=to_dev(rlk) if act or gate else None))
+    finally:
+        ctx.set_lazy_moddown(False)
+    want = nc.project(ck, xs, scale, W, tokens, n1, keys, layout, rlk, [b[0][None] for b in bs] if bias else None,
+                      scales["b"], act, gs, scales["g"], rs, scales["r"], 0.5, lazy)
+    assert len(got) == n_out
+    for j in range(n_out):
+        assert got[j].scale == scale
+        same(got[j].data, want[j], "output %d" % j)
+
+
+# ---- what the ciphertexts hold ----------------------------------------------------------------------------------
+
+def party():
+    return Party(log_n=13, n_q=14, n_p=5, dnum=3, seed=41)
+
+
+@pytest.mark.parametrize("degree", [2, 7, 15, 31])
+def test_poly_of_decrypted_slots(degree):
+    from paper_2609_12378_amd import Poly
+    P = party()
+    poly = Poly.fit(silu, degree, -8.0, 8.0)
+    x = rng(51, 1).uniform(-8, 8, P.ctx.n // 2)
+    x[:2] = -8.0, 8.0
+    y = P.ctx.poly_eval([P.encrypt(x, 8)], poly, P.relin())[0]
+    assert y.n_limbs == 8 - 1 - poly.depth and y.scale == P.scale
+    want = np.array([poly(v) for v in x])
+    err = np.max(np.abs(P.decrypt(y) - want))
+    # x is off by a fresh encryption's noise, below a step's; 2 / (hi - lo) < 1
+    bound = nc.poly_bound(poly.coefs, 2 * SLOT_BOUND, SLOT_BOUND)
+    say("degree %d: error %.3g, bound %.3g" % (degree, err, bound))
+    assert err < bound
+
+
+def norm_plain(x, poly, eps, newton):
+    mean = np.mean(x * x, axis=1, keepdims=True)
+    y = np.vectorize(poly)(mean)
+    for _ in range(newton):
+        y = y * (3 - (mean + eps) * y * y) / 2
+    return mean, y
+
+
+@pytest.mark.parametrize("layout,newton", [("fm", 0), ("fm", 2), ("tm", 1)])
+def test_norm_of_decrypted_slots(layout, newton):
+    from paper_2609_12378_amd import Buf, Context, Poly
+    P = party()
+    ctx, T, count, limbs = P.ctx, 32, 2, 14
+    D = ctx.n // 2 // T
+    g = rng(52, 1)
+    x = g.normal(0, 1, (T, count * D)) * g.uniform(0.5, 1.4, (T, 1))
+    w, res = g.normal(1, 0.2, count * D), g.normal(0, 1, (T, count * D))
+    eps = 1e-5
+    poly = Poly.fit(lambda v: (v + eps) ** -0.5, 15 if layout == "fm" else 7, 0.1, 3.0)
+    pack = lambda a: (a if layout == "tm" else a.T).reshape(-1)  # noqa: E731
+    cts = [P.encrypt(pack(x[:, i * D:(i + 1) * D]), limbs) for i in range(count)]
+    rts = [P.encrypt(pack(res[:, i * D:(i + 1) * D]), limbs) for i in range(count)]
+    ws = [ctx.encode(to_dev(pack(np.broadcast_to(w[i * D:(i + 1) * D], (T, D)).copy())), None, P.scale, limbs)
+          for i in range(count)]
+    keys = P.keys(Context.norm_steps(ctx.n // 2, T, layout))
+    mask = ctx.norm_mask(T, limbs - 1, P.scale) if layout == "tm" else None
+    out = ctx.rms_norm(cts, T, count * D, poly, P.relin(), keys, layout=layout, weights=ws, mask=mask, newton=newton, eps=eps,
+                       residual=rts, residual_scale=0.5)
+    mean, y = norm_plain(x, poly, eps, newton)
+    want = w * x * y + 0.5 * res
+    got = np.concatenate([P.decrypt(o).reshape((D, T) if layout == "fm" else (T, D)).T if layout == "fm" else
+                          P.decrypt(o).reshape(T, D) for o in out], 1)
+    err = np.max(np.abs(got - want))
+    # d a step.  The mean: each square is off by 2 |x| d + d, their mean by at most that, a round of 16 adds 15 rotations'
+    # noise to every of D / 16 .. 1 sums (over D features: 2 d), the mask's step is one more in 2 D sums of D.
+    d, X = SLOT_BOUND, np.max(np.abs(x))
+    e_mean = (2 * X + 1) * d + 32 * d + (3 * d * D if layout == "tm" else 0)
+    e1 = 2 / (poly.hi - poly.lo) * e_mean + d
+    e = nc.poly_bound(poly.coefs, e1, d)
+    M, Y = np.max(mean) + eps, np.max(y) + 0.1
+    for _ in range(newton):                                  # |dy'/dy| <= 3/2 (1 + M Y^2), |dy'/dmean| <= Y^3 / 2
+        e = 1.5 * (1 + M * Y * Y) * e + Y ** 3 / 2 * (e_mean + d) + (Y * Y + M * Y + 1) * d
+    B = np.max(np.abs(w * x))
+    bound = B * e + Y * (np.max(np.abs(w)) * d + X * d + d) + 2 * d
+    say("%s, %d Newton steps: error %.3g, bound %.3g" % (layout, newton, err, bound))
+    assert err < bound
+
+
+def test_a_block_of_them():
+    """norm -> SiLU(x W_g + b) * (x W_u) -> projection added to the stream, as a feed-forward block runs, on decrypted slots
+    against the plain block with the same polynomials."""
+    from paper_2609_12378_amd import Context, Epilogue, Poly
+    P = Party(log_n=13, n_q=18, n_p=6, dnum=3, seed=43)
+    ctx, T = P.ctx, 64
+    D, n1, limbs = ctx.n // 2 // T, 8, 18
+    g = rng(53, 1)
+    x = g.normal(0, 1, (T, D))
+    wn = g.normal(1, 0.1, D)
+    Wg, Wu, Wd = (g.normal(0, 0.02 * math.sqrt(8), s) for s in ((D, 2 * D), (D, 2 * D), (2 * D, D)))
+    b = g.normal(0, 0.1, 2 * D)
+    inv, act = Poly.fit(lambda v: (v + 1e-5) ** -0.5, 7, 0.3, 2.5), Poly.fit(silu, 15, -6.0, 6.0)
+    slots = lambda a: np.ascontiguousarray(a.T).reshape(-1)  # noqa: E731
+    every = lambda v: slots(np.broadcast_to(v, (T, len(v))))  # noqa: E731
+    keys = P.keys(sorted(set(Context.norm_steps(ctx.n // 2, T)) | {T * k for k in range(1, n1)} |
+                         {T * n1 * k for k in range(1, -(-D // n1))}))
+    rlk = P.relin()
+    ct = P.encrypt(slots(x), limbs)
+    w = ctx.encode(to_dev(every(wn)), None, P.scale, limbs)
+    h = ctx.rms_norm([ct], T, D, inv, rlk, keys, weights=[w], newton=1, eps=1e-5)       # 18 - 3 - 3 - 2 = 10 limbs
+    bias = [ctx.encode(to_dev(every(b[j * D:(j + 1) * D])), None, P.scale, 10) for j in range(2)]
+    u = ctx.linear_project(h, to_dev(Wu), T, n1, keys)                                    # 9 limbs
+    f = ctx.linear_project(h, to_dev(Wg), T, n1, keys, epilogue=Epilogue(bias=bias, act=act, gate=u, rlk=rlk))  # 4
+    y = ctx.linear_project(f, to_dev(Wd), T, n1, keys, epilogue=Epilogue(residual=[ct]))  # 3
+    assert (h[0].n_limbs, u[0].n_limbs, f[0].n_limbs, y[0].n_limbs) == (10, 9, 4, 3)
+    _, r = norm_plain(x, inv, 1e-5, 1)
+    ph = wn * x * r
+    pre = ph @ Wg + b
+    assert np.max(np.abs(pre)) < 6
+    pf = np.vectorize(act)(pre) * (ph @ Wu)
+    want = pf @ Wd + x
+    got = P.decrypt(y[0]).reshape(D, T).T
+    err = np.max(np.abs(got - want))
+    # The norm's outputs are off by at most e_h (the bound of the test above: below 2^-17 for degree 7 and one Newton
+    # step); a projection multiplies that by its column's sum of |w| and adds a step's noise for each of its D products
+    # summed in n1 + D / n1 rotated parts; the activation by poly_bound's factor, linear in e1.
+    d, eh = SLOT_BOUND, 2.0 ** -17
+    cols = max(np.max(np.sum(np.abs(m), 0)) for m in (Wg, Wu))
+    ep = cols * eh + 2 * D * d
+    ea = nc.poly_bound(act.coefs, 2 / 12 * ep + d, d)
+    ef = ea * np.max(np.abs(ph @ Wu)) + np.max(np.abs(np.vectorize(act)(pre))) * ep + ea * ep + d
+    bound = np.max(np.sum(np.abs(Wd), 0)) * ef + 2 * D * d + 2 * d
+    say("block: error %.3g, bound %.3g" % (err, bound))
+    assert err < bound < 0.1
+
+
+# ---- refusals ---------------------------------------------------------------------------------------------------
+
+def test_refused_calls_leave_their_outputs():
+    from paper_2609_12378_amd import Buf, CkksError, Context, Epilogue, Poly
+    import torch
+    ctx, ck = ring(12, 7, 2, 4, 50)
+    T, L, n = 64, 7, ck.n
+    D = n // 2 // T
+    rlk = to_dev(rlk_of(ck, 61))
+    xs, old = random_cts(ck, L, 2, 62), random_cts(ck, 3, 2, 63)
+    cts, outs = bufs(xs, SCALE), bufs(old, 1.0)
+    p7, p3 = some_poly(7, 1), some_poly(3, 1)
+
+    def refused(match, fn):
+        with pytest.raises(CkksError, match=match):
+            fn()
+
+    poly = lambda c=cts, p=p7, o=outs, k=rlk: ctx.poly_eval(c, p, k, outs=o)  # noqa: E731
+    refused("limbs, expected", lambda: poly(p=some_poly(3, 1)))
+    refused("needs 9 to 7 limbs", lambda: poly(p=some_poly(127, 1)))
+    refused("degree 128", lambda: poly(p=Poly((1.0,) * 129, 0.0, 1.0)))
+    refused("degree 0", lambda: poly(p=Poly((1.0,), 0.0, 1.0)))
+    refused("interval", lambda: poly(p=Poly((1.0, 2.0), 1.0, 1.0)))
+    refused("interval", lambda: poly(p=Poly((1.0, 2.0), math.nan, 1.0)))
+    refused("interval", lambda: poly(p=Poly((1.0, 2.0), -1e308, 1e308)))
+    refused("coefficient 1 is not finite", lambda: poly(p=Poly((1.0, math.inf), 0.0, 1.0)))
+    refused("2.120", lambda: poly(p=Poly((1.0, 1e30) + p7.coefs[2:], 0.0, 1.0)))
+    refused("scales differ", lambda: poly(c=[cts[0], Buf(cts[1].data, 2.0)]))
+    refused("scale must be positive", lambda: poly(c=[Buf(c.data, 0.0) for c in cts]))
+    refused("scale must be positive", lambda: poly(c=[Buf(c.data, math.inf) for c in cts]))
+    refused("limbs, expected", lambda: poly(c=[cts[0], Buf(cts[1].data[:, :5].contiguous(), SCALE)]))
+    refused("two outputs overlap", lambda: poly(o=[outs[0], outs[0]]))
+    refused("overlaps an input", lambda: poly(o=[outs[0], Buf(cts[1].data.view(-1)[:2 * 3 * n].view(2, 3, n), 1.0)]))
+    refused("ciphertext", lambda: poly(c=[Buf(torch.cat([c.data, c.data[:1]]), SCALE) for c in cts]))
+    refused("relinearisation key", lambda: poly(k=rlk[:1].contiguous()))
+    bare = Context(12, 7, 0, 1, q_bits=50)
+    refused("special primes", lambda: bare.poly_eval(cts, p7, torch.zeros(bare.key_shape(), dtype=torch.uint64, device="cuda"),
+                                                     outs=outs))
+
+    keys = dev_keys(random_keys(ck, Context.norm_steps(n // 2, T, "tm"), 64))
+    nouts = bufs(random_cts(ck, 1, 2, 65), 1.0)
+    mask = Buf(to_dev(plaintexts(ck, L - 1, 1, 66)[0]), SCALE)
+    ws = bufs(plaintexts(ck, L, 2, 67), SCALE)
+
+    def norm(c=cts, tokens=T, features=2 * D, p=p3, k=keys, layout="tm", mask=mask, o=nouts, **kw):
+        return ctx.rms_norm(c, tokens, features, p, rlk, k, layout=layout, mask=mask, outs=o, **kw)
+
+    refused("no key for step", lambda: norm(k={}))
+    refused("no key for step", lambda: norm(k={s: v for s, v in keys.items() if s != n // 2 - 1}))
+    refused("mask", lambda: norm(mask=None))
+    refused("mask", lambda: norm(layout="fm"))
+    refused("power of two", lambda: norm(tokens=63))
+    refused("power of two", lambda: norm(tokens=0))
+    refused("features", lambda: norm(features=0))
+    refused("features", lambda: norm(features=2 * D + 1))
+    refused("Newton", lambda: norm(newton=5))
+    refused("need 9 to 7", lambda: norm(newton=1))
+    refused("eps", lambda: norm(eps=-1.0))
+    refused("eps", lambda: norm(eps=math.nan))
+    refused("residual scale", lambda: norm(residual=cts, residual_scale=math.nan))
+    refused("weight 0 has 2 limbs", lambda: norm(weights=bufs(random_cts(ck, 2, 2, 68), 1.0)))
+    refused("is not a plaintext", lambda: norm(weights=[ws[0], cts[1]]))
+    refused("scales differ", lambda: norm(weights=[ws[0], Buf(ws[1].data, 1.0)]))
+    refused("mask 0 has 5", lambda: norm(mask=Buf(mask.data[:, :5].contiguous(), 1.0)))
+    refused("residual 0 has 1", lambda: norm(residual=bufs(random_cts(ck, 1, 2, 68), 1.0)))
+    refused("overlaps an input", lambda: norm(residual=[cts[0], Buf(cts[1].data.view(-1)[:4 * n].view(2, 2, n), SCALE)],
+                                              o=[nouts[0], Buf(cts[1].data.view(-1)[2 * n:4 * n].view(2, 1, n), 1.0)]))
+    refused("overlaps an input", lambda: norm(o=[nouts[0], Buf(mask.data.view(-1)[:2 * n].view(2, 1, n), 1.0)]))
+
+    room = to_dev(rng(69, 2).normal(0, 0.02, 4 * n))
+    W = room[:4 * D * D].view(2 * D, 2 * D)
+    pk = dev_keys(proj_keys(ck, T, "fm", 8))
+    gs, bs = bufs(random_cts(ck, L - 1, 2, 70), SCALE), bufs(plaintexts(ck, L, 2, 71), SCALE)
+    pouts = bufs(random_cts(ck, 2, 2, 72), 1.0)
+
+    def proj(o=pouts, W=W, keys=pk, layout="fm", **kw):
+        e = dict(act=p7, gate=gs, rlk=rlk)
+        e.update(kw)
+        return ctx.linear_project(cts, W, T, 8, keys, outs=o, layout=layout, epilogue=Epilogue(**e))
+
+    refused("limbs, expected", lambda: proj(gate=None))
+    refused("relinearisation key", lambda: proj(rlk=None))
+    refused("no key", lambda: proj(keys={}))
+    refused("no key", lambda: proj(layout="tm"))
+    refused("bias", lambda: proj(bias=bs[:1]))
+    refused("is not a plaintext", lambda: proj(bias=gs))
+    refused("is not a ciphertext", lambda: proj(gate=bs))
+    refused("gate 0 has 2", lambda: proj(gate=bufs(random_cts(ck, 2, 2, 73), 1.0)))
+    refused("bias 0 has 6", lambda: proj(bias=bufs(plaintexts(ck, L - 1, 2, 74), 1.0)))
+    refused("above 2.62", lambda: proj(act=Poly(p7.coefs, 0.0, 1e-4)))
+    refused("above 2.62", lambda: proj(act=None, o=bufs(random_cts(ck, 5, 2, 72)), gate=[Buf(g.data, 2.0 ** 36) for g in gs]))
+    refused("residual scale", lambda: proj(residual=cts, residual_scale=math.inf))
+    refused("overlaps an input", lambda: proj(o=[pouts[0], Buf(gs[1].data.view(-1)[:4 * n].view(2, 2, n), 1.0)]))
+    refused("overlaps an input", lambda: proj(o=[pouts[0], Buf(room.view(torch.uint64).view(2, 2, n), 1.0)]))
+    refused("limbs, 1 given", lambda: ctx.linear_project(bufs(random_cts(ck, 1, 2, 75)), W, T, 8, pk, outs=pouts,
+                                                         epilogue=Epilogue()))
+    for i in range(2):
+        same(outs[i].data, old[i], "a refused call's output")
+        same(nouts[i].data, random_cts(ck, 1, 2, 65)[i], "a refused norm's output")
+        same(pouts[i].data, random_cts(ck, 2, 2, 72)[i], "a refused projection's output")
+
+
+# ---- streams, graphs, workspaces --------------------------------------------------------------------------------
+
+RUNS = [((8, 9, 3, 3, 50), 9, 8), ((12, 7, 2, 4, 50), 7, 64), ((14, 7, 3, 3, 50), 7, 256), ((10, 7, 3, 3, 59), 7, 32)]
+
+
+def near(ring_args):
+    """A scale near the ring's primes."""
+    return SCALE * 2.0 ** (ring_args[4] - 50)
+
+
+def three_calls(ck, limbs, T, x, gate, seed=81):
+    """(the calls on a context, their workspaces): a polynomial, a norm, a projection with everything behind it."""
+    from paper_2609_12378_amd import Context, Epilogue
+    D, rlk = ck.n // 2 // T, to_dev(rlk_of(ck, seed))
+    keys = dev_keys({**random_keys(ck, Context.norm_steps(ck.n // 2, T), seed), **proj_keys(ck, T, "fm", 4)})
+    W = to_dev(rng(seed, 2).normal(0, 0.02, (2 * D, 2 * D)))
+    ws, bs = bufs(plaintexts(ck, limbs, 2, seed + 1), SCALE), bufs(plaintexts(ck, limbs, 2, seed + 2), SCALE)
+    p5, p3, p1 = some_poly(5, 1), some_poly(3, 2), some_poly(1, 3)
+
+    def calls(c):
+        return (c.poly_eval(x, p5, rlk) + c.rms_norm(x, T, 2 * D, p1, rlk, keys, weights=ws, newton=1, eps=0.1, residual=x)
+                + c.linear_project(x, W, T, 4, keys, epilogue=Epilogue(bias=bs, act=p3, gate=gate, residual=x, rlk=rlk)))
+
+    def sizes(c):
+        return [c.workspace_bytes(c.OP_POLY_EVAL, (limbs, 2, 5)), c.workspace_bytes(c.OP_RMS_NORM, (limbs, 2, T, 1, 1, 1)),
+                c.workspace_bytes(c.OP_PROJECT_EPILOGUE, (limbs, T, 2 * D, 2 * D, 4, 1, 3, 1))]
+
+    return calls, sizes
+
+
+@pytest.mark.parametrize("ring_args,limbs,T", RUNS, ids=str)
+def test_a_workspace_of_the_reported_size_and_one_too_small(ring_args, limbs, T):
+    from paper_2609_12378_amd import CkksError
+    import torch
+    ctx, ck = ring(*ring_args)
+    x, gate = (bufs(random_cts(ck, limbs, 2, seed), near(ring_args)) for seed in (82, 83))
+    ctx.set_proj_batch(4)
+    calls, sizes = three_calls(ck, limbs, T, x, gate)
+    want = [to_host(b.data) for b in calls(ctx)]
+    need = sizes(ctx)
+    assert all(s > 0 and s % 8 == 0 for s in need)
+    mem = torch.empty(-(-max(need) // 256) * 32 + 64, dtype=torch.uint64, device="cuda")
+    mem.fill_(7)
+    try:
+        ctx.set_workspace(mem[:max(need) // 8])
+        for _ in range(2):
+            assert all(np.array_equal(to_host(b.data), w) for b, w in zip(calls(ctx), want))
+        assert bool((mem[max(need) // 8:] == 7).all())
+        for size in need:
+            ctx.set_workspace(mem[:size // 8 - 32])
+            with pytest.raises(CkksError, match="too small"):
+                calls(ctx)
+    finally:
+        ctx.set_workspace(None)
+        ctx.set_proj_batch(0)
+    for op, shape in ((ctx.OP_POLY_EVAL, (2, 1, 1)), (ctx.OP_POLY_EVAL, (99, 1, 1)), (ctx.OP_POLY_EVAL, (limbs, 0, 1)),
+                      (ctx.OP_POLY_EVAL, (limbs, 1, 128)), (ctx.OP_RMS_NORM, (4, 1, T, 1, 1, 0)),
+                      (ctx.OP_RMS_NORM, (limbs, 1, T + 1, 1, 1, 0)), (ctx.OP_RMS_NORM, (limbs, 1, T, 2, 1, 0)),
+                      (ctx.OP_PROJECT_EPILOGUE, (limbs, T, 1, 1, 4, 1, 0, 0)),
+                      (ctx.OP_PROJECT_EPILOGUE, (limbs, T, ck.n // 2 // T, ck.n // 2 // T, 4, 2, 0, 0))):
+        with pytest.raises(CkksError):
+            ctx.workspace_bytes(op, shape)
+
+
+@pytest.mark.parametrize("ring_args,limbs,T", RUNS[1:], ids=str)
+def test_captured_calls_replay(ring_args, limbs, T):
+    import torch
+    from paper_2609_12378_amd import Buf, Context
+    eager, ck = ring(*ring_args)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ctx = Context(ck.log_n, ck.n_q, ck.n_p, ck.dnum, q=eager.q, p=eager.p, stream=stream)
+    x, gate = ([Buf(torch.zeros((2, limbs, ck.n), dtype=torch.uint64, device="cuda"), near(ring_args)) for _ in range(2)]
+               for _ in range(2))
+    calls, sizes = three_calls(ck, limbs, T, x, gate)
+    for c in (ctx, eager):
+        c.set_proj_batch(4)
+    torch.cuda.synchronize()
+    ws = torch.empty(max(sizes(ctx)) // 8, dtype=torch.uint64, device="cuda")
+    ctx.set_workspace(ws)
+    with torch.cuda.stream(stream):
+        calls(ctx)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out = calls(ctx)
+    torch.cuda.synchronize()
+    for r in range(4):
+        for b, a in zip(x + gate, random_cts(ck, limbs, 4, 90 + r)):
+            b.data.copy_(to_dev(a))
+        torch.cuda.synchronize()
+        want = [to_host(b.data) for b in calls(eager)]
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (g, w) in enumerate(zip(out, want)):
+            same(g.data, w, "replay %d: output %d" % (r, i))
+        junk = [torch.randn(1 << 20, device="cuda") for _ in range(4)]      # the program's own work between replays
+        del junk
+    eager.set_proj_batch(0)
+    del graph
+
+
+def test_a_context_on_its_own_stream():
+    """Inputs made on the default stream, the calls on the context's; tensors dropped right after a call stay whole until
+    it has run."""
+    import torch
+    from paper_2609_12378_amd import Context
+    (ring_args, limbs, T) = RUNS[2]
+    eager, ck = ring(*ring_args)
+    data = random_cts(ck, limbs, 4, 95)
+    calls, _ = three_calls(ck, limbs, T, bufs(data[:2], SCALE), bufs(data[2:], SCALE))
+    want = [to_host(b.data) for b in calls(eager)]
+    stream = torch.cuda.Stream()
+    ctx = Context(ck.log_n, ck.n_q, ck.n_p, ck.dnum, q=eager.q, p=eager.p, stream=stream)
+    for _ in range(3):
+        calls, _ = three_calls(ck, limbs, T, bufs(data[:2], SCALE), bufs(data[2:], SCALE))
+        torch.cuda.synchronize()
+        got = calls(ctx)
+        del calls
+        scrap = [torch.full((2, limbs, ck.n), 1, dtype=torch.int64, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            same(g.data, w, "a call on another stream")
+        del scrap
+
+
+def test_two_contexts_on_one_set_of_buffers():
+    """Calls of two contexts on two streams at once, from the same inputs, keys and weights."""
+    import torch
+    from paper_2609_12378_amd import Context
+    (ring_args, limbs, T) = RUNS[1]
+    eager, ck = ring(*ring_args)
+    data = random_cts(ck, limbs, 4, 96)
+    calls, _ = three_calls(ck, limbs, T, bufs(data[:2], SCALE), bufs(data[2:], SCALE))
+    want = [to_host(b.data) for b in calls(eager)]
+    ctxs = [Context(ck.log_n, ck.n_q, ck.n_p, ck.dnum, q=eager.q, p=eager.p, stream=torch.cuda.Stream()) for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [calls(c) for _ in range(3) for c in ctxs]
+    torch.cuda.synchronize()
+    for out in got:
+        for g, w in zip(out, want):
+            same(g.data, w, "two at once")
