@@ -15,6 +15,12 @@ struct PolySrc {
     __device__ const uint64_t *at(uint32_t r) const { return base ? base + r * stride : list[r]; }
 };
 
+// The same of products: polynomial r is mult[r] list[r] mul[r] (mul[r] null: list[r] itself).
+struct PolyProd {
+    const uint64_t *list[kPolyList], *mul[kPolyList];
+    int8_t mult[kPolyList];
+};
+
 // the NTT-domain position that sigma_g moves to position j: 2 brev(j') + 1 = (2 brev(j) + 1) g mod 2N
 __device__ __forceinline__ uint32_t auto_index(uint32_t j, uint32_t g, uint32_t log_n)
 {

@@ -46,8 +46,36 @@ struct Blocks {
     __device__ size_t at(uint32_t r, uint32_t l) const { return ((size_t)(r * nd + l / alpha) * ext + l) << log_n; }
 };
 
+// What k_up_row transforms: a polynomial's words, or a product's, formed where they are read, |x| <= q/2 + 1
+__device__ __forceinline__ void source_row(double (&x)[kE], const PolySrc &c1, uint32_t r, size_t at, uint32_t t, const A &)
+{
+    const uint64_t *in = c1.at(r) + at;
+#pragma unroll
+    for (int k = 0; k < kE; k++) x[k] = A::from_u64(in[t + 16 * k]);
+}
+__device__ __forceinline__ void source_row(double (&x)[kE], const PolyProd &c, uint32_t r, size_t at, uint32_t t,
+                                           const A &ar)
+{
+    const uint64_t *a = c.list[r] + at, *b = c.mul[r];
+    uint64_t v[kE];
+#pragma unroll
+    for (int k = 0; k < kE; k++) v[k] = a[t + 16 * k];
+    if (b) {
+        uint64_t w[kE];
+#pragma unroll
+        for (int k = 0; k < kE; k++) w[k] = b[at + t + 16 * k];
+        const double m = c.mult[r];
+#pragma unroll
+        for (int k = 0; k < kE; k++) x[k] = ar.red(m * ar.mul(A::from_u64(v[k]), A::from_u64(w[k])));
+    } else {
+#pragma unroll
+        for (int k = 0; k < kE; k++) x[k] = A::from_u64(v[k]);
+    }
+}
+
 // 1. rows of 256 points, 8 per block of 128 threads: inverse row pass of limb l of polynomial r to its row
-__global__ __launch_bounds__(128) void k_up_row(uint64_t *dst, PolySrc c1, Blocks bl, const ModQ *__restrict__ mods,
+template <typename Src>
+__global__ __launch_bounds__(128) void k_up_row(uint64_t *dst, Src c1, Blocks bl, const ModQ *__restrict__ mods,
                                                 const double *__restrict__ itwf)
 {
     __shared__ double lds[8 * 273];
@@ -56,11 +84,9 @@ __global__ __launch_bounds__(128) void k_up_row(uint64_t *dst, PolySrc c1, Block
     const uint32_t sub = threadIdx.x >> 4, t = threadIdx.x & 15u, h = (blockIdx.x % per) * 8 + sub;
     const A ar(mods[l]);
     const double *tw = itwf + ((size_t)l << bl.log_n);
-    const uint64_t *in = c1.at(r) + ((size_t)l << bl.log_n) + (size_t)h * 256;
     uint64_t *out = dst + bl.at(r, l) + (size_t)h * 256;
     double x[kE];
-#pragma unroll
-    for (int k = 0; k < kE; k++) x[k] = A::from_u64(in[t + 16 * k]);
+    source_row(x, c1, r, ((size_t)l << bl.log_n) + (size_t)h * 256, t, ar);
     nttc::transpose<8, true>(x, lds, sub, t);
     nttc::inv_low<8, true>(x, tw, n1 + h, t, ar);
     nttc::transpose<8, false>(x, lds, sub, t);
@@ -486,7 +512,11 @@ bool f64_level_ok(const ckks_ctx *ctx, uint32_t level)
     return true;
 }
 
-ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t level, uint64_t *digits, bool own_rows)
+namespace {
+
+template <typename Src>
+ckks_status modup_of(ckks_ctx *ctx, const Src &src, const PolySrc &c1, uint32_t count, uint32_t level, uint64_t *digits,
+                     bool own_rows)
 {
     Blocks bl{};
     bl.nd = n_digits(ctx, level);
@@ -509,7 +539,7 @@ ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t 
     const uint32_t per = 1u << (ctx->log_n - 11);  // blocks of eight 256-point rows
     const double res = (double)count * bl.L * ctx->n;
     prof_begin(ctx, K_NTT_INV_ROW, 16.0 * res, res * kOpsButterflyF64 * 4);
-    hipLaunchKernelGGL(k_up_row, dim3(count * bl.L * per), dim3(128), 0, ctx->stream, digits, c1, bl, ctx->d_mod,
+    hipLaunchKernelGGL(k_up_row<Src>, dim3(count * bl.L * per), dim3(128), 0, ctx->stream, digits, src, bl, ctx->d_mod,
                        ctx->d_itwf);
     prof_end(ctx, K_NTT_INV_ROW);
     HIP_TRY(hipGetLastError());
@@ -538,6 +568,17 @@ ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t 
     prof_end(ctx, K_NTT_FWD_ROW);
     HIP_TRY(hipGetLastError());
     return CKKS_OK;
+}
+
+}  // namespace
+
+ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t level, uint64_t *digits, bool own_rows)
+{
+    return modup_of(ctx, c1, c1, count, level, digits, own_rows);
+}
+ckks_status up_modup(ckks_ctx *ctx, const PolyProd &c, uint32_t count, uint32_t level, uint64_t *digits)
+{
+    return modup_of(ctx, c, PolySrc{}, count, level, digits, false);
 }
 
 ckks_status up_moddown(ckks_ctx *ctx, uint64_t *up, uint32_t polys, uint32_t level, uint64_t *cw)

@@ -28,8 +28,8 @@ struct Step {
     const uint64_t *a = nullptr, *b = nullptr;
     uint32_t a_limbs = 0, b_limbs = 0, b_polys = 2;
     int32_t mult = 1;         // 1, 2 or -1
-    // or a sum of products [3][L][N], which the call overwrites
-    uint64_t *d = nullptr;
+    // or a sum of products [3][L][N]
+    const uint64_t *d = nullptr;
     uint32_t n_terms = 0;
     StepTerm t[kStepTerms];
     StepInt c;

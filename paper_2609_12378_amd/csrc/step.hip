@@ -6,37 +6,18 @@
 
 #include "ks_args.h"
 #include "ops.h"
+#include "step_args.h"
 
 namespace {
 
 constexpr int kThreads = 256;
 
-// A step's operands in a launch's arguments.
-struct Operands {
-    const uint64_t *a, *b, *z[kStepTerms];
-    uint64_t *d;
-    int64_t k[kStepTerms + 1];                   // the terms' integers, then the constant's
-    uint8_t sh[kStepTerms + 1], limbs[kStepTerms], polys[kStepTerms];
-    uint8_t n, a_limbs, b_limbs, b_polys;
-    int8_t mult;
-};
-struct Batch {
-    Operands s[kStepBatch];
-};
-static_assert(sizeof(Batch) <= 4096 - 256, "a batch travels in the kernel arguments");
+using namespace steps;
 
-// m 2^sh mod q
-__device__ __forceinline__ uint64_t int_mod(int64_t m, uint32_t sh, uint64_t q)
-{
-    const uint64_t a = m < 0 ? 0 - (uint64_t)m : (uint64_t)m;
-    uint64_t r = a % q;
-    for (uint32_t i = 0; i < sh; i++) r = csub(2 * r, q);
-    return m < 0 && r ? q - r : r;
-}
-
-// d (dk: [3][L][N] or, for steps that switch no key, [2][L][N]) of every step, one position a thread.  The constant goes
+// d of every step ([dp][L][N] each, dp 3 where the steps switch a key, else 2), one position a thread.  The constant goes
 // in as c q_l: it vanishes modulo q_l and the rescale leaves c.  At most 11 products below 2^124 a sum.
-__global__ __launch_bounds__(kThreads) void k_step_lin(Batch bt, uint32_t L, uint32_t log_n, const ModQ *__restrict__ mods)
+__global__ __launch_bounds__(kThreads) void k_step_lin(Batch bt, uint64_t *d, uint32_t dp, uint32_t L, uint32_t log_n,
+                                                       const ModQ *__restrict__ mods)
 {
     __shared__ uint64_t ks[kStepTerms + 1];
     const Operands &s = bt.s[blockIdx.z];
@@ -51,28 +32,30 @@ __global__ __launch_bounds__(kThreads) void k_step_lin(Batch bt, uint32_t L, uin
     if (pos >> log_n) return;
     const size_t at = ((size_t)row << log_n) + pos, half = (size_t)L << log_n;
     acc128 x0{ks[s.n], 0}, x1{0, 0};
-    if (s.a) {
+    d += (size_t)blockIdx.z * dp * half;
+    if (s.kind == kProduct || s.kind == kPlain) {
         const uint64_t *a = s.a + at, *b = s.b + at;
         const uint64_t a0 = a[0], a1 = a[(size_t)s.a_limbs << log_n];
         auto scaled = [&](uint64_t v) { return s.mult == 2 ? csub(2 * v, m.q) : s.mult < 0 && v ? m.q - v : v; };
         const uint64_t b0 = scaled(b[0]);
         mac(x0, a0, b0);
         mac(x1, a1, b0);
-        if (s.b_polys == 2) {
+        if (s.kind == kProduct) {
             const uint64_t b1 = scaled(b[(size_t)s.b_limbs << log_n]);
             mac(x1, a0, b1);
-            s.d[2 * half + at] = mulmod(a1, b1, m);
+            d[2 * half + at] = mulmod(a1, b1, m);
         }
-    } else if (s.b_polys == 0) {   // a sum of products is there
-        mac(x0, s.d[at], 1);
-        mac(x1, s.d[half + at], 1);
+    } else if (s.kind == kGiven) {
+        mac(x0, s.a[at], 1);
+        mac(x1, s.a[half + at], 1);
+        d[2 * half + at] = s.a[2 * half + at];
     }
     for (uint32_t i = 0; i < s.n; i++) {
         mac(x0, s.z[i][at], ks[i]);
         if (s.polys[i] == 2) mac(x1, s.z[i][at + ((size_t)s.limbs[i] << log_n)], ks[i]);
     }
-    s.d[at] = reduce128(x0, m);
-    s.d[half + at] = reduce128(x1, m);
+    d[at] = reduce128(x0, m);
+    d[half + at] = reduce128(x1, m);
 }
 
 struct Squares {
@@ -102,15 +85,15 @@ __global__ __launch_bounds__(kThreads) void k_step_squares(Squares sq, uint64_t 
 
 dim3 grid_of(const ckks_ctx *ctx, uint32_t rows, uint32_t z) { return dim3((ctx->n + kThreads - 1) / kThreads, rows, z); }
 
-Operands operands(const Step &s, uint64_t *d)
+Operands operands(const Step &s)
 {
     Operands o{};
-    o.a = s.a;
+    o.kind = s.d ? kGiven : !s.a ? kNone : s.b_polys == 2 ? kProduct : kPlain;
+    o.a = s.d ? s.d : s.a;
     o.b = s.b;
-    o.d = s.d ? s.d : d;
+    o.out = s.out;
     o.a_limbs = (uint8_t)s.a_limbs;
     o.b_limbs = (uint8_t)s.b_limbs;
-    o.b_polys = s.d ? 0 : (uint8_t)s.b_polys;
     o.mult = (int8_t)s.mult;
     o.n = (uint8_t)s.n_terms;
     for (uint32_t i = 0; i < s.n_terms; i++) {
@@ -145,7 +128,8 @@ Rows rows_of(const ckks_ctx *ctx, uint32_t L, size_t n, bool switched)
     return r;
 }
 
-ckks_status run_batch(ckks_ctx *ctx, uint32_t L, const Step *const *steps, uint32_t n, bool switched, const uint64_t *rlk,
+// n steps that all switch a key, or none of them does, in any ring and arithmetic: d, ModUp, ModDown, rescale
+ckks_status run_batch(ckks_ctx *ctx, uint32_t L, const Batch &b, uint32_t n, bool switched, const uint64_t *rlk,
                       uint64_t *mem)
 {
     const size_t N = ctx->n;
@@ -153,30 +137,24 @@ ckks_status run_batch(ckks_ctx *ctx, uint32_t L, const Step *const *steps, uint3
     const Rows r = rows_of(ctx, L, n, switched);
     uint64_t *d = mem, *dig = d + r.d * N, *work = dig + (r.dig + r.stage) * N, *sum = work + r.work * N,
              *top = sum + r.sum * N;
-    Batch b{};
     double words = 0;
-    for (uint32_t i = 0; i < n; i++) {
-        b.s[i] = operands(*steps[i], d + (size_t)i * dp * L * N);
-        words += 2 + 2.0 * steps[i]->n_terms + (steps[i]->d ? 2 : steps[i]->switched() ? 5 : steps[i]->a ? 3 : 0);
-    }
+    for (uint32_t i = 0; i < n; i++) words += dp + 2.0 * b.s[i].n + (b.s[i].kind == kProduct ? 4 : b.s[i].kind ? 3 : 0);
     prof_begin(ctx, K_ELEM, 8.0 * words * L * N);
-    hipLaunchKernelGGL(k_step_lin, grid_of(ctx, L, n), dim3(kThreads), 0, ctx->stream, b, L, ctx->log_n, ctx->d_mod);
+    hipLaunchKernelGGL(k_step_lin, grid_of(ctx, L, n), dim3(kThreads), 0, ctx->stream, b, d, dp, L, ctx->log_n, ctx->d_mod);
     prof_end(ctx, K_ELEM);
     HIP_TRY(hipGetLastError());
     std::vector<uint64_t *> outs(n);
-    for (uint32_t i = 0; i < n; i++) outs[i] = steps[i]->out;
+    for (uint32_t i = 0; i < n; i++) outs[i] = b.s[i].out;
     if (!switched) return rescale_each(ctx, d, n, L - 1, outs.data(), top);
     // a relinearisation is a rotation by the identity: (d0 + u0, d1 + u1), u the key switch of d2
     std::vector<const uint64_t *> c0(n), add1(n), digs(n), keys(n, rlk);
     std::vector<uint32_t> g(n, 1);
     std::vector<uint64_t *> sums(n);
     for (uint32_t i = 0; i < n; i++) {
-        c0[i] = b.s[i].d;
+        c0[i] = d + (size_t)i * 3 * L * N;
         add1[i] = c0[i] + L * N;
         digs[i] = dig + (size_t)i * nd * ext * N;
         sums[i] = sum + (size_t)i * 2 * L * N;
-        if (steps[i]->d)   // the ModUps read one array
-            CK_TRY(launch_copy_rows(ctx, d + ((size_t)i * 3 + 2) * L * N, 0, nullptr, 0, c0[i] + 2 * (size_t)L * N, 0, L * N, 1));
     }
     CK_TRY(ks_modup_batch(ctx, d + 2 * (size_t)L * N, 3 * (size_t)L * N, n, L - 1, dig, r.stage));
     CK_TRY(ks_rotate_batch(ctx, L - 1, n, c0.data(), digs.data(), g.data(), keys.data(), sums.data(), work, nullptr,
@@ -201,18 +179,30 @@ bool step_int(double x, StepInt *out)
 
 size_t step_scratch_words(const ckks_ctx *ctx, uint32_t L, uint32_t steps, bool switched)
 {
-    return rows_of(ctx, L, std::min(steps, kStepBatch), switched).total * ctx->n;
+    const uint32_t n = std::min(steps, kStepBatch);
+    // one figure for both arithmetics: a workspace of it serves after ckks_ctx_set_ntt_arith as well
+    return std::max(rows_of(ctx, L, n, switched).total, step_f64_rows(ctx, L, n, switched)) * ctx->n;
 }
 
 ckks_status step_run(ckks_ctx *ctx, uint32_t L, const std::vector<Step> &steps, const uint64_t *rlk, uint64_t *mem)
 {
-    for (int sw = 0; sw < 2; sw++) {
-        std::vector<const Step *> list;
+    // those that switch a key first; the fp64 kernels take both kinds in one batch
+    std::vector<const Step *> list;
+    size_t n_sw = 0;
+    for (int sw = 1; sw >= 0; sw--) {
         for (const Step &s : steps)
             if (s.switched() == (sw != 0)) list.push_back(&s);
-        for (size_t at = 0; at < list.size(); at += kStepBatch)
-            CK_TRY(run_batch(ctx, L, list.data() + at, (uint32_t)std::min<size_t>(kStepBatch, list.size() - at), sw != 0, rlk,
-                             mem));
+        if (sw) n_sw = list.size();
+    }
+    const bool fast = step_f64_ok(ctx, L);
+    for (size_t at = 0; at < list.size();) {
+        const size_t sw = at < n_sw ? n_sw - at : 0;
+        const uint32_t n = (uint32_t)std::min<size_t>({kStepBatch, list.size() - at, !fast && sw ? sw : kStepBatch});
+        Batch b{};
+        for (uint32_t i = 0; i < n; i++) b.s[i] = operands(*list[at + i]);
+        if (fast) CK_TRY(step_f64(ctx, L, b, n, (uint32_t)std::min<size_t>(sw, n), rlk, mem));
+        else CK_TRY(run_batch(ctx, L, b, n, sw != 0, rlk, mem));
+        at += n;
     }
     return CKKS_OK;
 }

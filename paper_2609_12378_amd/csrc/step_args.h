@@ -1,0 +1,51 @@
+// Arguments that the kernels of steps share (step.hip, step_f64.hip).
+#pragma once
+#include "step.h"
+#include "wsum_args.h"
+
+namespace steps {
+
+// What a step's product is: none, of ciphertexts, of a ciphertext and a plaintext, a sum of products that is there
+enum : uint8_t { kNone = 0, kProduct = 1, kPlain = 2, kGiven = 3 };
+
+// A step's operands as they travel in a launch's arguments.
+struct Operands {
+    const uint64_t *a, *b, *z[kStepTerms];       // a: the sum [3][L][N] of a kGiven step
+    uint64_t *out;
+    int64_t k[kStepTerms + 1];                   // the terms' integers, then the constant's
+    uint8_t sh[kStepTerms + 1], limbs[kStepTerms], polys[kStepTerms];
+    uint8_t n, a_limbs, b_limbs, kind;
+    int8_t mult;
+    __host__ __device__ bool switched() const { return kind == kProduct || kind == kGiven; }
+};
+struct Batch {
+    Operands s[kStepBatch];
+};
+static_assert(sizeof(Batch) <= 4096 - 256, "a batch travels in the kernel arguments");
+
+// m 2^sh mod q
+__device__ __forceinline__ uint64_t int_mod(int64_t m, uint32_t sh, uint64_t q)
+{
+    const uint64_t a = m < 0 ? 0 - (uint64_t)m : (uint64_t)m;
+    uint64_t r = a % q;
+    for (uint32_t i = 0; i < sh; i++) r = csub(2 * r, q);
+    return m < 0 && r ? q - r : r;
+}
+// The same in doubles, |m| <= 2^62 and q < 2^50: the two halves of m are exact, and x - c q below q where c is at most a
+// unit off.
+__device__ __forceinline__ double int_mod(int64_t m, uint32_t sh, const wsum::A &ar)
+{
+    const double hi = ar.red((double)(m >> 31) * 0x1p31);
+    double r = ar.red(hi + (double)(m & 0x7fffffff));
+    for (uint32_t i = 0; i < sh; i++) r = ar.red(2.0 * r);
+    return r < 0.0 ? r + ar.q : r;
+}
+
+}  // namespace steps
+
+// fp64 arithmetic at L limbs, N >= 2^14: n steps, of which the first n_sw switch a key
+bool step_f64_ok(const ckks_ctx *ctx, uint32_t L);
+ckks_status step_f64(ckks_ctx *ctx, uint32_t L, const steps::Batch &b, uint32_t n, uint32_t n_sw, const uint64_t *rlk,
+                     uint64_t *mem);
+// words of its scratch
+size_t step_f64_rows(const ckks_ctx *ctx, uint32_t L, size_t n, bool switched);

@@ -24,6 +24,7 @@
 #include "conv_col.h"
 #include "ops.h"
 #include "wsum_args.h"
+#include "wsum_pos.h"
 
 namespace {
 
@@ -34,43 +35,6 @@ using nttc::kE8;
 
 // ------------------------------------------------------------------------- two passes, fp64 ----------------------------
 
-// The positions of thread t (of 32) in a row of 256: pairs (j, j + 1) at j = 64 c + 4 (t & 15) + 2 (t >> 4), register
-// e = 2 c + (0 or 1), so a wave's access is whole cache lines.  It is the layout that the transforms end in and inverse
-// ones start from (nttc::u8<2>, four adjacent positions a thread) with position bits 1 and 6 exchanged, which is one
-// swap of lane rows a register (swap_1_6).
-// sigma_g reads position j at j' with 2 brev(j') + 1 = (2 brev(j) + 1) g mod 2N.  Bit 0 of j is the top bit of
-// 2 brev(j) + 1 modulo 2N, which an odd g leaves in place up to a carry from below: the partner j + 1 of an even j is
-// read at j' ^ 1; likewise the sources of 64 aligned positions are 64 aligned positions.  So gathers are pairs and
-// whole lines as well.  (8-byte accesses, or 16-byte ones at a stride of 32, cost twice the requests to L2, which bound
-// the kernels.)
-struct Positions {
-    uint32_t at, log_n;
-    __device__ Positions(uint32_t h, uint32_t t, uint32_t log_n_)
-        : at(h * 256 + 4 * (t & 15u) + 2 * (t >> 4)), log_n(log_n_)
-    {
-    }
-    __device__ uint32_t pos(int e) const { return at + 64u * (uint32_t)(e >> 1) + (uint32_t)(e & 1); }
-    __device__ uint32_t start(uint32_t g) const { return (2u * (__brev(at) >> (32 - log_n)) + 1u) * g; }
-    // j' of pos(e), e even; kg = start(g).  Bits 6 and 7 of the position add 2^(log_n - 6) g and 2^(log_n - 7) g.
-    __device__ uint32_t source(uint32_t kg, uint32_t g, int e) const
-    {
-        const uint32_t dk = ((uint32_t)(e & 2) << (log_n - 7)) + ((uint32_t)(e >> 2) << (log_n - 7));
-        return (__brev(kg + dk * g) >> (31 - log_n)) & ((1u << log_n) - 1);
-    }
-};
-// u8<2> to Positions' order and back: registers e and e | 2 (e & 2 clear) exchange lane rows 1 (of e) and 0 (of e | 2)
-__device__ __forceinline__ void swap_1_6(double (&x)[kE8])
-{
-#pragma unroll
-    for (int e = 0; e < kE8; e++) {
-        if (e & 2) continue;
-        const uint64_t a = A::to_raw(x[e]), b = A::to_raw(x[e | 2]);
-        const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)a, (uint32_t)b, false, false);
-        const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(a >> 32), (uint32_t)(b >> 32), false, false);
-        x[e] = A::from_raw((uint64_t)hi[0] << 32 | lo[0]);
-        x[e | 2] = A::from_raw((uint64_t)hi[1] << 32 | lo[1]);
-    }
-}
 // the words of sigma_g(p) at an even position and the next, j' = source of the even one
 __device__ __forceinline__ Pair ld2_auto(const uint64_t *p, uint32_t src)
 {
@@ -636,11 +600,6 @@ Scratch scratch_of(const ckks_ctx *ctx, uint32_t L, uint32_t cts, uint32_t pages
     return s;
 }
 
-Dims dims_of(const ckks_ctx *ctx, uint32_t L)
-{
-    return Dims{L, ctx->n_p, L + ctx->n_p, n_digits(ctx, L - 1), ctx->alpha, ctx->n_q, ctx->n_primes(), ctx->log_n};
-}
-
 // The digits of the first n_rot ciphertexts, without their own rows (blk_modup writes those too).  With fp64 primes the
 // ModUps read c1 where it is; else it is gathered to `stage` and taken to coefficient form there.
 ckks_status modup_cts(ckks_ctx *ctx, uint32_t L, const Args &a, uint32_t n_rot, uint64_t *dig, uint64_t *stage)
@@ -672,7 +631,7 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
                           uint64_t *cw)
 {
     const size_t N = ctx->n;
-    const uint32_t level = d.L - 1, bpl = 1u << (d.log_n - 9), polys = 2 * n * pages;
+    const uint32_t level = d.L - 1, bpl = 1u << (d.log_n - 9);
     const ConvDev *cd;
     CK_TRY(ctx_conv(ctx, (int)level, -1, &cd));
     const Quot qt{cd->d_qhat_inv_f, cd->d_qhat_mod_f, ctx->d_pinv, ctx->d_qlinv + (size_t)level * ctx->n_q, ctx->d_pmodq};
@@ -695,6 +654,40 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
     prof_end(ctx, K_KEYIP);
     HIP_TRY(hipGetLastError());
 
+    CK_TRY(wsum_convert(ctx, a, n, pages, d, up, cw));
+
+    const double rows4 = (double)n * level * N;
+    prof_begin(ctx, K_MODDOWN, 8.0 * rows4 * (d.nd + 2.0 + 4.0 * pages),
+               rows4 * (prods * 7.0 + 2 * pages * (4 * kOpsButterflyF64 + 14.0)));
+#define CK_GO(ND)                                                                                                  \
+    do {                                                                                                           \
+        const dim3 grid(level * bpl * n);                                                                          \
+        if (pages == 1)                                                                                            \
+            hipLaunchKernelGGL((k_wsum_fin8<ND, 1>), grid, dim3(64), 0, ctx->stream, a, cw, d, n, qt,              \
+                               ctx->d_mod, ctx->d_twf);                                                            \
+        else                                                                                                       \
+            hipLaunchKernelGGL((k_wsum_fin8<ND, 2>), grid, dim3(64), 0, ctx->stream, a, cw, d, n, qt,              \
+                               ctx->d_mod, ctx->d_twf);                                                            \
+    } while (0)
+    CK_ND(d.nd, CK_GO);
+#undef CK_GO
+    prof_end(ctx, K_MODDOWN);
+    HIP_TRY(hipGetLastError());
+    return CKKS_OK;
+}
+
+}  // namespace
+
+// steps 2 and 3: the rows q_l and P of u ([2 n pages][K + 1][N], after the row pass of their inverse transforms) to the
+// converted rows cw ([2 n pages][l][N], after the column pass of their forward ones)
+ckks_status wsum_convert(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pages, const Dims &d, uint64_t *up,
+                         uint64_t *cw)
+{
+    const size_t N = ctx->n;
+    const uint32_t level = d.L - 1, polys = 2 * n * pages;
+    const ConvDev *cd;
+    CK_TRY(ctx_conv(ctx, (int)level, -1, &cd));
+    const Quot qt{cd->d_qhat_inv_f, cd->d_qhat_mod_f, ctx->d_pinv, ctx->d_qlinv + (size_t)level * ctx->n_q, ctx->d_pmodq};
     const bool fused = d.log_n == 16 && d.K <= 8;
     // above half a block a CU no block's targets are split and its columns are transformed where they are converted (us
     // a call with the pass apart and along, by blocks: 13 limbs 150.4 and 160.4 (64), 251.9 and 253.7 (128), 363 and 356
@@ -761,28 +754,8 @@ ckks_status two_pass_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
     prof_end(ctx, K_CONV);
     HIP_TRY(hipGetLastError());
     if (!fused && !col16) CK_TRY(launch_ntt_fwd_first_pass(ctx, cw, polys, level, limb_range(0, level)));
-
-    const double rows4 = (double)n * level * N;
-    prof_begin(ctx, K_MODDOWN, 8.0 * rows4 * (d.nd + 2.0 + 4.0 * pages),
-               rows4 * (prods * 7.0 + 2 * pages * (4 * kOpsButterflyF64 + 14.0)));
-#define CK_GO(ND)                                                                                                  \
-    do {                                                                                                           \
-        const dim3 grid(level * bpl * n);                                                                          \
-        if (pages == 1)                                                                                            \
-            hipLaunchKernelGGL((k_wsum_fin8<ND, 1>), grid, dim3(64), 0, ctx->stream, a, cw, d, n, qt,              \
-                               ctx->d_mod, ctx->d_twf);                                                            \
-        else                                                                                                       \
-            hipLaunchKernelGGL((k_wsum_fin8<ND, 2>), grid, dim3(64), 0, ctx->stream, a, cw, d, n, qt,              \
-                               ctx->d_mod, ctx->d_twf);                                                            \
-    } while (0)
-    CK_ND(d.nd, CK_GO);
-#undef CK_GO
-    prof_end(ctx, K_MODDOWN);
-    HIP_TRY(hipGetLastError());
     return CKKS_OK;
 }
-
-}  // namespace
 
 size_t wsum_scratch_words(const ckks_ctx *ctx, uint32_t L, uint32_t cts, uint32_t pages)
 {
@@ -792,7 +765,7 @@ size_t wsum_scratch_words(const ckks_ctx *ctx, uint32_t L, uint32_t cts, uint32_
 ckks_status wsum_run(ckks_ctx *ctx, uint32_t L, uint32_t pages, const WsumKind *kinds, const std::vector<WsumCt> &cts,
                      uint64_t *mem)
 {
-    const Dims d = dims_of(ctx, L);
+    const Dims d = wsum_dims(ctx, L);
     const bool fast = fp64_sums(ctx, L - 1), rows = fast && blk_switch(ctx, L - 1);
     for (size_t r0 = 0; r0 < cts.size();) {
         // a batch: rotated and unrotated ciphertexts together where the kernels take both

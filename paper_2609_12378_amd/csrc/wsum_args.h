@@ -101,6 +101,16 @@ __device__ __forceinline__ double top_factor(const Quot &qt, const Dims &d, int 
 
 }  // namespace wsum
 
+inline wsum::Dims wsum_dims(const ckks_ctx *ctx, uint32_t L)
+{
+    return wsum::Dims{L, ctx->n_p, L + ctx->n_p, n_digits(ctx, L - 1), ctx->alpha, ctx->n_q, ctx->n_primes(), ctx->log_n};
+}
+
+// The division by P q_l (q_l alone: unrotated kinds) of sums that are there, between their inverse row pass and their
+// forward one (wsum.hip, two passes).  Of a it reads whose kinds are rotated.
+ckks_status wsum_convert(ckks_ctx *ctx, const wsum::Args &a, uint32_t n, uint32_t pages, const wsum::Dims &d, uint64_t *up,
+                         uint64_t *cw);
+
 // N = 2^12 and 2^13 (wsum_block.hip): the sums and the division of n ciphertexts whose digits are formed;
 // u: 2 n pages (level+1+n_p) N words
 ckks_status wsum_blk_sums(ckks_ctx *ctx, const wsum::Args &a, uint32_t n, uint32_t pages, const wsum::Dims &d, uint64_t *u);

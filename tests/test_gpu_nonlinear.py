@@ -154,7 +154,7 @@ def test_norm_matches_the_oracle(case):
 PROJ = [((8, 7, 3, 3, 50), 7, 8, lay, 2, 3, 5, b, deg, g, r) for lay in ("fm", "tm") for b, deg, g, r in (
     (1, 0, 0, 0), (0, 0, 0, 1), (1, 0, 1, 1), (0, 5, 0, 1), (1, 9, 1, 0), (1, 7, 1, 1), (0, 1, 0, 0))] + [
     ((8, 7, 3, 3, 50), 2, 8, "fm", 1, 1, 16, 1, 0, 0, 1), ((8, 7, 3, 3, 50), 7, 32, "tm", 1, 17, 4, 1, 3, 1, 1),
-    ((9, 6, 2, 3, 59), 5, 16, "fm", 1, 2, 16, 1, 3, 1, 1), ((12, 4, 2, 2, 36), 4, 64, "fm", 1, 2, 8, 1, 1, 1, 1),
+    ((9, 6, 2, 3, 59), 5, 16, "fm", 1, 2, 16, 1, 3, 1, 1), ((9, 4, 2, 2, 59), 3, 1, "fm", 1, 1, 8, 1, 0, 1, 1), ((12, 4, 2, 2, 36), 4, 64, "fm", 1, 2, 8, 1, 1, 1, 1),
     ((12, 6, 2, 3, 50), 6, 64, "tm", 2, 2, 16, 1, 7, 1, 1), ((14, 4, 2, 2, 50), 4, 256, "fm", 1, 2, 8, 1, 2, 0, 1),
     ((13, 5, 2, 2, 0), 4, 128, "fm", 1, 1, 8, 1, 1, 1, 0)]
 
