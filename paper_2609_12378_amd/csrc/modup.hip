@@ -515,7 +515,7 @@ bool f64_level_ok(const ckks_ctx *ctx, uint32_t level)
 namespace {
 
 template <typename Src>
-ckks_status modup_of(ckks_ctx *ctx, const Src &src, const PolySrc &c1, uint32_t count, uint32_t level, uint64_t *digits,
+ckks_status modup_of(ckks_ctx *ctx, const Src &src, const PolySrc *c1, uint32_t count, uint32_t level, uint64_t *digits,
                      bool own_rows)
 {
     Blocks bl{};
@@ -562,8 +562,9 @@ ckks_status modup_of(ckks_ctx *ctx, const Src &src, const PolySrc &c1, uint32_t 
         prof_end(ctx, K_NTT_FWD_COL);
         HIP_TRY(hipGetLastError());
     }
+    if (!c1) return CKKS_OK;   // the caller ends the transforms
     prof_begin(ctx, K_NTT_FWD_ROW, 16.0 * rows * ctx->n, (double)rows * ctx->n * kOpsButterflyF64 * 4);
-    hipLaunchKernelGGL(k_up_frow, dim3(rows * per), dim3(128), 0, ctx->stream, digits, c1, bl, own_rows, ctx->d_mod,
+    hipLaunchKernelGGL(k_up_frow, dim3(rows * per), dim3(128), 0, ctx->stream, digits, *c1, bl, own_rows, ctx->d_mod,
                        ctx->d_twf);
     prof_end(ctx, K_NTT_FWD_ROW);
     HIP_TRY(hipGetLastError());
@@ -574,11 +575,11 @@ ckks_status modup_of(ckks_ctx *ctx, const Src &src, const PolySrc &c1, uint32_t 
 
 ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t level, uint64_t *digits, bool own_rows)
 {
-    return modup_of(ctx, c1, c1, count, level, digits, own_rows);
+    return modup_of(ctx, c1, &c1, count, level, digits, own_rows);
 }
-ckks_status up_modup(ckks_ctx *ctx, const PolyProd &c, uint32_t count, uint32_t level, uint64_t *digits)
+ckks_status up_modup_cols(ckks_ctx *ctx, const PolyProd &c, uint32_t count, uint32_t level, uint64_t *digits)
 {
-    return modup_of(ctx, c, PolySrc{}, count, level, digits, false);
+    return modup_of(ctx, c, nullptr, count, level, digits, false);
 }
 
 ckks_status up_moddown(ckks_ctx *ctx, uint64_t *up, uint32_t polys, uint32_t level, uint64_t *cw)

@@ -116,9 +116,10 @@ inline bool f64_switch(const ckks_ctx *ctx, uint32_t level)
 struct PolySrc;
 ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t level, uint64_t *digits,
                      bool own_rows = true);
-// of at most kPolyList products (ks_args.h), without the digits' own rows
+// of at most kPolyList products (ks_args.h), without the digits' own rows and up to the column pass of the others' forward
+// transforms (raw doubles below 4.3 q)
 struct PolyProd;
-ckks_status up_modup(ckks_ctx *ctx, const PolyProd &c, uint32_t count, uint32_t level, uint64_t *digits);
+ckks_status up_modup_cols(ckks_ctx *ctx, const PolyProd &c, uint32_t count, uint32_t level, uint64_t *digits);
 // up: [polys][n_p][N] rows modulo P after the row pass of their inverse transform (raw doubles below 2q): finishes it,
 // converts to the level's q limbs and runs the first forward pass into cw ([polys][level+1][N] raw doubles)
 ckks_status up_moddown(ckks_ctx *ctx, uint64_t *up, uint32_t polys, uint32_t level, uint64_t *cw);
