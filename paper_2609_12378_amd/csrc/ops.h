@@ -152,6 +152,8 @@ ckks_status blk_rescale(ckks_ctx *ctx, const uint64_t *c, uint32_t polys, uint32
 // second components start at c1 and at b + (level+1) N; stage: count (level+1) N words
 ckks_status blk_modup(ckks_ctx *ctx, const PolySrc &c1, const uint64_t *b, uint32_t count, uint32_t level,
                       uint64_t *digits, uint64_t *stage);
+// of at most kPolyList products (ks_args.h)
+ckks_status blk_modup(ckks_ctx *ctx, const PolyProd &c, uint32_t count, uint32_t level, uint64_t *digits, uint64_t *stage);
 // a rotation batch; with ta, tb2 (ciphertexts) the addends are the first two components of their tensor product.
 // work: count 2 (level+1+n_p) N words
 struct RotArgs;

@@ -272,11 +272,18 @@ struct Digits {
     uint32_t nd, alpha, L, K, n_q;
     const double *inv[kMaxPrimes], *mod[kMaxPrimes];
 };
-// A polynomial that is switched: c1 of entry r of the batch, or (b set) the product of the second components of the
-// ciphertexts a and b ([2][L][N] each), formed where it is read
+// A polynomial that is switched: c1 of entry r of the batch, or a product, mult[r] c1 mul[r] (mul[r] null: c1), formed
+// where it is read
 struct Source {
     PolySrc c1;
-    const uint64_t *b;
+    const uint64_t *mul[kPolyList];
+    int8_t mult[kPolyList];
+    // the product's word modulo prime ar, |x| <= q/2 + 1, or v itself
+    __device__ double word(uint64_t v, uint32_t r, size_t at, const A &ar) const
+    {
+        const double x = A::from_u64(v);
+        return mul[r] ? ar.red((double)mult[r] * ar.mul(x, A::from_u64(mul[r][at]))) : x;
+    }
 };
 
 // acc[k] += y_i w_i for G consecutive sources, all their loads issued first
@@ -347,8 +354,7 @@ __global__ __launch_bounds__(blk::Shape<LOGN>::NT) void k_blk_digits(double *y, 
 #pragma unroll
     for (int k = 0; k < kE; k++) {
         const uint32_t p = blk::row_pos(t, k);
-        x[k] = A::from_u64(in[p]);
-        if (TENSOR) x[k] = ar.mul(x[k], A::from_u64(src.b[((size_t)(dg.L + l) << LOGN) + p]));
+        x[k] = TENSOR ? src.word(in[p], r, ((size_t)l << LOGN) + p, ar) : A::from_u64(in[p]);
     }
     blk::inverse<LOGN>(x, lds, cw, rw, ar, scaled(ar, dg.inv[j][l - j * dg.alpha]));
     double *o = y + (((size_t)r * dg.L + l) << LOGN);
@@ -374,8 +380,7 @@ void k_blk_modup(uint64_t *digits, const double *__restrict__ y, Source src, Dig
         for (int k = 0; k < kE; k++) {
             const uint32_t p = blk::row_pos(t, k);
             uint64_t v = in[p];
-            if (TENSOR)
-                v = ar.to_canon(ar.mul(A::from_u64(v), A::from_u64(src.b[((size_t)(dg.L + row) << LOGN) + p])));
+            if (TENSOR) v = ar.to_canon(src.word(v, r, ((size_t)row << LOGN) + p, ar));
             o[p] = v;
         }
         return;
@@ -716,8 +721,10 @@ ckks_status blk_rescale(ckks_ctx *ctx, const uint64_t *c, uint32_t polys, uint32
     return CKKS_OK;
 }
 
-ckks_status blk_modup(ckks_ctx *ctx, const PolySrc &c1, const uint64_t *b, uint32_t count, uint32_t level,
-                      uint64_t *digits, uint64_t *stage)
+namespace {
+
+ckks_status modup_of(ckks_ctx *ctx, const Source &from, bool b, uint32_t count, uint32_t level, uint64_t *digits,
+                     uint64_t *stage)
 {
     Digits dg{};
     dg.nd = n_digits(ctx, level);
@@ -738,8 +745,8 @@ ckks_status blk_modup(ckks_ctx *ctx, const PolySrc &c1, const uint64_t *b, uint3
     // a launch takes at most 65535 entries (blockIdx.y and z)
     for (uint32_t r0 = 0; r0 < count; r0 += 65535u) {
         const uint32_t cnt = std::min(count - r0, 65535u);
-        Source src{c1, b};
-        if (c1.base) src.c1.base += r0 * c1.stride;
+        Source src = from;
+        if (src.c1.base) src.c1.base += r0 * src.c1.stride;
         uint64_t *d = digits + (size_t)r0 * dg.nd * ext * N;
         double *yr = y + (size_t)r0 * dg.L * N;
         prof_begin(ctx, K_NTT_INV_ROW, 16.0 * cnt * dg.L * N);
@@ -767,6 +774,27 @@ ckks_status blk_modup(ckks_ctx *ctx, const PolySrc &c1, const uint64_t *b, uint3
         HIP_TRY(hipGetLastError());
     }
     return CKKS_OK;
+}
+
+}  // namespace
+
+ckks_status blk_modup(ckks_ctx *ctx, const PolySrc &c1, const uint64_t *b, uint32_t count, uint32_t level,
+                      uint64_t *digits, uint64_t *stage)
+{
+    Source src{c1, {}, {}};
+    if (b) src.mul[0] = b + (size_t)(level + 1) * ctx->n;
+    src.mult[0] = 1;
+    return modup_of(ctx, src, b != nullptr, count, level, digits, stage);
+}
+ckks_status blk_modup(ckks_ctx *ctx, const PolyProd &c, uint32_t count, uint32_t level, uint64_t *digits, uint64_t *stage)
+{
+    Source src{};
+    for (uint32_t r = 0; r < count; r++) {
+        src.c1.list[r] = c.list[r];
+        src.mul[r] = c.mul[r];
+        src.mult[r] = c.mult[r];
+    }
+    return modup_of(ctx, src, true, count, level, digits, stage);
 }
 
 ckks_status blk_rotate_batch(ckks_ctx *ctx, uint32_t level, const RotArgs &ra, uint64_t *work, const uint64_t *ta,

@@ -13,49 +13,121 @@ namespace {
 constexpr int kThreads = 256;
 
 using namespace steps;
+using namespace wsum;
 
-// d of every step ([dp][L][N] each, dp 3 where the steps switch a key, else 2), one position a thread.  The constant goes
-// in as c q_l: it vanishes modulo q_l and the rescale leaves c.  At most 11 products below 2^124 a sum.
-__global__ __launch_bounds__(kThreads) void k_step_lin(Batch bt, uint64_t *d, uint32_t dp, uint32_t L, uint32_t log_n,
-                                                       const ModQ *__restrict__ mods)
+// v times 1, 2 or -1 mod q
+__device__ __forceinline__ uint64_t times(uint64_t v, int mult, uint64_t q)
+{
+    return mult == 2 ? csub(2 * v, q) : mult < 0 && v ? q - v : v;
+}
+
+// d2 of the steps that switch a key to out[z][L][N], two positions a thread
+__global__ __launch_bounds__(kThreads) void k_step_d2(Batch bt, uint64_t *out, uint32_t L, uint32_t log_n,
+                                                      const ModQ *__restrict__ mods)
+{
+    const Operands &s = bt.s[blockIdx.z];
+    const uint32_t row = blockIdx.y, col = 2 * (blockIdx.x * kThreads + threadIdx.x);
+    if (col >> log_n) return;
+    const ModQ m = mods[row];
+    const size_t at = ((size_t)row << log_n) + col;
+    Pair v = ld2(s.a + at + ((size_t)(s.kind == kGiven ? 2 * L : s.a_limbs) << log_n));
+    if (s.kind == kProduct) {
+        const Pair w = ld2(s.b + at + ((size_t)s.b_limbs << log_n));
+        v = Pair{times(mulmod(v.x, w.x, m), s.mult, m.q), times(mulmod(v.y, w.y, m), s.mult, m.q)};
+    }
+    *(Pair *)(out + ((size_t)blockIdx.z * L << log_n) + at) = v;
+}
+
+// u[z][k][row] (wsum.hip) of every step, all of which switch a key or none, in exact 128-bit sums: a step's linear part is
+// at most 11 products below 2^124.  The constant goes in as c q_l: it vanishes modulo q_l and the division leaves c.  A
+// digit's own row is d2, formed again.  Two positions a thread.
+__global__ __launch_bounds__(kThreads) void k_step_u(Batch bt, const uint64_t *dig, const uint64_t *rlk, uint64_t *u, Dims d,
+                                                     uint32_t n, uint32_t per_row, const ulonglong2 *__restrict__ pmodq,
+                                                     const ModQ *__restrict__ mods)
 {
     __shared__ uint64_t ks[kStepTerms + 1];
-    const Operands &s = bt.s[blockIdx.z];
-    const uint32_t row = blockIdx.y, pos = blockIdx.x * kThreads + threadIdx.x;
-    const ModQ m = mods[row];
-    if (threadIdx.x <= s.n) {
+    uint32_t z, tile;
+    tile_of(n, z, tile);
+    const uint32_t row = tile / per_row, col = 2 * (tile % per_row * kThreads + threadIdx.x);
+    if (row >= d.ext) return;
+    const Operands &s = bt.s[z];
+    const uint32_t prime = d.prime(row);
+    const ModQ m = mods[prime];
+    const bool q_row = row < d.L;
+    if (q_row && threadIdx.x <= s.n) {
         const uint32_t i = threadIdx.x < s.n ? threadIdx.x : kStepTerms;
         const uint64_t r = int_mod(s.k[i], s.sh[i], m.q);
-        ks[threadIdx.x] = i < kStepTerms ? r : mulmod(r, mods[L - 1].q % m.q, m);
+        ks[threadIdx.x] = i < kStepTerms ? r : mulmod(r, mods[d.L - 1].q % m.q, m);
     }
     __syncthreads();
-    if (pos >> log_n) return;
-    const size_t at = ((size_t)row << log_n) + pos, half = (size_t)L << log_n;
-    acc128 x0{ks[s.n], 0}, x1{0, 0};
-    d += (size_t)blockIdx.z * dp * half;
-    if (s.kind == kProduct || s.kind == kPlain) {
-        const uint64_t *a = s.a + at, *b = s.b + at;
-        const uint64_t a0 = a[0], a1 = a[(size_t)s.a_limbs << log_n];
-        auto scaled = [&](uint64_t v) { return s.mult == 2 ? csub(2 * v, m.q) : s.mult < 0 && v ? m.q - v : v; };
-        const uint64_t b0 = scaled(b[0]);
-        mac(x0, a0, b0);
-        mac(x1, a1, b0);
-        if (s.kind == kProduct) {
-            const uint64_t b1 = scaled(b[(size_t)s.b_limbs << log_n]);
-            mac(x1, a0, b1);
-            d[2 * half + at] = mulmod(a1, b1, m);
+    if (col >> d.log_n) return;
+    const size_t at = ((size_t)row << d.log_n) + col, half = (size_t)d.L << d.log_n;
+    uint64_t r[2][2] = {}, d2[2] = {};   // [component][position]
+    if (q_row) {
+        acc128 x[2][2] = {{{ks[s.n], 0}, {ks[s.n], 0}}, {}};
+        if (s.kind == kGiven) {
+            const Pair v0 = ld2(s.a + at), v1 = ld2(s.a + half + at), v2 = ld2(s.a + 2 * half + at);
+            mac(x[0][0], v0.x, 1);
+            mac(x[0][1], v0.y, 1);
+            mac(x[1][0], v1.x, 1);
+            mac(x[1][1], v1.y, 1);
+            d2[0] = v2.x;
+            d2[1] = v2.y;
+        } else if (s.kind != kNone) {
+            const Pair a0 = ld2(s.a + at), a1 = ld2(s.a + at + ((size_t)s.a_limbs << d.log_n)), b0 = ld2(s.b + at);
+            const uint64_t c0 = times(b0.x, s.mult, m.q), c1 = times(b0.y, s.mult, m.q);
+            mac(x[0][0], a0.x, c0);
+            mac(x[0][1], a0.y, c1);
+            mac(x[1][0], a1.x, c0);
+            mac(x[1][1], a1.y, c1);
+            if (s.kind == kProduct) {
+                const Pair b1 = ld2(s.b + at + ((size_t)s.b_limbs << d.log_n));
+                const uint64_t e0 = times(b1.x, s.mult, m.q), e1 = times(b1.y, s.mult, m.q);
+                mac(x[1][0], a0.x, e0);
+                mac(x[1][1], a0.y, e1);
+                d2[0] = mulmod(a1.x, e0, m);
+                d2[1] = mulmod(a1.y, e1, m);
+            }
         }
-    } else if (s.kind == kGiven) {
-        mac(x0, s.a[at], 1);
-        mac(x1, s.a[half + at], 1);
-        d[2 * half + at] = s.a[2 * half + at];
+        for (uint32_t i = 0; i < s.n; i++) {
+            const Pair v = ld2(s.z[i] + at);
+            mac(x[0][0], v.x, ks[i]);
+            mac(x[0][1], v.y, ks[i]);
+            if (s.polys[i] < 2) continue;
+            const Pair w = ld2(s.z[i] + at + ((size_t)s.limbs[i] << d.log_n));
+            mac(x[1][0], w.x, ks[i]);
+            mac(x[1][1], w.y, ks[i]);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; k++) r[k >> 1][k & 1] = reduce128(x[k >> 1][k & 1], m);
     }
-    for (uint32_t i = 0; i < s.n; i++) {
-        mac(x0, s.z[i][at], ks[i]);
-        if (s.polys[i] == 2) mac(x1, s.z[i][at + ((size_t)s.limbs[i] << log_n)], ks[i]);
+    if (s.switched()) {
+        const uint64_t pq = q_row ? pmodq[row].x : 0;
+        const uint32_t own = q_row ? row / d.alpha : d.nd;
+        acc128 t[2][2] = {};
+#pragma unroll
+        for (int k = 0; k < 4; k++) mac(t[k >> 1][k & 1], r[k >> 1][k & 1], pq);
+        dig += ((size_t)z * d.nd * d.ext << d.log_n) + at;
+        const uint64_t *key = rlk + ((size_t)prime << d.log_n) + col;
+        for (uint32_t i = 0; i < d.nd; i++) {
+            Pair v{d2[0], d2[1]};
+            if (i != own) v = ld2(dig + ((size_t)i * d.ext << d.log_n));
+            const Pair k0 = ld2(key + ((size_t)(2 * i) * d.key_rows << d.log_n));
+            const Pair k1 = ld2(key + ((size_t)(2 * i + 1) * d.key_rows << d.log_n));
+            mac(t[0][0], v.x, k0.x);
+            mac(t[0][1], v.y, k0.y);
+            mac(t[1][0], v.x, k1.x);
+            mac(t[1][1], v.y, k1.y);
+            if ((i & 7u) == 7u)   // eight products and what is left of those before, below 2^128
+#pragma unroll
+                for (int k = 0; k < 4; k++) t[k >> 1][k & 1] = acc128{reduce128(t[k >> 1][k & 1], m), 0};
+        }
+#pragma unroll
+        for (int k = 0; k < 4; k++) r[k >> 1][k & 1] = reduce128(t[k >> 1][k & 1], m);
     }
-    d[at] = reduce128(x0, m);
-    d[half + at] = reduce128(x1, m);
+#pragma unroll
+    for (int k = 0; k < 2; k++)
+        *(Pair *)(u + (((size_t)(z * 2 + k) * d.ext + row) << d.log_n) + col) = Pair{r[k][0], r[k][1]};
 }
 
 struct Squares {
@@ -108,61 +180,74 @@ Operands operands(const Step &s)
     return o;
 }
 
-// rows (of N words) of a batch of n steps, region by region
+// rows (of N words) of a batch of n steps, region by region: the digits, d2 for the ModUp, u, the converted rows.  One
+// figure for both arithmetics: a workspace of it serves after ckks_ctx_set_ntt_arith as well.  The fp64 kernels take no
+// more: of u they write the rows q_l and P alone.
 struct Rows {
-    size_t d, dig, stage, work, sum, top, total;
+    size_t dig, stage, u, x, total;
 };
 Rows rows_of(const ckks_ctx *ctx, uint32_t L, size_t n, bool switched)
 {
-    const size_t ext = L + ctx->n_p, nd = n_digits(ctx, L - 1);
+    const size_t ext = L + (switched ? ctx->n_p : 0);
     Rows r{};
-    r.d = (switched ? 3 : 2) * L * n;
-    r.top = 2 * L * n;
     if (switched) {
-        r.dig = nd * ext * n;
-        r.stage = std::max(L, ctx->alpha) * n;
-        r.work = (2 * ext + 2 * L) * n;
-        r.sum = 2 * L * n;
+        r.dig = n_digits(ctx, L - 1) * ext * n;
+        r.stage = L * n;
     }
-    r.total = r.d + r.dig + r.stage + r.work + r.sum + r.top;
+    r.u = 2 * ext * n;
+    r.x = 2 * (L - 1) * n;
+    r.total = r.dig + r.stage + r.u + r.x;
     return r;
 }
 
-// n steps that all switch a key, or none of them does, in any ring and arithmetic: d, ModUp, ModDown, rescale
-ckks_status run_batch(ckks_ctx *ctx, uint32_t L, const Batch &b, uint32_t n, bool switched, const uint64_t *rlk,
+// n steps that all switch a key, or none of them does, in any ring and primes (wsum_exact.hip divides)
+ckks_status run_exact(ckks_ctx *ctx, uint32_t L, const Batch &b, uint32_t n, bool switched, const uint64_t *rlk,
                       uint64_t *mem)
 {
     const size_t N = ctx->n;
-    const uint32_t ext = L + ctx->n_p, nd = n_digits(ctx, L - 1), dp = switched ? 3 : 2;
+    Dims d = wsum_dims(ctx, L);
     const Rows r = rows_of(ctx, L, n, switched);
-    uint64_t *d = mem, *dig = d + r.d * N, *work = dig + (r.dig + r.stage) * N, *sum = work + r.work * N,
-             *top = sum + r.sum * N;
+    uint64_t *dig = mem, *stage = dig + r.dig * N, *u = stage + r.stage * N, *x = u + r.u * N;
+    const uint32_t per_row = (ctx->n + 2 * kThreads - 1) / (2 * kThreads);
+    Args a{};
+    a.kind[0].rotated = switched;
     double words = 0;
-    for (uint32_t i = 0; i < n; i++) words += dp + 2.0 * b.s[i].n + (b.s[i].kind == kProduct ? 4 : b.s[i].kind ? 3 : 0);
-    prof_begin(ctx, K_ELEM, 8.0 * words * L * N);
-    hipLaunchKernelGGL(k_step_lin, grid_of(ctx, L, n), dim3(kThreads), 0, ctx->stream, b, d, dp, L, ctx->log_n, ctx->d_mod);
-    prof_end(ctx, K_ELEM);
-    HIP_TRY(hipGetLastError());
-    std::vector<uint64_t *> outs(n);
-    for (uint32_t i = 0; i < n; i++) outs[i] = b.s[i].out;
-    if (!switched) return rescale_each(ctx, d, n, L - 1, outs.data(), top);
-    // a relinearisation is a rotation by the identity: (d0 + u0, d1 + u1), u the key switch of d2
-    std::vector<const uint64_t *> c0(n), add1(n), digs(n), keys(n, rlk);
-    std::vector<uint32_t> g(n, 1);
-    std::vector<uint64_t *> sums(n);
     for (uint32_t i = 0; i < n; i++) {
-        c0[i] = d + (size_t)i * 3 * L * N;
-        add1[i] = c0[i] + L * N;
-        digs[i] = dig + (size_t)i * nd * ext * N;
-        sums[i] = sum + (size_t)i * 2 * L * N;
+        a.ct[i].out[0] = b.s[i].out;
+        words += 2.0 * b.s[i].n + (b.s[i].kind == kProduct ? 4 : b.s[i].kind ? 3 : 0);
     }
-    CK_TRY(ks_modup_batch(ctx, d + 2 * (size_t)L * N, 3 * (size_t)L * N, n, L - 1, dig, r.stage));
-    CK_TRY(ks_rotate_batch(ctx, L - 1, n, c0.data(), digs.data(), g.data(), keys.data(), sums.data(), work, nullptr,
-                           add1.data()));
-    return rescale_each(ctx, sum, n, L - 1, outs.data(), top);
+    if (switched) {
+        prof_begin(ctx, K_ELEM, 24.0 * L * N * n);
+        hipLaunchKernelGGL(k_step_d2, dim3(per_row, L, n), dim3(kThreads), 0, ctx->stream, b, stage, L, ctx->log_n, ctx->d_mod);
+        prof_end(ctx, K_ELEM);
+        HIP_TRY(hipGetLastError());
+        CK_TRY(ks_modup_staged(ctx, stage, n, L - 1, dig));
+    } else {
+        d.K = 0;
+        d.ext = L;
+    }
+    prof_begin(ctx, K_KEYIP, 8.0 * N * (words * L + n * d.ext * (switched ? d.nd + 2.0 : 2.0)));
+    hipLaunchKernelGGL(k_step_u, dim3((d.ext * per_row + 7) / 8 * 8 * n), dim3(kThreads), 0, ctx->stream, b, dig, rlk, u, d, n,
+                       per_row, ctx->d_pmodq, ctx->d_mod);
+    prof_end(ctx, K_KEYIP);
+    HIP_TRY(hipGetLastError());
+    return wsum_exact_divide(ctx, a, n, 1, d, switched, u, x);
 }
 
 }  // namespace
+
+PolyProd step_sources(const ckks_ctx *ctx, uint32_t L, const Batch &b, uint32_t n_sw)
+{
+    static_assert(kStepBatch <= (uint32_t)kPolyList && kStepBatch <= kWsumCts, "a batch fits the lists");
+    PolyProd src{};
+    for (uint32_t i = 0; i < n_sw; i++) {
+        const Operands &s = b.s[i];
+        src.list[i] = s.a + (s.kind == kGiven ? 2 * (size_t)L : s.a_limbs) * ctx->n;
+        src.mul[i] = s.kind == kGiven ? nullptr : s.b + (size_t)s.b_limbs * ctx->n;
+        src.mult[i] = s.mult;
+    }
+    return src;
+}
 
 bool step_int(double x, StepInt *out)
 {
@@ -179,9 +264,7 @@ bool step_int(double x, StepInt *out)
 
 size_t step_scratch_words(const ckks_ctx *ctx, uint32_t L, uint32_t steps, bool switched)
 {
-    const uint32_t n = std::min(steps, kStepBatch);
-    // one figure for both arithmetics: a workspace of it serves after ckks_ctx_set_ntt_arith as well
-    return std::max(rows_of(ctx, L, n, switched).total, step_f64_rows(ctx, L, n, switched)) * ctx->n;
+    return rows_of(ctx, L, std::min(steps, kStepBatch), switched).total * ctx->n;
 }
 
 ckks_status step_run(ckks_ctx *ctx, uint32_t L, const std::vector<Step> &steps, const uint64_t *rlk, uint64_t *mem)
@@ -194,14 +277,14 @@ ckks_status step_run(ckks_ctx *ctx, uint32_t L, const std::vector<Step> &steps, 
             if (s.switched() == (sw != 0)) list.push_back(&s);
         if (sw) n_sw = list.size();
     }
-    const bool fast = step_f64_ok(ctx, L);
+    const bool fast = f64_switch(ctx, L - 1);
     for (size_t at = 0; at < list.size();) {
         const size_t sw = at < n_sw ? n_sw - at : 0;
         const uint32_t n = (uint32_t)std::min<size_t>({kStepBatch, list.size() - at, !fast && sw ? sw : kStepBatch});
         Batch b{};
         for (uint32_t i = 0; i < n; i++) b.s[i] = operands(*list[at + i]);
-        if (fast) CK_TRY(step_f64(ctx, L, b, n, (uint32_t)std::min<size_t>(sw, n), rlk, mem));
-        else CK_TRY(run_batch(ctx, L, b, n, sw != 0, rlk, mem));
+        if (fast) CK_TRY((blk_switch(ctx, L - 1) ? step_blk : step_f64)(ctx, L, b, n, (uint32_t)std::min<size_t>(sw, n), rlk, mem));
+        else CK_TRY(run_exact(ctx, L, b, n, sw != 0, rlk, mem));
         at += n;
     }
     return CKKS_OK;

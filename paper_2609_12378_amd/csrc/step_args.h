@@ -43,9 +43,13 @@ __device__ __forceinline__ double int_mod(int64_t m, uint32_t sh, const wsum::A 
 
 }  // namespace steps
 
-// fp64 arithmetic at L limbs, N >= 2^14: n steps, of which the first n_sw switch a key
-bool step_f64_ok(const ckks_ctx *ctx, uint32_t L);
+// the products d2 of the first n_sw steps, as a ModUp reads them
+PolyProd step_sources(const ckks_ctx *ctx, uint32_t L, const steps::Batch &b, uint32_t n_sw);
+
+// n steps at L >= 2 limbs, of which the first n_sw switch a key, in `mem` of step_scratch_words(ctx, L, n, n_sw > 0) words:
+// fp64 arithmetic (f64_switch) in two passes a transform, N >= 2^14 (step_f64.hip) ...
 ckks_status step_f64(ckks_ctx *ctx, uint32_t L, const steps::Batch &b, uint32_t n, uint32_t n_sw, const uint64_t *rlk,
                      uint64_t *mem);
-// words of its scratch
-size_t step_f64_rows(const ckks_ctx *ctx, uint32_t L, size_t n, bool switched);
+// ... or in whole rows, N = 2^12 and 2^13 (step_block.hip)
+ckks_status step_blk(ckks_ctx *ctx, uint32_t L, const steps::Batch &b, uint32_t n, uint32_t n_sw, const uint64_t *rlk,
+                     uint64_t *mem);

@@ -262,18 +262,6 @@ __global__ __launch_bounds__(64) void k_step_fin8(Batch bt, const uint64_t *dig,
 
 }  // namespace
 
-bool step_f64_ok(const ckks_ctx *ctx, uint32_t L)
-{
-    return L >= 2 && ctx->log_n >= 14 && f64_switch(ctx, L - 1);
-}
-
-// rows of N words: the digits, the rows q_l and P of u, the converted rows
-size_t step_f64_rows(const ckks_ctx *ctx, uint32_t L, size_t n, bool switched)
-{
-    const size_t K = switched ? ctx->n_p : 0, dig = switched ? (size_t)n_digits(ctx, L - 1) * (L + K) : 0;
-    return n * (dig + 2 * (K + 1) + 2 * (L - 1));
-}
-
 ckks_status step_f64(ckks_ctx *ctx, uint32_t L, const Batch &b, uint32_t n, uint32_t n_sw, const uint64_t *rlk,
                      uint64_t *mem)
 {
@@ -283,14 +271,7 @@ ckks_status step_f64(ckks_ctx *ctx, uint32_t L, const Batch &b, uint32_t n, uint
     const uint32_t level = L - 1, bpl = 1u << (d.log_n - 9);
     uint64_t *dig = mem, *up = dig + (size_t)n_sw * d.nd * d.ext * N;
     if (n_sw) {
-        PolyProd src{};
-        for (uint32_t i = 0; i < n_sw; i++) {
-            const Operands &s = b.s[i];
-            src.list[i] = s.a + (s.kind == kGiven ? 2 * (size_t)L : s.a_limbs) * N;
-            src.mul[i] = s.kind == kGiven ? nullptr : s.b + (size_t)s.b_limbs * N;
-            src.mult[i] = s.mult;
-        }
-        CK_TRY(up_modup_cols(ctx, src, n_sw, level, dig));
+        CK_TRY(up_modup_cols(ctx, step_sources(ctx, L, b, n_sw), n_sw, level, dig));
     } else {
         d.K = 0;
         d.ext = L;

@@ -120,5 +120,8 @@ ckks_status wsum_blk_sums(ckks_ctx *ctx, const wsum::Args &a, uint32_t n, uint32
 // n pages level N
 ckks_status wsum_exact_sums(ckks_ctx *ctx, const wsum::Args &a, uint32_t n, uint32_t pages, const wsum::Dims &d, bool rot,
                             uint64_t *u, uint64_t *x);
+// ... from u that is there to the outputs
+ckks_status wsum_exact_divide(ckks_ctx *ctx, const wsum::Args &a, uint32_t n, uint32_t pages, const wsum::Dims &d, bool rot,
+                              uint64_t *u, uint64_t *x);
 // c1 of the first n ciphertexts to out[n][L][N]
 ckks_status wsum_gather_c1(ckks_ctx *ctx, const wsum::Args &a, uint32_t n, uint32_t L, uint64_t *out);

@@ -282,7 +282,6 @@ ckks_status wsum_exact_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t p
         d.ext = d.L;
     }
     const size_t N = ctx->n;
-    const uint32_t level = d.L - 1, outs = n * pages, polys = 2 * outs;
     if (rot) {
         const uint32_t per_row = grid_of(ctx, 1, 1, 2).x, tiles = (d.ext * per_row + 7) / 8 * 8;
         prof_begin(ctx, K_KEYIP, 8.0 * N * d.ext * n * (d.nd + 1.0 + 2.0 * pages));
@@ -299,7 +298,19 @@ ckks_status wsum_exact_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t p
         prof_end(ctx, K_ELEM);
     }
     HIP_TRY(hipGetLastError());
+    return wsum_exact_divide(ctx, a, n, pages, dims, rot, u, x);
+}
 
+ckks_status wsum_exact_divide(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pages, const Dims &dims, bool rot,
+                              uint64_t *u, uint64_t *x)
+{
+    Dims d = dims;
+    if (!rot) {
+        d.K = 0;
+        d.ext = d.L;
+    }
+    const size_t N = ctx->n;
+    const uint32_t level = d.L - 1, outs = n * pages, polys = 2 * outs;
     LimbMap m = limb_range(level, 1);
     for (uint32_t i = 0; i < d.K; i++) m.prime[m.n++] = (uint8_t)(d.n_q + i);
     uint64_t *top = u + (size_t)level * N;
