@@ -278,11 +278,23 @@ struct Source {
     PolySrc c1;
     const uint64_t *mul[kPolyList];
     int8_t mult[kPolyList];
-    // the product's word modulo prime ar, |x| <= q/2 + 1, or v itself
-    __device__ double word(uint64_t v, uint32_t r, size_t at, const A &ar) const
+    // entry r's words of the row at `row` at a thread's 16 points, |x| <= q/2 + 1 or canonical
+    __device__ void words(double (&x)[kE], uint32_t r, size_t row, const A &ar) const
     {
-        const double x = A::from_u64(v);
-        return mul[r] ? ar.red((double)mult[r] * ar.mul(x, A::from_u64(mul[r][at]))) : x;
+        const uint64_t *a = c1.at(r) + row, *b = mul[r];
+        uint64_t v[kE], w[kE];
+#pragma unroll
+        for (int k = 0; k < kE; k++) v[k] = a[blk::row_pos(threadIdx.x, k)];
+        if (b) {
+#pragma unroll
+            for (int k = 0; k < kE; k++) w[k] = b[row + blk::row_pos(threadIdx.x, k)];
+            const double m = mult[r];
+#pragma unroll
+            for (int k = 0; k < kE; k++) x[k] = ar.red(m * ar.mul(A::from_u64(v[k]), A::from_u64(w[k])));
+        } else {
+#pragma unroll
+            for (int k = 0; k < kE; k++) x[k] = A::from_u64(v[k]);
+        }
     }
 };
 
@@ -349,12 +361,13 @@ __global__ __launch_bounds__(blk::Shape<LOGN>::NT) void k_blk_digits(double *y, 
     const A ar(tb.mods[l]);
     const blk::ColTw<LOGN> cw(table<LOGN>(tb.itwf, l));
     const blk::RowTw<LOGN> rw(table<LOGN>(tb.itwf, l));
-    const uint64_t *in = src.c1.at(r) + ((size_t)l << LOGN);
     double x[kE];
+    if constexpr (TENSOR) {
+        src.words(x, r, (size_t)l << LOGN, ar);
+    } else {
+        const uint64_t *in = src.c1.at(r) + ((size_t)l << LOGN);
 #pragma unroll
-    for (int k = 0; k < kE; k++) {
-        const uint32_t p = blk::row_pos(t, k);
-        x[k] = TENSOR ? src.word(in[p], r, ((size_t)l << LOGN) + p, ar) : A::from_u64(in[p]);
+        for (int k = 0; k < kE; k++) x[k] = A::from_u64(in[blk::row_pos(t, k)]);
     }
     blk::inverse<LOGN>(x, lds, cw, rw, ar, scaled(ar, dg.inv[j][l - j * dg.alpha]));
     double *o = y + (((size_t)r * dg.L + l) << LOGN);
@@ -375,13 +388,18 @@ void k_blk_modup(uint64_t *digits, const double *__restrict__ y, Source src, Dig
     const A ar(tb.mods[prime]);
     uint64_t *o = digits + ((((size_t)r * dg.nd + j) * ext + row) << LOGN);
     if (row >= lo && row < hi) {
-        const uint64_t *in = src.c1.at(r) + ((size_t)row << LOGN);
+        if constexpr (TENSOR) {
+            double x[kE];
+            src.words(x, r, (size_t)row << LOGN, ar);
 #pragma unroll
-        for (int k = 0; k < kE; k++) {
-            const uint32_t p = blk::row_pos(t, k);
-            uint64_t v = in[p];
-            if (TENSOR) v = ar.to_canon(src.word(v, r, ((size_t)row << LOGN) + p, ar));
-            o[p] = v;
+            for (int k = 0; k < kE; k++) o[blk::row_pos(t, k)] = ar.to_canon(x[k]);
+        } else {
+            const uint64_t *in = src.c1.at(r) + ((size_t)row << LOGN);
+#pragma unroll
+            for (int k = 0; k < kE; k++) {
+                const uint32_t p = blk::row_pos(t, k);
+                o[p] = in[p];
+            }
         }
         return;
     }

@@ -114,6 +114,9 @@ ckks_status wsum_convert(ckks_ctx *ctx, const wsum::Args &a, uint32_t n, uint32_
 // N = 2^12 and 2^13 (wsum_block.hip): the sums and the division of n ciphertexts whose digits are formed;
 // u: 2 n pages (level+1+n_p) N words
 ckks_status wsum_blk_sums(ckks_ctx *ctx, const wsum::Args &a, uint32_t n, uint32_t pages, const wsum::Dims &d, uint64_t *u);
+// ... from u that is there (raw doubles of at most q/2 + 1) to the outputs
+ckks_status wsum_blk_divide(ckks_ctx *ctx, const wsum::Args &a, uint32_t n, uint32_t pages, const wsum::Dims &d,
+                            uint64_t *u);
 
 // Any ring and any primes (wsum_exact.hip): the same in exact 128-bit sums, of ciphertexts that are all of rotated
 // kinds (rot) or all of unrotated ones; a.ct[z].dig's own rows are not read.  u: 2 n pages (level+1+n_p) N words, x: 2

@@ -8,13 +8,20 @@
 // Few ciphertexts are bounded by one row's latency a launch: one of 4 limbs at N = 2^12 takes 4, 7 and 11 us in the
 // three (35 us a call, as long as the host takes to issue it), three of 6 limbs at 2^13 7, 11 and 17 (58 us a call).  The
 // sums of 1 could be formed where 2 and 3 read them, a row a block, in one launch fewer; that is not tried.
+#include "ntt_block.h"
 #include "ops.h"
-#include "wsum_block.h"
+#include "wsum_args.h"
 
 namespace {
 
 using namespace wsum;
+using nttc::GridSum;
 using nttc::kE;
+
+struct Tab {
+    const ModQ *mods;
+    const double *twf, *itwf;
+};
 
 // u[z P + o][k][row][n] as doubles of at most q/2 + 1: one position a thread, every load issued before the first
 // product. Unrotated kinds: pt c, on the q rows alone.
@@ -122,6 +129,40 @@ __global__ __launch_bounds__(blk::Shape<LOGN>::NT) void k_blk_wtop(uint64_t *u, 
     for (int k = 0; k < kE; k++) row[blk::col_pos<LOGN>(t, k)] = A::to_raw(centre(ar, x[k]));
 }
 
+// v = sum_i y_i m(i) mod q, |v| <= q/2 + 1, at a thread's 16 points of the K digit rows that follow yr
+template <int LOGN, typename Factor>
+__device__ __forceinline__ void digit_sums(double (&v)[kE], const uint64_t *yr, const Dims &d, const A &ar, Factor m)
+{
+    const uint32_t t = threadIdx.x;
+    const int K = (int)d.K;
+#pragma unroll
+    for (int e0 = 0; e0 < kE; e0 += 8) {
+        GridSum acc[8];
+        // two sources' loads at a time
+        for (int s = 0; s < K; s += 2) {
+            double y[2][8];
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    y[h][e] = A::from_raw(yr[((size_t)min(s + h + 1, K) << LOGN) + blk::col_pos<LOGN>(t, e0 + e)]);
+            if (s && s % GridSum::kTerms == 0) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) acc[e].fold(ar);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                if (s + h >= K) break;
+                const double w = m(s + h);
+#pragma unroll
+                for (int e = 0; e < 8; e++) acc[e].add(y[h][e], w);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e0 + e] = ar.red(acc[e].value(ar));
+    }
+}
+
 // row i of component k of output o: grid (level, 2, outs).  The K digits and the q_l row follow one another in u.
 template <int LOGN>
 __global__ __launch_bounds__(blk::Shape<LOGN>::NT) void k_blk_wfin(Args a, const uint64_t *u, Dims d, uint32_t pages,
@@ -179,12 +220,7 @@ __global__ __launch_bounds__(blk::Shape<LOGN>::NT) void k_blk_wfin(Args a, const
 
 ckks_status wsum_blk_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pages, const Dims &d, uint64_t *u)
 {
-    const uint32_t level = d.L - 1, polys = 2 * n * pages;
     const double N = ctx->n;
-    const ConvDev *cd;
-    CK_TRY(ctx_conv(ctx, (int)level, -1, &cd));
-    const Quot qt{cd->d_qhat_inv_f, cd->d_qhat_mod_f, ctx->d_pinv, ctx->d_qlinv + (size_t)level * ctx->n_q, ctx->d_pmodq};
-    const Tab tb{ctx->d_mod, ctx->d_twf, ctx->d_itwf};
     prof_begin(ctx, K_KEYIP, 8.0 * N * d.ext * n * (d.nd + 1.0 + 2.0 * pages));
 #define CK_GO(ND)                                                                                                  \
     do {                                                                                                           \
@@ -204,6 +240,17 @@ ckks_status wsum_blk_sums(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pag
 #undef CK_GO
     prof_end(ctx, K_KEYIP);
     HIP_TRY(hipGetLastError());
+    return wsum_blk_divide(ctx, a, n, pages, d, u);
+}
+
+ckks_status wsum_blk_divide(ckks_ctx *ctx, const Args &a, uint32_t n, uint32_t pages, const Dims &d, uint64_t *u)
+{
+    const uint32_t level = d.L - 1, polys = 2 * n * pages;
+    const double N = ctx->n;
+    const ConvDev *cd;
+    CK_TRY(ctx_conv(ctx, (int)level, -1, &cd));
+    const Quot qt{cd->d_qhat_inv_f, cd->d_qhat_mod_f, ctx->d_pinv, ctx->d_qlinv + (size_t)level * ctx->n_q, ctx->d_pmodq};
+    const Tab tb{ctx->d_mod, ctx->d_twf, ctx->d_itwf};
     prof_begin(ctx, K_NTT_INV_ROW, 16.0 * polys * (d.K + 1) * N, polys * (d.K + 1) * N * kOpsButterflyF64 * d.log_n / 2);
 #define CK_BLK(KERNEL, GRID, ...)                                                                                  \
     do {                                                                                                           \
