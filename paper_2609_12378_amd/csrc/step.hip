@@ -30,9 +30,9 @@ __global__ __launch_bounds__(kThreads) void k_step_d2(Batch bt, uint64_t *out, u
     if (col >> log_n) return;
     const ModQ m = mods[row];
     const size_t at = ((size_t)row << log_n) + col;
-    Pair v = ld2(s.a + at + ((size_t)(s.kind == kGiven ? 2 * L : s.a_limbs) << log_n));
-    if (s.kind == kProduct) {
-        const Pair w = ld2(s.b + at + ((size_t)s.b_limbs << log_n));
+    Pair v = ld2(s.a + at + ((size_t)(s.kind() == kGiven ? 2 * L : s.a_limbs()) << log_n));
+    if (s.kind() == kProduct) {
+        const Pair w = ld2(s.b + at + ((size_t)s.b_limbs() << log_n));
         v = Pair{times(mulmod(v.x, w.x, m), s.mult, m.q), times(mulmod(v.y, w.y, m), s.mult, m.q)};
     }
     *(Pair *)(out + ((size_t)blockIdx.z * L << log_n) + at) = v;
@@ -54,9 +54,9 @@ __global__ __launch_bounds__(kThreads) void k_step_u(Batch bt, const uint64_t *d
     const uint32_t prime = d.prime(row);
     const ModQ m = mods[prime];
     const bool q_row = row < d.L;
-    if (q_row && threadIdx.x <= s.n) {
-        const uint32_t i = threadIdx.x < s.n ? threadIdx.x : kStepTerms;
-        const uint64_t r = int_mod(s.k[i], s.sh[i], m.q);
+    if (q_row && threadIdx.x <= s.n()) {
+        const uint32_t i = threadIdx.x < s.n() ? threadIdx.x : kStepTerms;
+        const uint64_t r = int_mod(s.k[i], s.sh(i), m.q);
         ks[threadIdx.x] = i < kStepTerms ? r : mulmod(r, mods[d.L - 1].q % m.q, m);
     }
     __syncthreads();
@@ -64,8 +64,8 @@ __global__ __launch_bounds__(kThreads) void k_step_u(Batch bt, const uint64_t *d
     const size_t at = ((size_t)row << d.log_n) + col, half = (size_t)d.L << d.log_n;
     uint64_t r[2][2] = {}, d2[2] = {};   // [component][position]
     if (q_row) {
-        acc128 x[2][2] = {{{ks[s.n], 0}, {ks[s.n], 0}}, {}};
-        if (s.kind == kGiven) {
+        acc128 x[2][2] = {{{ks[s.n()], 0}, {ks[s.n()], 0}}, {}};
+        if (s.kind() == kGiven) {
             const Pair v0 = ld2(s.a + at), v1 = ld2(s.a + half + at), v2 = ld2(s.a + 2 * half + at);
             mac(x[0][0], v0.x, 1);
             mac(x[0][1], v0.y, 1);
@@ -73,15 +73,15 @@ __global__ __launch_bounds__(kThreads) void k_step_u(Batch bt, const uint64_t *d
             mac(x[1][1], v1.y, 1);
             d2[0] = v2.x;
             d2[1] = v2.y;
-        } else if (s.kind != kNone) {
-            const Pair a0 = ld2(s.a + at), a1 = ld2(s.a + at + ((size_t)s.a_limbs << d.log_n)), b0 = ld2(s.b + at);
+        } else if (s.kind() != kNone) {
+            const Pair a0 = ld2(s.a + at), a1 = ld2(s.a + at + ((size_t)s.a_limbs() << d.log_n)), b0 = ld2(s.b + at);
             const uint64_t c0 = times(b0.x, s.mult, m.q), c1 = times(b0.y, s.mult, m.q);
             mac(x[0][0], a0.x, c0);
             mac(x[0][1], a0.y, c1);
             mac(x[1][0], a1.x, c0);
             mac(x[1][1], a1.y, c1);
-            if (s.kind == kProduct) {
-                const Pair b1 = ld2(s.b + at + ((size_t)s.b_limbs << d.log_n));
+            if (s.kind() == kProduct) {
+                const Pair b1 = ld2(s.b + at + ((size_t)s.b_limbs() << d.log_n));
                 const uint64_t e0 = times(b1.x, s.mult, m.q), e1 = times(b1.y, s.mult, m.q);
                 mac(x[1][0], a0.x, e0);
                 mac(x[1][1], a0.y, e1);
@@ -89,12 +89,12 @@ __global__ __launch_bounds__(kThreads) void k_step_u(Batch bt, const uint64_t *d
                 d2[1] = mulmod(a1.y, e1, m);
             }
         }
-        for (uint32_t i = 0; i < s.n; i++) {
+        for (uint32_t i = 0; i < s.n(); i++) {
             const Pair v = ld2(s.z[i] + at);
             mac(x[0][0], v.x, ks[i]);
             mac(x[0][1], v.y, ks[i]);
-            if (s.polys[i] < 2) continue;
-            const Pair w = ld2(s.z[i] + at + ((size_t)s.limbs[i] << d.log_n));
+            if (!s.two(i)) continue;
+            const Pair w = ld2(s.z[i] + at + ((size_t)s.limbs(i) << d.log_n));
             mac(x[1][0], w.x, ks[i]);
             mac(x[1][1], w.y, ks[i]);
         }
@@ -160,23 +160,19 @@ dim3 grid_of(const ckks_ctx *ctx, uint32_t rows, uint32_t z) { return dim3((ctx-
 Operands operands(const Step &s)
 {
     Operands o{};
-    o.kind = s.d ? kGiven : !s.a ? kNone : s.b_polys == 2 ? kProduct : kPlain;
+    const uint32_t kind = s.d ? kGiven : !s.a ? kNone : s.b_polys == 2 ? kProduct : kPlain;
     o.a = s.d ? s.d : s.a;
     o.b = s.b;
     o.out = s.out;
-    o.a_limbs = (uint8_t)s.a_limbs;
-    o.b_limbs = (uint8_t)s.b_limbs;
-    o.mult = (int8_t)s.mult;
-    o.n = (uint8_t)s.n_terms;
+    o.info = s.n_terms | kind << 8 | s.a_limbs << 16 | s.b_limbs << 24;
+    o.mult = s.mult;
     for (uint32_t i = 0; i < s.n_terms; i++) {
         o.z[i] = s.t[i].z;
         o.k[i] = s.t[i].k.m;
-        o.sh[i] = (uint8_t)s.t[i].k.sh;
-        o.limbs[i] = (uint8_t)s.t[i].limbs;
-        o.polys[i] = (uint8_t)s.t[i].polys;
+        o.term[i] = s.t[i].k.sh | s.t[i].limbs << 8 | s.t[i].polys << 16;
     }
     o.k[kStepTerms] = s.c.m;
-    o.sh[kStepTerms] = (uint8_t)s.c.sh;
+    o.term[kStepTerms] = s.c.sh;
     return o;
 }
 
@@ -214,7 +210,7 @@ ckks_status run_exact(ckks_ctx *ctx, uint32_t L, const Batch &b, uint32_t n, boo
     double words = 0;
     for (uint32_t i = 0; i < n; i++) {
         a.ct[i].out[0] = b.s[i].out;
-        words += 2.0 * b.s[i].n + (b.s[i].kind == kProduct ? 4 : b.s[i].kind ? 3 : 0);
+        words += 2.0 * b.s[i].n() + (b.s[i].kind() == kProduct ? 4 : b.s[i].kind() ? 3 : 0);
     }
     if (switched) {
         prof_begin(ctx, K_ELEM, 24.0 * L * N * n);
@@ -242,8 +238,8 @@ PolyProd step_sources(const ckks_ctx *ctx, uint32_t L, const Batch &b, uint32_t 
     PolyProd src{};
     for (uint32_t i = 0; i < n_sw; i++) {
         const Operands &s = b.s[i];
-        src.list[i] = s.a + (s.kind == kGiven ? 2 * (size_t)L : s.a_limbs) * ctx->n;
-        src.mul[i] = s.kind == kGiven ? nullptr : s.b + (size_t)s.b_limbs * ctx->n;
+        src.list[i] = s.a + (s.kind() == kGiven ? 2 * (size_t)L : s.a_limbs()) * ctx->n;
+        src.mul[i] = s.kind() == kGiven ? nullptr : s.b + (size_t)s.b_limbs() * ctx->n;
         src.mult[i] = s.mult;
     }
     return src;

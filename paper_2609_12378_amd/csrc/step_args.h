@@ -6,17 +6,25 @@
 namespace steps {
 
 // What a step's product is: none, of ciphertexts, of a ciphertext and a plaintext, a sum of products that is there
-enum : uint8_t { kNone = 0, kProduct = 1, kPlain = 2, kGiven = 3 };
+enum : uint32_t { kNone = 0, kProduct = 1, kPlain = 2, kGiven = 3 };
 
-// A step's operands as they travel in a launch's arguments.
+// A step's operands as they travel in a launch's arguments.  Counts share words: a byte of the arguments is not a scalar
+// load, and waiting for it is waiting for every load before it.
 struct Operands {
     const uint64_t *a, *b, *z[kStepTerms];       // a: the sum [3][L][N] of a kGiven step
     uint64_t *out;
     int64_t k[kStepTerms + 1];                   // the terms' integers, then the constant's
-    uint8_t sh[kStepTerms + 1], limbs[kStepTerms], polys[kStepTerms];
-    uint8_t n, a_limbs, b_limbs, kind;
-    int8_t mult;
-    __host__ __device__ bool switched() const { return kind == kProduct || kind == kGiven; }
+    uint32_t term[kStepTerms + 1];               // their shifts, limbs and polynomials
+    uint32_t info;                               // terms, kind, limbs of a and of b
+    int32_t mult;
+    __host__ __device__ uint32_t n() const { return info & 0xff; }
+    __host__ __device__ uint32_t kind() const { return info >> 8 & 0xff; }
+    __host__ __device__ uint32_t a_limbs() const { return info >> 16 & 0xff; }
+    __host__ __device__ uint32_t b_limbs() const { return info >> 24; }
+    __host__ __device__ bool switched() const { return kind() == kProduct || kind() == kGiven; }
+    __device__ uint32_t sh(uint32_t i) const { return term[i] & 0xff; }
+    __device__ uint32_t limbs(uint32_t i) const { return term[i] >> 8 & 0xff; }
+    __device__ bool two(uint32_t i) const { return term[i] >> 16 == 2; }
 };
 struct Batch {
     Operands s[kStepBatch];

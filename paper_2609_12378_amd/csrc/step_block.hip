@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256) void k_step_sums(Batch bt, const uint64_t *dig
     const Operands &s = bt.s[z];
     const bool q_row = row < d.L, sw = s.switched();
     if (!sw && !q_row) return;
-    const uint32_t prime = d.prime(row), kind = q_row ? s.kind : kNone;
+    const uint32_t prime = d.prime(row), kind = q_row ? s.kind() : kNone;
     const A ar(mods[prime]);
     const size_t at = ((size_t)row << d.log_n) + pos, dstride = (size_t)d.ext << d.log_n,
                  kstride = (size_t)d.key_rows << d.log_n;
@@ -35,9 +35,9 @@ __global__ __launch_bounds__(256) void k_step_sums(Batch bt, const uint64_t *dig
         w[1] = s.a[at + ((size_t)d.L << d.log_n)];
     } else if (kind != kNone) {
         w[0] = s.a[at];
-        w[1] = s.a[at + ((size_t)s.a_limbs << d.log_n)];
+        w[1] = s.a[at + ((size_t)s.a_limbs() << d.log_n)];
         w[2] = s.b[at];
-        if (kind == kProduct) w[3] = s.b[at + ((size_t)s.b_limbs << d.log_n)];
+        if (kind == kProduct) w[3] = s.b[at + ((size_t)s.b_limbs() << d.log_n)];
     }
     if constexpr (ND > 0) {
         if (sw) {
@@ -52,11 +52,11 @@ __global__ __launch_bounds__(256) void k_step_sums(Batch bt, const uint64_t *dig
     double u0 = 0.0, u1 = 0.0;
     if (q_row) {
         // linear terms: a product at most 0.875 q, reduced every four
-        for (uint32_t i = 0; i < s.n; i++) {
-            const double k = int_mod(s.k[i], s.sh[i], ar);
+        for (uint32_t i = 0; i < s.n(); i++) {
+            const double k = int_mod(s.k[i], s.sh(i), ar);
             const uint64_t *zp = s.z[i] + at;
             u0 += ar.mul(A::from_u64(zp[0]), k);
-            if (s.polys[i] == 2) u1 += ar.mul(A::from_u64(zp[(size_t)s.limbs[i] << d.log_n]), k);
+            if (s.two(i)) u1 += ar.mul(A::from_u64(zp[(size_t)s.limbs(i) << d.log_n]), k);
             if ((i & 3) == 3) {
                 u0 = ar.red(u0);
                 u1 = ar.red(u1);
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void k_step_sums(Batch bt, const uint64_t *dig
         }
         if (s.k[kStepTerms]) {   // the constant c as c q_l, which the division leaves as c
             const double ql = ar.red((double)mods[d.L - 1].qd);
-            u0 += ar.mul(int_mod(s.k[kStepTerms], s.sh[kStepTerms], ar), ql < 0.0 ? ql + ar.q : ql);
+            u0 += ar.mul(int_mod(s.k[kStepTerms], s.sh(kStepTerms), ar), ql < 0.0 ? ql + ar.q : ql);
         }
         const double w0 = A::from_u64(w[0]), w1 = A::from_u64(w[1]), w2 = A::from_u64(w[2]), m = s.mult;
         if (kind == kGiven) {

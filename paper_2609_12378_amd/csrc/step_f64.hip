@@ -9,6 +9,7 @@
 //   4. k_step_fin8    the row passes of that and of the digits, u on the rows below q_l, out = (u - NTT(x)) (P q_l)^-1.
 // Steps without a product of ciphertexts have no digits and no rows P: u = (d0, d1), divided by q_l.
 #include <algorithm>
+#include <type_traits>
 
 #include "ops.h"
 #include "step_args.h"
@@ -28,8 +29,8 @@ struct RowPass {
 
 // u at the 8 positions of a thread, both components, |u| <= q/2 + 1.  Q: the row is one of the q limbs (the P rows have
 // no d0, d1).  The digits' rows come after their column pass and end their transforms here: a relinearisation reads each
-// once, so they need not be written.  A digit's own row is d2.  In units of q: a digit below 2.6, its product with a key
-// below 1.5, four of them and what is left of those before, below 7.
+// once, so they need not be written.  A digit's own row is d2 and is taken first.  In units of q: a digit below 2.6, its
+// product with a key below 1.5, four of them and what is left of those before, below 7.
 template <bool Q>
 __device__ __forceinline__ void step8(const Operands &s, const uint64_t *dig, const uint64_t *key0, const Dims &d,
                                       uint32_t row, double pq, const A &ar, const A &top, const Positions &ps,
@@ -37,28 +38,30 @@ __device__ __forceinline__ void step8(const Operands &s, const uint64_t *dig, co
 {
     const size_t rw = (size_t)row << d.log_n;
     const bool sw = s.switched();
-    const uint32_t kind = Q ? s.kind : kNone, own = Q ? row / d.alpha : ~0u;
-    double x[kE8], next[kE8], d2[kE8];
+    const uint32_t kind = Q ? s.kind() : kNone, own = Q ? row / d.alpha : ~0u;
+    const size_t kstride = (size_t)d.key_rows << d.log_n;
+    const uint64_t *key = key0 + ((size_t)d.prime(row) << d.log_n);
+    double x[kE8], next[kE8];
     auto ask = [&](uint32_t i) {
-        if (!sw || i == own) return;
         const uint64_t *p = dig + ((size_t)i * d.ext << d.log_n) + rw + (size_t)h * 256;
 #pragma unroll
         for (int e = 0; e < kE8; e++) next[e] = A::from_raw(nttc::ld_stream(p + nttc::u8<0>(rp.t, e)));
     };
-    ask(0);
+    const uint32_t first = own == 0 ? 1 : 0;
+    if (sw && first < d.nd) ask(first);
 #pragma unroll
     for (int e = 0; e < kE8; e++) u[0][e] = u[1][e] = 0.0;
     if constexpr (Q) {
         // linear terms: a product at most 0.875 q, reduced every four
-        for (uint32_t i = 0; i < s.n; i++) {
-            const double k = int_mod(s.k[i], s.sh[i], ar);
+        for (uint32_t i = 0; i < s.n(); i++) {
+            const double k = int_mod(s.k[i], s.sh(i), ar);
             const uint64_t *z = s.z[i] + rw;
             Pair v[2][kE8 / 2];
-            const bool two = s.polys[i] == 2;
+            const bool two = s.two(i);
 #pragma unroll
             for (int e = 0; e < kE8; e += 2) v[0][e / 2] = ld2(z + ps.pos(e));
             if (two) {
-                const uint64_t *z1 = z + ((size_t)s.limbs[i] << d.log_n);
+                const uint64_t *z1 = z + ((size_t)s.limbs(i) << d.log_n);
 #pragma unroll
                 for (int e = 0; e < kE8; e += 2) v[1][e / 2] = ld2(z1 + ps.pos(e));
             }
@@ -82,66 +85,79 @@ __device__ __forceinline__ void step8(const Operands &s, const uint64_t *dig, co
         // the constant c as c q_l, which the division leaves as c
         if (s.k[kStepTerms]) {
             const double ql = ar.red(top.q);
-            const double c = ar.mul(int_mod(s.k[kStepTerms], s.sh[kStepTerms], ar), ql < 0.0 ? ql + ar.q : ql);
+            const double c = ar.mul(int_mod(s.k[kStepTerms], s.sh(kStepTerms), ar), ql < 0.0 ? ql + ar.q : ql);
 #pragma unroll
             for (int e = 0; e < kE8; e++) u[0][e] += c;
         }
-        if (kind != kNone) {
-            // the product's operands (a0, a1, b0, b1; a0, a1, plaintext; d0, d1, d2)
-            const uint64_t *w0 = s.a + rw, *w1, *w2 = s.b + rw, *w3 = w2;
-            if (kind == kGiven) {
-                w1 = w0 + ((size_t)d.L << d.log_n);
-                w2 = w1 + ((size_t)d.L << d.log_n);
-            } else {
-                w1 = w0 + ((size_t)s.a_limbs << d.log_n);
-                if (kind == kProduct) w3 = w2 + ((size_t)s.b_limbs << d.log_n);
-            }
-            const double mult = s.mult;
-            Pair w[4][kE8 / 2];
+        // the product's operands (a0, a1, b0, b1; a0, a1, plaintext; d0, d1, d2), four positions at a time, and the key's
+        // words for d2
+        const double mult = s.mult;
+        const uint64_t *kb = key + 2 * own * kstride, *ka = kb + kstride;
+        auto finish = [&](auto is) {
+            constexpr uint32_t KIND = decltype(is)::value;
+            constexpr bool SW = KIND == kProduct || KIND == kGiven;
+            const uint64_t *w0 = s.a + rw, *w1 = w0 + ((size_t)(KIND == kGiven ? d.L : s.a_limbs()) << d.log_n),
+                           *w2 = KIND == kGiven ? w1 + ((size_t)d.L << d.log_n) : s.b + rw,
+                           *w3 = w2 + ((size_t)s.b_limbs() << d.log_n);
 #pragma unroll
-            for (int e = 0; e < kE8; e += 2) {
-                w[0][e / 2] = ld2(w0 + ps.pos(e));
-                w[1][e / 2] = ld2(w1 + ps.pos(e));
-                w[2][e / 2] = ld2(w2 + ps.pos(e));
-                if (kind == kProduct) w[3][e / 2] = ld2(w3 + ps.pos(e));
-            }
+            for (int e0 = 0; e0 < kE8; e0 += 4) {
+                Pair w[4][2], b[2], a[2];
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int e = 0; e < kE8; e++) {
-                auto word = [&](int j) { return A::from_u64(e & 1 ? w[j][e / 2].y : w[j][e / 2].x); };
-                if (kind == kProduct) {
-                    const double a0 = word(0), a1 = word(1), b0 = word(2), b1 = word(3);
-                    ProductSum p1;
-                    p1.add(a0, b1);
-                    p1.add(a1, b0);
-                    u[0][e] += mult * ar.mul(a0, b0);
-                    u[1][e] += mult * p1.value(ar);
-                    d2[e] = ar.red(mult * ar.mul(a1, b1));
-                } else if (kind == kPlain) {
-                    u[0][e] += ar.mul(word(0), word(2));
-                    u[1][e] += ar.mul(word(1), word(2));
-                } else {
-                    u[0][e] += word(0);
-                    u[1][e] += word(1);
-                    d2[e] = word(2);
+                for (int p = 0; p < 2; p++) {
+                    const uint32_t at = ps.pos(e0 + 2 * p);
+                    if constexpr (KIND != kNone) {
+                        w[0][p] = ld2(w0 + at);
+                        w[1][p] = ld2(w1 + at);
+                        w[2][p] = ld2(w2 + at);
+                    }
+                    if constexpr (KIND == kProduct) w[3][p] = ld2(w3 + at);
+                    if constexpr (SW) {
+                        b[p] = ld2(kb + at);
+                        a[p] = ld2(ka + at);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int o = 0; o < 4; o++) {
+                    const int e = e0 + o;
+                    auto get = [&](const Pair &v) { return A::from_u64(o & 1 ? v.y : v.x); };
+                    auto word = [&](int j) { return get(w[j][o / 2]); };
+                    double d2 = 0.0;
+                    if constexpr (KIND == kProduct) {
+                        const double a0 = word(0), a1 = word(1), b0 = word(2), b1 = word(3);
+                        ProductSum p1;
+                        p1.add(a0, b1);
+                        p1.add(a1, b0);
+                        u[0][e] += mult * ar.mul(a0, b0);
+                        u[1][e] += mult * p1.value(ar);
+                        d2 = ar.red(mult * ar.mul(a1, b1));
+                    } else if constexpr (KIND == kPlain) {
+                        u[0][e] += ar.mul(word(0), word(2));
+                        u[1][e] += ar.mul(word(1), word(2));
+                    } else if constexpr (KIND == kGiven) {
+                        u[0][e] += word(0);
+                        u[1][e] += word(1);
+                        d2 = word(2);
+                    }
+                    u[0][e] = ar.red(u[0][e]);
+                    u[1][e] = ar.red(u[1][e]);
+                    if constexpr (SW) {
+                        u[0][e] = ar.red(ar.mul(u[0][e], pq) + ar.mul(d2, get(b[o / 2])));
+                        u[1][e] = ar.red(ar.mul(u[1][e], pq) + ar.mul(d2, get(a[o / 2])));
+                    }
                 }
             }
-        }
-#pragma unroll
-        for (int e = 0; e < kE8; e++) {
-            u[0][e] = ar.red(u[0][e]);
-            u[1][e] = ar.red(u[1][e]);
-        }
-        if (!sw) return;
-#pragma unroll
-        for (int e = 0; e < kE8; e++) {
-            u[0][e] = ar.mul(u[0][e], pq);
-            u[1][e] = ar.mul(u[1][e], pq);
-        }
+        };
+        if (kind == kProduct) finish(std::integral_constant<uint32_t, kProduct>());
+        else if (kind == kNone) finish(std::integral_constant<uint32_t, kNone>());
+        else if (kind == kPlain) finish(std::integral_constant<uint32_t, kPlain>());
+        else finish(std::integral_constant<uint32_t, kGiven>());
     }
-    const size_t kstride = (size_t)d.key_rows << d.log_n;
-    const uint64_t *key = key0 + ((size_t)d.prime(row) << d.log_n);
+    if (!sw) return;
 #pragma unroll 1
-    for (uint32_t i = 0; i < d.nd; i++) {
+    for (uint32_t i = first, n = 0; i < d.nd; n++) {
+        const uint32_t j = i + 1 == own ? i + 2 : i + 1;   // the next digit
         Pair kb[kE8 / 2], ka[kE8 / 2];
         uint32_t t = rp.t;
         asm volatile("" : "+v"(t));   // the twiddles' reads stay in the loop: held across it they cost a wave a SIMD
@@ -153,28 +169,24 @@ __device__ __forceinline__ void step8(const Operands &s, const uint64_t *dig, co
         }
 #pragma unroll
         for (int e = 0; e < kE8; e++) x[e] = next[e];
-        if (i + 1 < d.nd) ask(i + 1);
+        if (j < d.nd) ask(j);
         __builtin_amdgcn_sched_barrier(0);
-        if (Q && i == own) {
-#pragma unroll
-            for (int e = 0; e < kE8; e++) x[e] = d2[e];
-        } else {
-            nttc::fwd8_256<nttc::kRowMask8>(x, rp.tws, rp.tr, t, ar);
-            swap_1_6(x);
-        }
+        nttc::fwd8_256<nttc::kRowMask8>(x, rp.tws, rp.tr, t, ar);
+        swap_1_6(x);
 #pragma unroll
         for (int e = 0; e < kE8; e++) {
             const Pair &b = kb[e / 2], &a = ka[e / 2];
             u[0][e] += ar.mul(x[e], A::from_u64(e & 1 ? b.y : b.x));
             u[1][e] += ar.mul(x[e], A::from_u64(e & 1 ? a.y : a.x));
         }
-        if ((i & 3) == 3 || i + 1 == d.nd) {
+        if ((n & 3) == 3 || j >= d.nd) {
 #pragma unroll
             for (int e = 0; e < kE8; e++) {
                 u[0][e] = ar.red(u[0][e]);
                 u[1][e] = ar.red(u[1][e]);
             }
         }
+        i = j;
     }
 }
 
@@ -185,7 +197,7 @@ __global__ __launch_bounds__(64) void k_step_intt8(Batch bt, const uint64_t *dig
                                                    const ModQ *__restrict__ mods, const double *__restrict__ twf,
                                                    const double *__restrict__ itwf)
 {
-    __shared__ double tws[2][257], twd[2][257];
+    __shared__ double tws[2][257];
     __shared__ double tr[2][nttc::kTr8];
     const uint32_t bpl = 1u << (d.log_n - 9);
     uint32_t z, tile;
@@ -195,15 +207,17 @@ __global__ __launch_bounds__(64) void k_step_intt8(Batch bt, const uint64_t *dig
     if (s && !o.switched()) return;
     const A ar(mods[prime]);
     const uint32_t sub = threadIdx.x >> 5, t = threadIdx.x & 31, h = blk * 2 + sub;
-    nttc::stage_twiddles8(tws[sub], itwf + ((size_t)prime << d.log_n), (1u << (d.log_n - 8)) + h, t, 32);
-    nttc::stage_twiddles8(twd[sub], twf + ((size_t)prime << d.log_n), (1u << (d.log_n - 8)) + h, t, 32);
+    nttc::stage_twiddles8(tws[sub], twf + ((size_t)prime << d.log_n), (1u << (d.log_n - 8)) + h, t, 32);
     const Positions ps(h, t, d.log_n);
-    const RowPass rp{twd[sub], tr[sub], t};
+    const RowPass rp{tws[sub], tr[sub], t};
     __syncthreads();
     const uint64_t *mine = dig + ((size_t)z * d.nd * d.ext << d.log_n);
     double u[2][kE8];
     if (s) step8<false>(o, mine, rlk, d, row, 0.0, ar, ar, ps, rp, h, u);
     else step8<true>(o, mine, rlk, d, row, (double)pmodq[row].x, ar, ar, ps, rp, h, u);
+    __syncthreads();
+    nttc::stage_twiddles8(tws[sub], itwf + ((size_t)prime << d.log_n), (1u << (d.log_n - 8)) + h, t, 32);
+    __syncthreads();
 #pragma unroll
     for (int k = 0; k < 2; k++) {
         swap_1_6(u[k]);
@@ -284,7 +298,7 @@ ckks_status step_f64(ckks_ctx *ctx, uint32_t L, const Batch &b, uint32_t n, uint
     CK_TRY(ctx_conv(ctx, (int)level, -1, &cd));
     const Quot qt{cd->d_qhat_inv_f, cd->d_qhat_mod_f, ctx->d_pinv, ctx->d_qlinv + (size_t)level * ctx->n_q, ctx->d_pmodq};
     double terms = 0;
-    for (uint32_t i = 0; i < n; i++) terms += 2.0 * b.s[i].n + (b.s[i].kind == kProduct ? 4 : b.s[i].kind ? 3 : 0);
+    for (uint32_t i = 0; i < n; i++) terms += 2.0 * b.s[i].n() + (b.s[i].kind() == kProduct ? 4 : b.s[i].kind() ? 3 : 0);
     const double rows1 = (double)n_sw * d.K * N;
     prof_begin(ctx, K_KEYIP, 8.0 * (rows1 * (d.nd + 2.0) + N * (terms + n_sw * d.nd + 2.0 * n)),
                rows1 * (4.0 * d.nd * 4 + 2 * 4 * kOpsButterflyF64));
