@@ -134,28 +134,71 @@ struct Squares {
     const uint64_t *a[kStepBatch];
     uint32_t n, limbs;
 };
-// d (+)= sum_j (a0^2, 2 a0 a1, a1^2)
+// d (+)= sum_j (a0^2, 2 a0 a1, a1^2), two positions a thread.  F64 (primes below 2^50): four ciphertexts' products under
+// one quotient, their loads issued together (16 ciphertexts of 24 limbs at N = 2^16 in exact products 124 us).
+template <bool F64>
 __global__ __launch_bounds__(kThreads) void k_step_squares(Squares sq, uint64_t *d, bool accumulate, uint32_t L,
                                                            uint32_t log_n, const ModQ *__restrict__ mods)
 {
-    const uint32_t row = blockIdx.y, pos = blockIdx.x * kThreads + threadIdx.x;
-    if (pos >> log_n) return;
+    const uint32_t row = blockIdx.y, col = 2 * (blockIdx.x * kThreads + threadIdx.x);
+    if (col >> log_n) return;
     const ModQ m = mods[row];
-    const size_t at = ((size_t)row << log_n) + pos, half = (size_t)L << log_n;
-    uint64_t s0 = 0, s1 = 0, s2 = 0;
-    if (accumulate) s0 = d[at], s1 = d[half + at], s2 = d[2 * half + at];
-    for (uint32_t j = 0; j < sq.n; j++) {
-        const uint64_t a0 = sq.a[j][at], a1 = sq.a[j][at + ((size_t)sq.limbs << log_n)];
-        s0 = addmod(s0, mulmod(a0, a0, m), m.q);
-        s1 = addmod(s1, mulmod(csub(2 * a0, m.q), a1, m), m.q);
-        s2 = addmod(s2, mulmod(a1, a1, m), m.q);
+    const size_t at = ((size_t)row << log_n) + col, half = (size_t)L << log_n, next = (size_t)sq.limbs << log_n;
+    Pair r[3] = {};
+    if (accumulate)
+#pragma unroll
+        for (int k = 0; k < 3; k++) r[k] = ld2(d + k * half + at);
+    if constexpr (F64) {
+        const A ar(m);
+        double t[3][2];
+#pragma unroll
+        for (int k = 0; k < 3; k++) {
+            t[k][0] = A::from_u64(r[k].x);
+            t[k][1] = A::from_u64(r[k].y);
+        }
+        for (uint32_t j0 = 0; j0 < sq.n; j0 += 4) {
+            Pair a0[4], a1[4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const uint64_t *p = sq.a[min(j0 + j, sq.n - 1)] + at;
+                a0[j] = ld2(p);
+                a1[j] = ld2(p + next);
+            }
+            ProductSum s[3][2];
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                if (j0 + j >= sq.n) break;
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    const double x = A::from_u64(e ? a0[j].y : a0[j].x), y = A::from_u64(e ? a1[j].y : a1[j].x);
+                    s[0][e].add(x, x);
+                    s[1][e].add(x, y);
+                    s[2][e].add(y, y);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                t[0][e] = ar.red(t[0][e] + s[0][e].value(ar));
+                t[1][e] = ar.red(t[1][e] + 2.0 * s[1][e].value(ar));
+                t[2][e] = ar.red(t[2][e] + s[2][e].value(ar));
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 3; k++) r[k] = Pair{ar.to_canon(t[k][0]), ar.to_canon(t[k][1])};
+    } else {
+        for (uint32_t j = 0; j < sq.n; j++) {
+            const Pair a0 = ld2(sq.a[j] + at), a1 = ld2(sq.a[j] + at + next);
+            r[0].x = addmod(r[0].x, mulmod(a0.x, a0.x, m), m.q);
+            r[0].y = addmod(r[0].y, mulmod(a0.y, a0.y, m), m.q);
+            r[1].x = addmod(r[1].x, mulmod(csub(2 * a0.x, m.q), a1.x, m), m.q);
+            r[1].y = addmod(r[1].y, mulmod(csub(2 * a0.y, m.q), a1.y, m), m.q);
+            r[2].x = addmod(r[2].x, mulmod(a1.x, a1.x, m), m.q);
+            r[2].y = addmod(r[2].y, mulmod(a1.y, a1.y, m), m.q);
+        }
     }
-    d[at] = s0;
-    d[half + at] = s1;
-    d[2 * half + at] = s2;
+#pragma unroll
+    for (int k = 0; k < 3; k++) *(Pair *)(d + k * half + at) = r[k];
 }
-
-dim3 grid_of(const ckks_ctx *ctx, uint32_t rows, uint32_t z) { return dim3((ctx->n + kThreads - 1) / kThreads, rows, z); }
 
 Operands operands(const Step &s)
 {
@@ -294,8 +337,13 @@ ckks_status step_squares(ckks_ctx *ctx, uint32_t L, const std::vector<const uint
         sq.limbs = limbs;
         for (uint32_t j = 0; j < sq.n; j++) sq.a[j] = a[j0 + j];
         prof_begin(ctx, K_ELEM, 8.0 * L * ctx->n * (2.0 * sq.n + (j0 ? 6 : 3)));
-        hipLaunchKernelGGL(k_step_squares, grid_of(ctx, L, 1), dim3(kThreads), 0, ctx->stream, sq, d, j0 > 0, L, ctx->log_n,
-                           ctx->d_mod);
+        const dim3 grid((ctx->n + 2 * kThreads - 1) / (2 * kThreads), L);
+        if (ntt_uses_f64(ctx, L))
+            hipLaunchKernelGGL(k_step_squares<true>, grid, dim3(kThreads), 0, ctx->stream, sq, d, j0 > 0, L, ctx->log_n,
+                               ctx->d_mod);
+        else
+            hipLaunchKernelGGL(k_step_squares<false>, grid, dim3(kThreads), 0, ctx->stream, sq, d, j0 > 0, L, ctx->log_n,
+                               ctx->d_mod);
         prof_end(ctx, K_ELEM);
         HIP_TRY(hipGetLastError());
     }
