@@ -180,8 +180,8 @@ ckks_status giant_steps(ckks_ctx *ctx, const uint64_t *acc, uint64_t *tot, uint6
     const uint32_t L = level + 1;
     const size_t ctw = 2 * (size_t)L * ctx->n;
     const uint32_t first = g == 0 ? 1 : 0;
-    if (first) HIP_TRY(hipMemcpyAsync(tot, acc, jc * ctw * 8, hipMemcpyDeviceToDevice, ctx->stream));
     const uint32_t count = (gc - first) * jc;
+    if (first && (lazy || !count)) HIP_TRY(hipMemcpyAsync(tot, acc, jc * ctw * 8, hipMemcpyDeviceToDevice, ctx->stream));
     if (!count) return CKKS_OK;
     std::vector<int32_t> steps(count);
     std::vector<const uint64_t *> keys(count);
@@ -196,9 +196,7 @@ ckks_status giant_steps(ckks_ctx *ctx, const uint64_t *acc, uint64_t *tot, uint6
     if (lazy)
         return rotate_each_lazy(ctx, cs, ctw, count, level, steps.data(), keys.data(), uacc, jc, g + first > 1, work);
     CK_TRY(rotate_each(ctx, cs, ctw, count, level, steps.data(), keys.data(), outs.data(), work));
-    for (uint32_t r = 0; r < count; r += jc)
-        CK_TRY(launch_binary(ctx, tot, tot, rot + r * ctw, jc * 2 * L, limb_range(0, L), EW_ADD));
-    return CKKS_OK;
+    return launch_sum_cts(ctx, tot, first ? acc : tot, rot, gc - first, jc * ctw, L, jc);
 }
 
 ckks_status rescale_many(ckks_ctx *ctx, const uint64_t *c, uint32_t count, uint32_t l, uint64_t *out,

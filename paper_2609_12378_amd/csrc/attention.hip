@@ -215,20 +215,6 @@ __global__ __launch_bounds__(kThreads) void k_attn_corr(uint64_t *out, const uin
     }
 }
 
-// out[w] = (accumulate ? out[w] : 0) + sum_{r < count} src[r * stride + w] mod q, w < 2 L N (one ciphertext).
-__global__ __launch_bounds__(kThreads) void k_sum_cts(uint64_t *out, const uint64_t *__restrict__ src, uint32_t count,
-                                                      size_t stride, uint32_t L, uint32_t log_n, int accumulate,
-                                                      const ModQ *__restrict__ mods)
-{
-    const size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x;
-    const size_t total = (size_t)2 * L << log_n;
-    if (i >= total) return;
-    const uint64_t q = mods[(i >> log_n) % L].q;
-    uint64_t s = accumulate ? out[i] : 0;
-    for (uint32_t r = 0; r < count; r++) s = addmod(s, src[(size_t)r * stride + i], q);
-    out[i] = s;
-}
-
 // d ([3][L][N]) = sum_{r < count} E_r x C_r: d0 += e0 c0, d1 += e0 c1 + e1 c0, d2 += e1 c1, the sums held in 128
 // bits and reduced once: the attention calls take primes below 2^50 only, so each product is below 2^100 and
 // count <= 2^16 (2^17 products in d1) keeps every sum below 2^117.  E_r at E + r * 2 L N ([2][L][N]); C_r at
@@ -329,19 +315,6 @@ ckks_status launch_corr(ckks_ctx *ctx, uint64_t *out, const uint64_t *x, uint32_
     }
 #undef CK_CORR
     prof_end(ctx, K_ATTN_CORR);
-    HIP_TRY(hipGetLastError());
-    return CKKS_OK;
-}
-
-ckks_status launch_sum_cts(ckks_ctx *ctx, uint64_t *out, const uint64_t *src, uint32_t count, size_t stride,
-                           uint32_t L, bool accumulate)
-{
-    if (!count && accumulate) return CKKS_OK;
-    const size_t total = (size_t)2 * L * ctx->n;
-    prof_begin(ctx, K_ELEM, 8.0 * total * (count + 1 + (accumulate ? 1 : 0)));
-    hipLaunchKernelGGL(k_sum_cts, grid_of(total), dim3(kThreads), 0, ctx->stream, out, src, count, stride, L,
-                       ctx->log_n, (int)accumulate, ctx->d_mod);
-    prof_end(ctx, K_ELEM);
     HIP_TRY(hipGetLastError());
     return CKKS_OK;
 }
@@ -609,13 +582,13 @@ extern "C" ckks_status ckks_attention_scores(ckks_ctx *ctx, const ckks_buf *q, u
             }
             CK_TRY(ks_moddown(ctx, uacc, 2, level, Ub, 1, Ub + (size_t)L * N, tot, work));
         } else {
-            CK_TRY(launch_sum_cts(ctx, tot, Ub, 1, ctw, L, false));
+            CK_TRY(launch_sum_cts(ctx, tot, nullptr, Ub, 1, ctw, L, 1));
             for (uint32_t k0 = 1; k0 < hd; k0 += ss.Jt) {
                 const uint32_t cnt = std::min(ss.Jt, hd - k0);
                 for (uint32_t r = 0; r < cnt; r++) outs[r] = rot + (size_t)r * ctw;
                 CK_TRY(rotate_each(ctx, Ub + (size_t)k0 * ctw, ctw, cnt, level, osteps.data() + (k0 - 1),
                                    okeys.data() + (k0 - 1), outs.data(), work));
-                CK_TRY(launch_sum_cts(ctx, tot, rot, cnt, ctw, L, true));
+                CK_TRY(launch_sum_cts(ctx, tot, tot, rot, cnt, ctw, L, 1));
             }
         }
         // 4. the two rescales (by q_level, the masks' scale, and by q_(level-1))

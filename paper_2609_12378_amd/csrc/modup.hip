@@ -82,8 +82,9 @@ __global__ __launch_bounds__(128) void k_up_row(uint64_t *dst, Src c1, Blocks bl
     const uint32_t n1 = 1u << (bl.log_n - 8), per = n1 / 8;
     const uint32_t row = blockIdx.x / per, r = row / bl.L, l = row % bl.L;
     const uint32_t sub = threadIdx.x >> 4, t = threadIdx.x & 15u, h = (blockIdx.x % per) * 8 + sub;
-    const A ar(mods[l]);
-    const double *tw = itwf + ((size_t)l << bl.log_n);
+    const uint32_t prime = bl.src_prime(l);
+    const A ar(mods[prime]);
+    const double *tw = itwf + ((size_t)prime << bl.log_n);
     uint64_t *out = dst + bl.at(r, l) + (size_t)h * 256;
     double x[kE];
     source_row(x, c1, r, ((size_t)l << bl.log_n) + (size_t)h * 256, t, ar);
@@ -582,19 +583,28 @@ ckks_status up_modup_cols(ckks_ctx *ctx, const PolyProd &c, uint32_t count, uint
     return modup_of(ctx, c, nullptr, count, level, digits, false);
 }
 
-ckks_status up_moddown(ckks_ctx *ctx, uint64_t *up, uint32_t polys, uint32_t level, uint64_t *cw)
+ckks_status up_moddown(ckks_ctx *ctx, uint64_t *up, uint32_t polys, uint32_t level, uint64_t *cw, uint32_t stride)
 {
     const ConvDev *cd;
     CK_TRY(ctx_conv(ctx, (int)level, -1, &cd));
     Blocks bl{};
     bl.nd = 1;
-    bl.alpha = bl.L = bl.ext = ctx->n_p;
+    bl.alpha = bl.L = ctx->n_p;
+    bl.ext = stride ? stride : ctx->n_p;
     bl.n_q = ctx->n_q;
     bl.log_n = ctx->log_n;
     bl.down = true;
     bl.out_rows = level + 1;
     bl.inv[0] = cd->d_qhat_inv_f;
     bl.mod[0] = cd->d_qhat_mod_f;
+    if (stride) {
+        const double res = (double)polys * ctx->n_p * ctx->n;
+        prof_begin(ctx, K_NTT_INV_ROW, 16.0 * res, res * kOpsButterflyF64 * 4);
+        hipLaunchKernelGGL(k_up_row<PolySrc>, dim3((polys * ctx->n_p) << (ctx->log_n - 11)), dim3(128), 0, ctx->stream, up,
+                           PolySrc{up, (size_t)stride * ctx->n, {}}, bl, ctx->d_mod, ctx->d_itwf);
+        prof_end(ctx, K_NTT_INV_ROW);
+        HIP_TRY(hipGetLastError());
+    }
     if (!conv_cols(ctx, ctx->n_p, polys, bl)) CK_TRY(launch_col_digits(ctx, up, polys, bl));
     CK_TRY(launch_blocks_conv(ctx, cw, up, polys, bl, ctx->n_p, level + 1, ctx->n_p == 8));
     if (!conv_fused(ctx, ctx->n_p) && !conv_col(ctx, bl, polys, ctx->n_p, level + 1))

@@ -60,6 +60,9 @@ ckks_status ks_modup_staged(ckks_ctx *ctx, uint64_t *c1, uint32_t count, uint32_
 // out: [polys][level+1][N]; work: [polys][level+1][N]
 ckks_status ks_moddown(ckks_ctx *ctx, uint64_t *u, uint32_t polys, uint32_t level, const uint64_t *add0,
                        uint32_t add0_g, const uint64_t *add1, uint64_t *out, uint64_t *work);
+// out = base (null: zero) + sum_{r < count} src_r, each cts ciphertexts [2][L][N], src_r at src + r * stride; out may be base
+ckks_status launch_sum_cts(ckks_ctx *ctx, uint64_t *out, const uint64_t *base, const uint64_t *src, uint32_t count,
+                           size_t stride, uint32_t L, uint32_t cts);
 // scratch words for rotations at `level` processed `batch` at a time (see rotate_core)
 size_t ks_scratch_words(const ckks_ctx *ctx, uint32_t level, uint32_t batch, uint32_t n_ct = 1);
 // rotations per batched launch for `count` requested rotations
@@ -121,8 +124,9 @@ ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t 
 struct PolyProd;
 ckks_status up_modup_cols(ckks_ctx *ctx, const PolyProd &c, uint32_t count, uint32_t level, uint64_t *digits);
 // up: [polys][n_p][N] rows modulo P after the row pass of their inverse transform (raw doubles below 2q): finishes it,
-// converts to the level's q limbs and runs the first forward pass into cw ([polys][level+1][N] raw doubles)
-ckks_status up_moddown(ckks_ctx *ctx, uint64_t *up, uint32_t polys, uint32_t level, uint64_t *cw);
+// converts to the level's q limbs and runs the first forward pass into cw ([polys][level+1][N] raw doubles).  With a
+// stride (rows from one polynomial to the next): of canonical NTT-domain rows, that row pass first
+ckks_status up_moddown(ckks_ctx *ctx, uint64_t *up, uint32_t polys, uint32_t level, uint64_t *cw, uint32_t stride = 0);
 
 // Whole rows per block (ring_block.hip): fp64 primes, N = 2^12 and 2^13, at 2^14 for launches of many rows.
 // the ring has them and the fp64 arithmetic is not switched off
