@@ -1157,7 +1157,7 @@ ckks_status ks_moddown(ckks_ctx *ctx, uint64_t *u, uint32_t polys, uint32_t leve
     if (s1 > 0 && s2 == 8 && polys % 2 == 0 && polys / 2 <= (uint32_t)kRotBatch && ntt_uses_f64(ctx, L) &&
         ntt_map_f64(ctx, pm) && up_conv_ok(ctx, cd)) {
         // a rotation batch's ModDown: the row pass of the P rows, their columns with the conversion, the quotient in the
-        // last row pass (two polynomials of 24 + 8 limbs at N = 2^16 72 -> 55 us)
+        // last row pass (two polynomials of 24 + 8 limbs at N = 2^16 76 -> 58 us)
         RotArgs ra{};
         ra.count = polys / 2;
         for (uint32_t r = 0; r < ra.count; r++) {

@@ -292,12 +292,14 @@ __device__ __forceinline__ void pack_digits(const uint64_t (&v)[4], uint32_t (&p
 }
 
 // x2 ([n_in][n1][xr, xw][2][L][N] canonical) -> Xd[a][l][kappa / 64][poly N + pos][kappa mod 64],
-// kappa = 2 (i n1 + b) + uv < kt (zeros from kt to kt_pad).  Block: (l, 64 columns, 64 kappa), staged through LDS.
+// kappa = 2 (i n1 + b) + uv < kt.  Block: (l, 64 columns, 64 kappa), staged through LDS.  Groups of 16 kappa from kt on
+// are left as they were: they are read against zero plaintext digits (32 kappa of 128, 10 limbs of N = 2^16: 306 us
+// with all written, so 273).
 __global__ __launch_bounds__(kThreads) void k_xdigits(const uint64_t *__restrict__ x2, int8_t *Xd, uint32_t L,
                                                       uint32_t log_n, uint32_t kt, uint32_t kt_pad)
 {
     __shared__ uint64_t tile[64][65];
-    const uint32_t cols = 2u << log_n, cblocks = cols / 64, kblocks = kt_pad / 64;
+    const uint32_t cols = 2u << log_n, cblocks = cols / 64, kblocks = (kt + 63) / 64;
     const uint32_t kb = blockIdx.x % kblocks, rest = blockIdx.x / kblocks;
     const uint32_t cb = rest % cblocks, l = rest / cblocks;
     const size_t n = (size_t)1 << log_n, ctw = 2 * (size_t)L * n;
@@ -320,6 +322,7 @@ __global__ __launch_bounds__(kThreads) void k_xdigits(const uint64_t *__restrict
     const size_t plane = (size_t)L * cols * kt_pad;
     static_assert(kThreads == 256, "64 columns x 4 groups of 16 kappa");
     const uint32_t cc = threadIdx.x >> 2, kq = (threadIdx.x & 3u) << 4;
+    if (k0 + kq >= kt) return;
     uint32_t w[8][4];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
@@ -331,7 +334,7 @@ __global__ __launch_bounds__(kThreads) void k_xdigits(const uint64_t *__restrict
 #pragma unroll
         for (int a = 0; a < kDig; a++) w[a][i] = packed[a];
     }
-    int8_t *dst = Xd + (((size_t)l * kblocks + kb) * cols + c0 + cc) * 64 + kq;
+    int8_t *dst = Xd + (((size_t)l * (kt_pad / 64) + kb) * cols + c0 + cc) * 64 + kq;
 #pragma unroll
     for (int a = 0; a < kDig; a++)
         *(uint4 *)(dst + (size_t)a * plane) = make_uint4(w[a][0], w[a][1], w[a][2], w[a][3]);
@@ -612,8 +615,8 @@ uint32_t mac_max_outputs() { return kMaxJtMfma; }
 
 ckks_status launch_xdigits(ckks_ctx *ctx, const uint64_t *x2, int8_t *Xd, uint32_t L, uint32_t kt, uint32_t kt_pad)
 {
-    const uint32_t blocks = L * (uint32_t)((2 * ctx->n) / 64) * (kt_pad / 64);
-    prof_begin(ctx, K_ELEM, 8.0 * kt * 2 * L * ctx->n + (double)kDig * kt_pad * 2 * L * ctx->n);
+    const uint32_t blocks = L * (uint32_t)((2 * ctx->n) / 64) * ((kt + 63) / 64);
+    prof_begin(ctx, K_ELEM, (8.0 * kt + (double)kDig * ((kt + 15) & ~15u)) * 2 * L * ctx->n);
     hipLaunchKernelGGL(k_xdigits, dim3(blocks), dim3(kThreads), 0, ctx->stream, x2, Xd, L, ctx->log_n, kt, kt_pad);
     prof_end(ctx, K_ELEM);
     HIP_TRY(hipGetLastError());
