@@ -109,6 +109,7 @@ extern "C" ckks_status ckks_linear_project_epilogue(ckks_ctx *ctx, const ckks_bu
         StepInt c{}, kb{}, kr{};
         ProjHook hook{};
         double left = to;
+        CK_TRY(check_scale(to, what, "gate's factor"));
         if (act) {
             double by;
             CK_TRY(poly_map(*act, top(L - 1), &by, &c, what));

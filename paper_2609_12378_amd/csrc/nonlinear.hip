@@ -43,7 +43,6 @@ ckks_status check_list(const ckks_ctx *ctx, const ckks_buf *b, uint32_t n, uint3
     return check_scale(b[0].scale, what, name);
 }
 
-
 ckks_status poly_map(const ckks_poly &p, double s1, double *by, StepInt *c, const char *what)
 {
     *by = 2.0 / (p.hi - p.lo) * s1;
@@ -316,6 +315,9 @@ ckks_status ckks_rms_norm(ckks_ctx *ctx, const ckks_buf *in, uint32_t count, con
         if (tm) sv = sv * mask->scale / top(L - 1);
         const double sx = weights ? S * weights[0].scale / top(m + 1) : S;
         const double last = S * top(m) / sx;
+        CK_TRY(check_scale(sv, what, "sum of squares"));
+        CK_TRY(check_scale(sx, what, "weighted input"));
+        CK_TRY(check_scale(last, what, "inverse root"));
         const double s1 = top(Lv - 1);
         double by;
         StepInt k, c, kr{};

@@ -1,0 +1,134 @@
+"""Polynomials, norms and the projection's epilogue at the edges of what they allow: residues at the ends of their ranges,
+buffers and keys that start at an odd word, operands that are one another, primes of 62 bits, scales that leave the doubles."""
+import math
+
+import numpy as np
+import pytest
+
+import nonlinear_common as nc
+from gpu_common import to_dev, to_host
+from rope_common import random_cts, random_keys
+from test_gpu_nonlinear import SCALE, norm_inputs, plaintexts, proj_keys, rlk_of, some_poly
+from test_gpu_rope import bufs, dev_keys, ring, same
+from test_gpu_rope_rules import odd_words
+from workloads import rng
+
+pytestmark = pytest.mark.gpu
+
+
+def extremes(ck, lead, primes, seed, mixed):
+    """Canonical residues that are q - 1 everywhere, or one of 0, 1, (q - 1) / 2, (q + 1) / 2 and q - 1."""
+    g = rng(seed, 3)
+    out = np.empty((*lead, len(primes), ck.n), dtype=np.uint64)
+    for i, q in enumerate(primes):
+        values = np.array([q - 1, 0, 1, q // 2, q // 2 + 1], dtype=np.uint64)
+        out[..., i, :] = values[g.integers(0, 5, (*lead, ck.n))] if mixed else values[0]
+    return out
+
+
+EXTREME = [((8, 9, 3, 3, 62), 2.0 ** 60), ((8, 9, 3, 3, 50), SCALE), ((12, 9, 3, 3, 50), SCALE), ((13, 9, 5, 2, 50), SCALE),
+           ((14, 9, 3, 3, 50), SCALE), ((10, 9, 9, 1, 59), 2.0 ** 58), ((12, 9, 1, 9, 50), SCALE)]
+
+
+@pytest.mark.parametrize("mixed", [False, True])
+@pytest.mark.parametrize("ring_args,scale", EXTREME, ids=str)
+def test_residues_at_the_ends_of_their_ranges(ring_args, scale, mixed):
+    """Every lazy sum at its largest: a polynomial of nine terms a step, a norm of five ciphertexts with a Newton step."""
+    ctx, ck = ring(*ring_args)
+    limbs, T = 9, ck.n // 32
+    make = lambda lead, primes, seed: extremes(ck, lead, primes, seed, mixed)  # noqa: E731
+    xs = [make((2,), ck.q[:limbs], 400 + i) for i in range(5)]
+    rlk = make((ck.dnum, 2), ck.primes, 410)
+    poly, inv = some_poly(13, 411), some_poly(3, 412, 0.5, 3.0)
+    got = ctx.poly_eval(bufs(xs[:2], scale), poly, to_dev(rlk))
+    for g, x in zip(got, xs):
+        same(g.data, nc.poly_eval(ck, x, scale, poly, rlk), "polynomial")
+    st = norm_inputs(ck, limbs, T, "fm", 1, None, None, 420)
+    keys = {s: make((ck.dnum, 2), ck.primes, 430 + s) for s in st["keys"]}
+    ws = [make((1,), ck.q[:limbs], 440 + i) for i in range(5)]
+    x = bufs(xs, scale)
+    got = ctx.rms_norm(x, T, 5 * 16, inv, to_dev(rlk), dev_keys(keys), weights=bufs(ws, scale), newton=1, eps=0.5, residual=x)
+    want = nc.rms_norm(ck, xs, scale, T, 5 * 16, inv, rlk, keys, "fm", ws, scale, newton=1, eps=0.5, residual=xs,
+                       r_scale=scale)
+    for g, w in zip(got, want):
+        same(g.data, w, "norm")
+
+
+@pytest.mark.parametrize("ring_args,near", [((8, 8, 3, 3, 50), 1.0), ((12, 8, 3, 3, 50), 1.0), ((14, 8, 3, 3, 50), 1.0),
+                                            ((10, 8, 3, 3, 59), 2.0 ** 9)], ids=str)
+def test_buffers_at_an_odd_word(ring_args, near):
+    from paper_2609_12378_amd import Epilogue
+    ctx, ck = ring(*ring_args)
+    limbs, T, scale = 8, ck.n // 32, SCALE * near
+    xs, rlk, poly = random_cts(ck, limbs, 2, 500), rlk_of(ck, 501), some_poly(9, 502)
+    odd = lambda a, s=scale: odd_words(a, s)  # noqa: E731
+    outs = odd([np.zeros((2, 3, ck.n), dtype=np.uint64)] * 2)
+    k = odd([rlk])[0].data
+    ctx.poly_eval(odd(xs), poly, k, outs=outs)
+    for g, x in zip(outs, xs):
+        same(g.data, nc.poly_eval(ck, x, scale, poly, rlk), "polynomial")
+    for layout in ("fm", "tm"):
+        st = norm_inputs(ck, limbs, T, layout, 2, "plain", "other", 510)
+        inv = some_poly(3, 511, 0.5, 3.0)
+        keys = {s: odd([v])[0].data for s, v in st["keys"].items()}
+        got = ctx.rms_norm(odd(st["xs"]), T, 2 * 16, inv, odd([st["rlk"]])[0].data, keys, layout=layout,
+                           weights=odd(st["ws"]), mask=odd([st["mask"]])[0] if layout == "tm" else None,
+                           residual=odd(st["res"]))
+        want = nc.rms_norm(ck, st["xs"], scale, T, 2 * 16, inv, st["rlk"], st["keys"], layout, st["ws"], scale, st["mask"],
+                           scale, residual=st["res"], r_scale=scale)
+        for g, w in zip(got, want):
+            same(g.data, w, "norm, %s" % layout)
+    keys, W = proj_keys(ck, T, "fm", 5), rng(520, 2).normal(0, 0.02, (16, 16))
+    b, gate, res = plaintexts(ck, limbs, 1, 521), random_cts(ck, limbs, 1, 522), random_cts(ck, limbs, 1, 523)
+    act = some_poly(3, 524)
+    got = ctx.linear_project(odd(xs[:1]), to_dev(W), T, 5, {s: odd([v])[0].data for s, v in keys.items()}, epilogue=Epilogue(
+        bias=odd(b), act=act, gate=odd(gate), residual=odd(res), rlk=k))
+    want = nc.project(ck, xs[:1], scale, W, T, 5, keys, "fm", rlk, [b[0][0][None]], scale, act, gate, scale, res, scale)
+    same(got[0].data, want[0], "projection")
+
+
+@pytest.mark.parametrize("ring_args", [(8, 8, 3, 3, 50), (12, 8, 3, 3, 50), (14, 8, 3, 3, 50)], ids=str)
+def test_operands_that_are_one_another(ring_args):
+    """A ciphertext twice in a list, weights and residual that are the input, one gate for two outputs that is their
+    residual too."""
+    from paper_2609_12378_amd import Epilogue
+    ctx, ck = ring(*ring_args)
+    limbs, T = 8, ck.n // 32
+    x, rlk, poly = random_cts(ck, limbs, 1, 600), rlk_of(ck, 601), some_poly(6, 602)
+    two, both = bufs(x, SCALE) * 2, x * 2
+    for g in ctx.poly_eval(two, poly, to_dev(rlk)):
+        same(g.data, nc.poly_eval(ck, x[0], SCALE, poly, rlk), "polynomial")
+    keys, inv = norm_inputs(ck, limbs, T, "fm", 1, None, None, 603)["keys"], some_poly(3, 604, 0.5, 3.0)
+    got = ctx.rms_norm(two, T, 20, inv, to_dev(rlk), dev_keys(keys), weights=two, residual=two, residual_scale=2.0)
+    want = nc.rms_norm(ck, both, SCALE, T, 20, inv, rlk, keys, "fm", both, SCALE, residual=both, r_scale=SCALE,
+                       residual_scale=2.0)
+    for g, w in zip(got, want):
+        same(g.data, w, "norm")
+    keys, W = proj_keys(ck, T, "fm", 16), rng(605, 2).normal(0, 0.02, (32, 32))
+    act = some_poly(3, 606)
+    got = ctx.linear_project(two, to_dev(W), T, 16, dev_keys(keys), epilogue=Epilogue(act=act, gate=two, residual=two,
+                                                                                      rlk=to_dev(rlk)))
+    want = nc.project(ck, both, SCALE, W, T, 16, keys, "fm", rlk, None, 1.0, act, both, SCALE, both, SCALE)
+    for g, w in zip(got, want):
+        same(g.data, w, "projection")
+
+
+def test_scales_that_leave_the_doubles():
+    """Products of scales that overflow or vanish would turn factors into zeros: refused, outputs as they were."""
+    from paper_2609_12378_amd import Buf, CkksError, Epilogue
+    ctx, ck = ring(8, 8, 3, 3, 50)
+    limbs, T = 8, ck.n // 32
+    st = norm_inputs(ck, limbs, T, "fm", 1, "plain", None, 700)
+    x, inv, old = to_dev(st["xs"][0]), some_poly(3, 701, 0.5, 3.0), random_cts(ck, 3, 1, 702)
+    out, rlk, keys = bufs(old, 1.0), to_dev(st["rlk"]), dev_keys(st["keys"])
+    w = to_dev(st["ws"][0])
+    for scale, w_scale in ((1e200, 1.0), (1e-200, 1.0), (1e150, 1e200), (1e-150, 1e-220), (SCALE, 1e308)):
+        with pytest.raises(CkksError, match="scale"):
+            ctx.rms_norm([Buf(x, scale)], T, 16, inv, rlk, keys, weights=[Buf(w, w_scale)], outs=out)
+    keys, W = dev_keys(proj_keys(ck, T, "fm", 16)), to_dev(rng(703, 2).normal(0, 0.02, (16, 16)))
+    x = x[:, :7].contiguous()
+    for scale, g_scale in ((1e-200, 1e200), (1e200, 1e-150), (math.inf, 1.0)):
+        with pytest.raises(CkksError, match="scale"):
+            ctx.linear_project([Buf(x, scale)], W, T, 16, keys, outs=out, epilogue=Epilogue(
+                act=inv, gate=[Buf(x, g_scale)], rlk=rlk))
+    assert np.array_equal(to_host(out[0].data), old[0])
