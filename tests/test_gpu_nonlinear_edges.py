@@ -132,3 +132,55 @@ def test_scales_that_leave_the_doubles():
             ctx.linear_project([Buf(x, scale)], W, T, 16, keys, outs=out, epilogue=Epilogue(
                 act=inv, gate=[Buf(x, g_scale)], rlk=rlk))
     assert np.array_equal(to_host(out[0].data), old[0])
+
+
+@pytest.mark.parametrize("log_n,q_bits,p_bits", [(8, 45, 60), (12, 45, 60), (14, 45, 60), (14, 50, 40), (13, 30, 50)])
+def test_special_primes_of_another_size(log_n, q_bits, p_bits):
+    """Transforms in fp64 with conversions and sums in integers, and the other way round; both layouts of a norm and a
+    projection with everything behind it."""
+    from oracle import Ckks
+    from paper_2609_12378_amd import Buf, Context, Epilogue
+    ctx = Context(log_n, 8, 3, 3, q_bits=q_bits, p_bits=p_bits)
+    ck = Ckks(log_n, ctx.q, ctx.p, 3)
+    limbs, T, scale = 8, ck.n // 32, 1.01 * 2.0 ** (q_bits - 1)
+    xs, rlk, poly = random_cts(ck, limbs, 2, 800), rlk_of(ck, 801), some_poly(11, 802)
+    for g, x in zip(ctx.poly_eval(bufs(xs, scale), poly, to_dev(rlk)), xs):
+        same(g.data, nc.poly_eval(ck, x, scale, poly, rlk), "polynomial")
+    inv = some_poly(3, 803, 0.5, 3.0)
+    for layout in ("fm", "tm"):
+        st = norm_inputs(ck, limbs, T, layout, 2, "plain", "in", 810)
+        got = ctx.rms_norm(bufs(st["xs"], scale), T, 32, inv, to_dev(st["rlk"]), dev_keys(st["keys"]), layout=layout,
+                           weights=bufs(st["ws"], scale), residual=bufs(st["xs"], scale),
+                           mask=Buf(to_dev(st["mask"]), scale) if layout == "tm" else None)
+        want = nc.rms_norm(ck, st["xs"], scale, T, 32, inv, st["rlk"], st["keys"], layout, st["ws"], scale, st["mask"], scale,
+                           residual=st["xs"], r_scale=scale)
+        for g, w in zip(got, want):
+            same(g.data, w, "norm, %s" % layout)
+    keys, W, act = proj_keys(ck, T, "fm", 5), rng(820, 2).normal(0, 0.02, (16, 16)), some_poly(2, 821)
+    got = ctx.linear_project(bufs(xs[:1], scale), to_dev(W), T, 5, dev_keys(keys), epilogue=Epilogue(
+        act=act, gate=bufs(xs[1:], scale), residual=bufs(xs[:1], scale), rlk=to_dev(rlk)))
+    want = nc.project(ck, xs[:1], scale, W, T, 5, keys, "fm", rlk, None, 1.0, act, xs[1:], scale, xs[:1], scale)
+    same(got[0].data, want[0], "projection")
+
+
+@pytest.mark.parametrize("ring_args,limbs", [((12, 7, 2, 4, 50), 7), ((14, 7, 3, 3, 50), 7)], ids=str)
+def test_one_workspace_for_either_arithmetic(ring_args, limbs):
+    """Polynomials and norms by integers in the workspace that was asked for under fp64, the same words."""
+    import torch
+    from test_gpu_nonlinear import three_calls
+    ctx, ck = ring(*ring_args)
+    T = ck.n // 64
+    x, gate = (bufs(random_cts(ck, limbs, 2, seed), SCALE) for seed in (900, 901))
+    calls, sizes = three_calls(ck, limbs, T, x, gate)
+    want = [to_host(b.data) for b in calls(ctx)]
+    mem = torch.full((max(sizes(ctx)) // 8 + 64,), 7, dtype=torch.uint64, device="cuda")
+    try:
+        ctx.set_workspace(mem[:-64])
+        for arith in (1, 0):
+            ctx.set_ntt_arith(arith)
+            for b, w in zip(calls(ctx), want):
+                same(b.data, w, "arithmetic %d" % arith)
+        assert bool((mem[-64:] == 7).all())
+    finally:
+        ctx.set_ntt_arith(0)
+        ctx.set_workspace(None)
