@@ -276,7 +276,7 @@ ckks_status rescale_each(ckks_ctx *ctx, const uint64_t *c, uint32_t count, uint3
 // matrix-core multiply-accumulate over residues (project_tm.hip): acc[jj] (+)= sum_kappa Q[kappa][jj] x_kappa for
 // jj < jc and the K ciphertexts kappa_base .. kappa_base + K - 1 of a digit layout Xd, per limb l and run x of
 // 2^logT positions: Q is [L][D2][K][jc] canonical residues as doubles (D2 runs), acc [jc][2][L][N] canonical.
-uint32_t mac_kt_pad(uint32_t kt);
+uint32_t mac_kt_pad(uint32_t kt);   // bytes of a row of the digit layout
 size_t mac_digit_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t kt_pad);
 uint32_t mac_max_outputs();
 // x2 ([kt][2][L][N] canonical) -> Xd, the digit layout of kt ciphertexts (mac_digit_bytes bytes)

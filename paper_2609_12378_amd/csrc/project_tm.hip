@@ -291,38 +291,40 @@ __device__ __forceinline__ void pack_digits(const uint64_t (&v)[4], uint32_t (&p
     }
 }
 
-// x2 ([n_in][n1][xr, xw][2][L][N] canonical) -> Xd[a][l][kappa / 64][poly N + pos][kappa mod 64],
-// kappa = 2 (i n1 + b) + uv < kt.  Block: (l, 64 columns, 64 kappa), staged through LDS.  Groups of 16 kappa from kt on
-// are left as they were: they are read against zero plaintext digits (32 kappa of 128, 10 limbs of N = 2^16: 306 us
-// with all written, so 273).
+// x2 ([n_in][n1][xr, xw][2][L][N] canonical) -> Xd[a][l][kappa / 64][poly N + pos][kappa mod 64], kappa = 2 (i n1 + b)
+// + uv < kt (zeros up to the next multiple of KW).  Block: (l, 4096 / KW columns, KW kappa), staged through LDS.  Up to
+// 32 kappa have rows of KW = 16 or 32 bytes (kt_pad = KW): a launch writes whole lines (10 limbs of N = 2^16, us: 16 kappa
+// in quarters of 64-byte rows 252, so 52; 32 kappa in halves 274, so 100, and their products 469, so 418; 96 kappa with
+// the last row half written 516, with its zeros 431).
+template <int KW>
 __global__ __launch_bounds__(kThreads) void k_xdigits(const uint64_t *__restrict__ x2, int8_t *Xd, uint32_t L,
                                                       uint32_t log_n, uint32_t kt, uint32_t kt_pad)
 {
-    __shared__ uint64_t tile[64][65];
-    const uint32_t cols = 2u << log_n, cblocks = cols / 64, kblocks = (kt + 63) / 64;
+    constexpr int kCols = 4096 / KW, kRows = kThreads > kCols ? kThreads / kCols : 1, kLoads = 4096 / kThreads;
+    static_assert(kThreads == kCols * KW / 16 && kRows * kCols == kThreads, "16 values a thread");
+    __shared__ uint64_t tile[KW][kCols + 1];
+    const uint32_t cols = 2u << log_n, cblocks = cols / kCols, kblocks = (kt + KW - 1) / KW;
     const uint32_t kb = blockIdx.x % kblocks, rest = blockIdx.x / kblocks;
     const uint32_t cb = rest % cblocks, l = rest / cblocks;
     const size_t n = (size_t)1 << log_n, ctw = 2 * (size_t)L * n;
-    const uint32_t c0 = cb * 64, k0 = kb * 64;
+    const uint32_t c0 = cb * kCols, k0 = kb * KW;
     // all 16 loads of a thread issued before any is stored (one memory wait per thread, not sixteen)
-    const uint32_t cc_r = threadIdx.x % 64, c = c0 + cc_r;
+    const uint32_t cc_r = threadIdx.x % kCols, r0 = threadIdx.x / kCols, c = c0 + cc_r;
     const uint32_t poly = c >> log_n, pos = c & ((1u << log_n) - 1);
     const uint64_t *src = x2 + ((size_t)poly * L + l) * n + pos;
-    uint64_t vals[64 * 64 / kThreads];
+    uint64_t vals[kLoads];
 #pragma unroll
-    for (int i = 0; i < 64 * 64 / kThreads; i++) {
-        const uint32_t kappa = k0 + threadIdx.x / 64 + (kThreads / 64) * i;
+    for (int i = 0; i < kLoads; i++) {
+        const uint32_t kappa = k0 + r0 + kRows * i;
         vals[i] = kappa < kt ? src[(size_t)kappa * ctw] : 0;
     }
 #pragma unroll
-    for (int i = 0; i < 64 * 64 / kThreads; i++) tile[threadIdx.x / 64 + (kThreads / 64) * i][cc_r] = vals[i];
+    for (int i = 0; i < kLoads; i++) tile[r0 + kRows * i][cc_r] = vals[i];
     __syncthreads();
     // each thread writes 16 consecutive kappa of one column: one 16-byte store per digit plane (kt_pad, k0 and the
     // 16-kappa offset are multiples of 16, and Xd is 16-byte aligned)
     const size_t plane = (size_t)L * cols * kt_pad;
-    static_assert(kThreads == 256, "64 columns x 4 groups of 16 kappa");
-    const uint32_t cc = threadIdx.x >> 2, kq = (threadIdx.x & 3u) << 4;
-    if (k0 + kq >= kt) return;
+    const uint32_t cc = threadIdx.x / (KW / 16), kq = threadIdx.x % (KW / 16) * 16;
     uint32_t w[8][4];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
@@ -334,7 +336,7 @@ __global__ __launch_bounds__(kThreads) void k_xdigits(const uint64_t *__restrict
 #pragma unroll
         for (int a = 0; a < kDig; a++) w[a][i] = packed[a];
     }
-    int8_t *dst = Xd + (((size_t)l * (kt_pad / 64) + kb) * cols + c0 + cc) * 64 + kq;
+    int8_t *dst = Xd + (((size_t)l * (kt_pad / KW) + kb) * cols + c0 + cc) * KW + kq;
 #pragma unroll
     for (int a = 0; a < kDig; a++)
         *(uint4 *)(dst + (size_t)a * plane) = make_uint4(w[a][0], w[a][1], w[a][2], w[a][3]);
@@ -384,13 +386,14 @@ __global__ __launch_bounds__(64 * NW) void k_mac_tm_mfma(uint64_t *acc, const in
     const size_t n = (size_t)1 << log_n, cols = 2 * n;
     const size_t plane = (size_t)L * cols * kt_pad;
     // this lane's 16 kappa of a 64-kappa step lie in one 64-kappa block of Xd (kappa_base is a multiple of 16): a
-    // 32-bit lane offset from a uniform base per step and digit
-    const uint32_t kl = (kappa_base & 63u) + 16 * (lane >> 4);
-    const uint32_t loff = ((kl >> 6) * (uint32_t)cols + pos) * 64 + (kl & 63u);
+    // 32-bit lane offset from a uniform base per step and digit.  Rows shorter than 64 are read again where they end,
+    // against zero plaintext digits.
+    const uint32_t kl = (kappa_base & 63u) + 16 * (lane >> 4), width = min(kt_pad, 64u);
+    const uint32_t loff = ((width < 64 ? 0u : kl >> 6) * (uint32_t)cols + pos) * width + (kl & (width - 1));
     const uint32_t kblocks = (K + kKB - 1) / kKB, steps = polys * kblocks;
     auto step_base = [&](uint32_t s) {
         const uint32_t poly = poly0 + s / kblocks, kb = (kappa_base >> 6) + s % kblocks;
-        return Xd + (((size_t)l * (kt_pad / 64) + kb) * cols + poly * n) * 64;
+        return Xd + (((size_t)l * (kt_pad / width) + kb) * cols + poly * n) * width;
     };
     const double *qx = Q + ((size_t)l * D2 + x) * (size_t)K * jc + jj0;
     // the digits of kappa c0 .. c0 + 64 nkb - 1
@@ -521,7 +524,7 @@ TmScratch tm_scratch(const ckks_ctx *ctx, uint32_t L, uint32_t D, uint32_t d_in,
     Pb &= ~7u;
     ts.Pb = std::min(Pb, maxpairs);
     ts.kt = 2 * n_in * n1;
-    ts.kt_pad = ((ts.kt + 63) & ~63u) + 64;
+    ts.kt_pad = mac_kt_pad(ts.kt);
     ts.x2_w = (size_t)n_in * n1 * 2 * ctw;
     ts.acc_w = ts.rot_w = (size_t)rows * ctw;
     ts.tot_w = (size_t)ts.Jt * ctw;
@@ -604,7 +607,7 @@ ckks_status tm_check_shape(const ckks_ctx *ctx, uint32_t L, uint32_t T, uint32_t
 
 }  // namespace
 
-uint32_t mac_kt_pad(uint32_t kt) { return ((kt + 63) & ~63u) + 64; }
+uint32_t mac_kt_pad(uint32_t kt) { return kt <= 16 ? 16 : kt <= 32 ? 32 : ((kt + 63) & ~63u) + 64; }
 
 size_t mac_digit_bytes(const ckks_ctx *ctx, uint32_t L, uint32_t kt_pad)
 {
@@ -615,9 +618,15 @@ uint32_t mac_max_outputs() { return kMaxJtMfma; }
 
 ckks_status launch_xdigits(ckks_ctx *ctx, const uint64_t *x2, int8_t *Xd, uint32_t L, uint32_t kt, uint32_t kt_pad)
 {
-    const uint32_t blocks = L * (uint32_t)((2 * ctx->n) / 64) * ((kt + 63) / 64);
-    prof_begin(ctx, K_ELEM, (8.0 * kt + (double)kDig * ((kt + 15) & ~15u)) * 2 * L * ctx->n);
-    hipLaunchKernelGGL(k_xdigits, dim3(blocks), dim3(kThreads), 0, ctx->stream, x2, Xd, L, ctx->log_n, kt, kt_pad);
+    const uint32_t rows = std::min(kt_pad, (kt + 63) & ~63u);
+    prof_begin(ctx, K_ELEM, (8.0 * kt + (double)kDig * rows) * 2 * L * ctx->n);
+    const auto go = [&](auto kernel, uint32_t kw) {
+        const uint32_t blocks = L * (2 * ctx->n / (4096 / kw)) * ((kt + kw - 1) / kw);
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, ctx->stream, x2, Xd, L, ctx->log_n, kt, kt_pad);
+    };
+    if (kt_pad == 16) go(k_xdigits<16>, 16);
+    else if (kt_pad == 32) go(k_xdigits<32>, 32);
+    else go(k_xdigits<64>, 64);
     prof_end(ctx, K_ELEM);
     HIP_TRY(hipGetLastError());
     return CKKS_OK;
@@ -628,7 +637,7 @@ ckks_status launch_mac_mfma(ckks_ctx *ctx, uint64_t *acc, const int8_t *Xd, cons
 {
     const uint32_t tiles16 = 1u << (logT - 4);
     CK_REQUIRE(jc >= 1 && jc <= (uint32_t)kMaxRowsMfma && kbase % 16 == 0 && K >= 1 && K <= 4096 && logT >= 4 &&
-                   logT <= 7 && kbase + ((K + 63) & ~63u) <= kt_pad,
+                   logT <= 7 && kbase + (kt_pad < 64 ? K : (K + 63) & ~63u) <= kt_pad,
                CKKS_EINVAL, "matrix-core multiply-accumulate: unsupported tile (jc %u, kappa base %u, K %u, T %u)",
                jc, kbase, K, 1u << logT);
     const double res = (double)jc * 2 * L * ctx->n;
