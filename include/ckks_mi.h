@@ -584,8 +584,10 @@ typedef struct {
  *   out  the step of y, m limbs, with (w x), the step of x and w from m + 1 limbs,
  *        and the residual: m - 1 limbs, scale S
  * so m = Lv - 1 - D' - 2 newton >= 2; L = 4 + D' + 2 newton (+ 1) at least.  Keys
- * (Galois; steps modulo N/2): the rounds' rotations, both signs token-major; a round
- * of 16 reads 15 keys for one ModUp and one ModDown.
+ * (Galois; steps modulo N/2): the rounds' rotations, both signs token-major; of two
+ * keys for one rotation (one token a ciphertext: k and k - N/2) the one given for the
+ * signed step, k times the stride, else the first.  A round of 16 reads 15 keys for
+ * one ModUp and one ModDown.
  * Scratch: CKKS_OP_RMS_NORM.  Other errors as ckks_poly_eval's, CKKS_ENOKEY. */
 ckks_status ckks_rms_norm(ckks_ctx *ctx, const ckks_buf *in, uint32_t count, const ckks_norm_shape *shape,
                           const ckks_poly *inv_root, const ckks_buf *weights, const ckks_buf *mask,

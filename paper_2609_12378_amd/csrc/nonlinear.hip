@@ -105,8 +105,11 @@ ckks_status sum_rounds(const ckks_ctx *ctx, uint32_t count, int64_t stride, cons
         for (uint32_t k = 1; k < radix; k++) {
             const int64_t st = ((k * stride) % slots + slots) % slots;
             const uint64_t *key = nullptr;
-            for (uint32_t i = 0; i < n_keys && !key; i++)
-                if (((int64_t)key_steps[i] % slots + slots) % slots == st) key = keys[i];
+            bool exact = false;   // a key given for the step itself is taken before one for an equal rotation
+            for (uint32_t i = 0; i < n_keys && !exact; i++) {
+                exact = keys[i] && key_steps[i] == k * stride;
+                if (exact || (!key && ((int64_t)key_steps[i] % slots + slots) % slots == st)) key = keys[i];
+            }
             CK_REQUIRE(key, CKKS_ENOKEY, "rms_norm: no key for step %lld (modulo %lld)", (long long)st, (long long)slots);
             r.g.push_back(ckks_galois_elt(ctx, (int32_t)st));
             r.key.push_back(key);

@@ -184,3 +184,36 @@ def test_one_workspace_for_either_arithmetic(ring_args, limbs):
     finally:
         ctx.set_ntt_arith(0)
         ctx.set_workspace(None)
+
+
+@pytest.mark.parametrize("log_n", [8, 12])
+def test_two_keys_for_one_rotation(log_n, monkeypatch):
+    """One token a ciphertext, token-major: left rotations by k and by k - N/2 are one. A key for each is given, and each is
+    used where its step is asked for, whatever their order; one key alone serves both."""
+    from paper_2609_12378_amd import Buf
+    ctx, ck = ring(log_n, 8, 3, 3, 50)
+    limbs, slots = 8, ck.n // 2
+    st = norm_inputs(ck, limbs, 1, "tm", 1, None, None, 950)
+    there, unit = {}, 1
+    for radix in nc.radixes(slots):
+        there.update({k * unit: None for k in range(1, radix)})
+        unit *= radix
+    back = random_keys(ck, there, 951)
+    there = random_keys(ck, there, 952)
+    spread = {(-s) % slots: back[s] for s in back}
+    plain = nc.all_positions
+    inv, mask = some_poly(3, 953, 0.5, 3.0), Buf(to_dev(st["mask"]), SCALE)
+
+    def want(fwd, rev):
+        monkeypatch.setattr(nc, "all_positions", lambda ck, v, n, stride, keys: plain(ck, v, n, stride,
+                                                                                      fwd if stride > 0 else rev))
+        return nc.rms_norm(ck, st["xs"], SCALE, 1, slots, inv, st["rlk"], {}, "tm", None, 1.0, st["mask"], SCALE)[0]
+
+    def got(keys):
+        return ctx.rms_norm(bufs(st["xs"], SCALE), 1, slots, inv, to_dev(st["rlk"]), dev_keys(keys), layout="tm", mask=mask)[0]
+
+    signed, both = {-s: back[s] for s in back}, want(there, spread)
+    same(got({**signed, **there}).data, both, "the keys back first")
+    same(got({**there, **signed}).data, both, "the keys there first")
+    one = {**spread, **there}
+    same(got(one).data, want(one, one), "one key a rotation")
