@@ -27,7 +27,7 @@ struct Step {
     // a product (a null: none): b a ciphertext or (b_polys 1) a plaintext, which needs no key; limbs >= L
     const uint64_t *a = nullptr, *b = nullptr;
     uint32_t a_limbs = 0, b_limbs = 0, b_polys = 2;
-    int32_t mult = 1;         // 1, 2 or -1
+    int32_t mult = 1;         // 1, 2 or -1; of a product with a plaintext 1
     // or a sum of products [3][L][N]
     const uint64_t *d = nullptr;
     uint32_t n_terms = 0;

@@ -313,8 +313,10 @@ ckks_status step_run(ckks_ctx *ctx, uint32_t L, const std::vector<Step> &steps, 
     std::vector<const Step *> list;
     size_t n_sw = 0;
     for (int sw = 1; sw >= 0; sw--) {
-        for (const Step &s : steps)
+        for (const Step &s : steps) {
+            CK_REQUIRE(!s.a || s.b_polys == 2 || s.mult == 1, CKKS_EINVAL, "a step's product with a plaintext times %d", s.mult);
             if (s.switched() == (sw != 0)) list.push_back(&s);
+        }
         if (sw) n_sw = list.size();
     }
     const bool fast = f64_switch(ctx, L - 1);
