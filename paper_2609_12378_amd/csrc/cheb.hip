@@ -159,7 +159,7 @@ ckks_status cheb_run(ckks_ctx *ctx, const ChebPlan &plan, const std::vector<cons
                     Step s;
                     if (o.x >= 0) s.product(of(o.x, r), limbs(o.x), of(o.y, r), limbs(o.y), o.mult);
                     for (const ChebTerm &t : o.t) s.term(of(t.of, r), limbs(t.of), t.k);
-                    if (i == last && !extra.empty()) s.t[s.n_terms++] = extra[r0 + r];
+                    if (i == last && !extra.empty()) s.term(extra[r0 + r]);
                     s.c = o.c;
                     s.out = i == last ? out[r0 + r] : base[i] + (size_t)r * 2 * limbs(i) * N;
                     steps.push_back(s);

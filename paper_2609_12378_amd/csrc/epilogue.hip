@@ -137,7 +137,7 @@ extern "C" ckks_status ckks_linear_project_epilogue(ckks_ctx *ctx, const ckks_bu
                 Step &s = st[j];
                 s.term(tot + (size_t)j * 2 * L * N, L, StepInt{1, 0});
                 if (epi->bias) s.term(epi->bias[j0 + j].data, epi->bias[j0 + j].n_limbs, kb, 1);
-                if (epi->residual && !act && !gate) s.t[s.n_terms++] = residual(j0 + j);
+                if (epi->residual && !act && !gate) s.term(residual(j0 + j));
                 s.c = c;
                 s.out = act || gate ? mid(j0 + j) : out[j0 + j].data;
             }
@@ -162,7 +162,7 @@ extern "C" ckks_status ckks_linear_project_epilogue(ckks_ctx *ctx, const ckks_bu
             std::vector<Step> st(n_out);
             for (uint32_t j = 0; j < n_out; j++) {
                 st[j].product(x[j], m, epi->gate[j].data, epi->gate[j].n_limbs);
-                if (epi->residual) st[j].t[st[j].n_terms++] = residual(j);
+                if (epi->residual) st[j].term(residual(j));
                 st[j].out = out[j].data;
             }
             CK_TRY(step_run(ctx, m, st, epi->dev_rlk, work));

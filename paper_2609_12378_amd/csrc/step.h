@@ -30,7 +30,7 @@ struct Step {
     int32_t mult = 1;         // 1, 2 or -1; of a product with a plaintext 1
     // or a sum of products [3][L][N]
     const uint64_t *d = nullptr;
-    uint32_t n_terms = 0;
+    uint32_t n_terms = 0;     // more than kStepTerms are counted and not kept: step_run refuses them
     StepTerm t[kStepTerms];
     StepInt c;
     uint64_t *out = nullptr;  // [2][L - 1][N]; overlaps no operand of the call's steps
@@ -40,7 +40,12 @@ struct Step {
     {
         a = a_, a_limbs = al, b = b_, b_limbs = bl, mult = m, b_polys = bp;
     }
-    void term(const uint64_t *z, uint32_t limbs, StepInt k, uint32_t polys = 2) { t[n_terms++] = {z, limbs, polys, k}; }
+    void term(const StepTerm &s)
+    {
+        if (n_terms < kStepTerms) t[n_terms] = s;
+        n_terms++;
+    }
+    void term(const uint64_t *z, uint32_t limbs, StepInt k, uint32_t polys = 2) { term(StepTerm{z, limbs, polys, k}); }
 };
 
 // words of scratch for up to `steps` steps at L limbs; switched: some have a product of ciphertexts

@@ -315,6 +315,7 @@ ckks_status step_run(ckks_ctx *ctx, uint32_t L, const std::vector<Step> &steps, 
     for (int sw = 1; sw >= 0; sw--) {
         for (const Step &s : steps) {
             CK_REQUIRE(!s.a || s.b_polys == 2 || s.mult == 1, CKKS_EINVAL, "a step's product with a plaintext times %d", s.mult);
+            CK_REQUIRE(s.n_terms <= kStepTerms, CKKS_EINVAL, "a step of %u terms, at most %u", s.n_terms, kStepTerms);
             if (s.switched() == (sw != 0)) list.push_back(&s);
         }
         if (sw) n_sw = list.size();
