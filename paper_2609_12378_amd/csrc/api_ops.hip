@@ -541,7 +541,7 @@ ckks_status ckks_modup(ckks_ctx *ctx, const uint64_t *c, uint32_t level, uint64_
     CK_TRY(ctx_scratch(ctx, op_workspace_bytes(ctx, CKKS_OP_MODUP, &level), &w));
     const size_t dig_w = (size_t)nd * ext * N, c_w = (size_t)(level + 1) * N;
     if (f64_switch(ctx, level) && !overlap(digits, dig_w, c, c_w)) {
-        if (blk_switch(ctx, level)) return blk_modup(ctx, PolySrc{c, 0, {}}, nullptr, 1, level, digits, (uint64_t *)w);
+        if (blk_switch(ctx, level)) return blk_modup(ctx, PolySrc{c, 0, {}}, 1, level, digits, (uint64_t *)w);
         return up_modup(ctx, PolySrc{c, 0, {}}, 1, level, digits);
     }
     CK_TRY(ks_modup(ctx, c, level, (uint64_t *)w, ctx->alpha));

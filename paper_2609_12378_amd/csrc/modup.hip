@@ -580,6 +580,7 @@ ckks_status up_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t 
 }
 ckks_status up_modup_cols(ckks_ctx *ctx, const PolyProd &c, uint32_t count, uint32_t level, uint64_t *digits)
 {
+    CK_REQUIRE(count <= (uint32_t)kPolyList, CKKS_EINVAL, "a ModUp of %u products, at most %d", count, kPolyList);
     return modup_of(ctx, c, nullptr, count, level, digits, false);
 }
 

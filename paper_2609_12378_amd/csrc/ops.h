@@ -152,10 +152,8 @@ ckks_status blk_decrypt(ckks_ctx *ctx, uint64_t *pt, const uint64_t *c0, const u
                         uint32_t limbs);
 // rescale of `polys` polynomials c ([polys][l+1][N]) into out ([polys][l][N]); work: polys N words
 ckks_status blk_rescale(ckks_ctx *ctx, const uint64_t *c, uint32_t polys, uint32_t l, uint64_t *out, uint64_t *work);
-// ModUp of `count` polynomials, or (b set, count 1) of the product of the second components of the ciphertexts whose
-// second components start at c1 and at b + (level+1) N; stage: count (level+1) N words
-ckks_status blk_modup(ckks_ctx *ctx, const PolySrc &c1, const uint64_t *b, uint32_t count, uint32_t level,
-                      uint64_t *digits, uint64_t *stage);
+// ModUp of `count` polynomials; stage: count (level+1) N words
+ckks_status blk_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t level, uint64_t *digits, uint64_t *stage);
 // of at most kPolyList products (ks_args.h)
 ckks_status blk_modup(ckks_ctx *ctx, const PolyProd &c, uint32_t count, uint32_t level, uint64_t *digits, uint64_t *stage);
 // a rotation batch; with ta, tb2 (ciphertexts) the addends are the first two components of their tensor product.

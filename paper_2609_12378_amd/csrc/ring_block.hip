@@ -741,7 +741,7 @@ ckks_status blk_rescale(ckks_ctx *ctx, const uint64_t *c, uint32_t polys, uint32
 
 namespace {
 
-ckks_status modup_of(ckks_ctx *ctx, const Source &from, bool b, uint32_t count, uint32_t level, uint64_t *digits,
+ckks_status modup_of(ckks_ctx *ctx, const Source &from, bool products, uint32_t count, uint32_t level, uint64_t *digits,
                      uint64_t *stage)
 {
     Digits dg{};
@@ -769,10 +769,10 @@ ckks_status modup_of(ckks_ctx *ctx, const Source &from, bool b, uint32_t count, 
         double *yr = y + (size_t)r0 * dg.L * N;
         prof_begin(ctx, K_NTT_INV_ROW, 16.0 * cnt * dg.L * N);
 #define CK_K(LG) k_blk_digits<LG, true>
-        if (b) CK_BLK13(CK_K, dim3(dg.L, cnt), yr, src, dg, tb);
+        if (products) CK_BLK13(CK_K, dim3(dg.L, cnt), yr, src, dg, tb);
 #undef CK_K
 #define CK_K(LG) k_blk_digits<LG, false>
-        if (!b) CK_BLK13(CK_K, dim3(dg.L, cnt), yr, src, dg, tb);
+        if (!products) CK_BLK13(CK_K, dim3(dg.L, cnt), yr, src, dg, tb);
 #undef CK_K
         prof_end(ctx, K_NTT_INV_ROW);
         HIP_TRY(hipGetLastError());
@@ -780,12 +780,12 @@ ckks_status modup_of(ckks_ctx *ctx, const Source &from, bool b, uint32_t count, 
         const size_t blocks = (size_t)ext * dg.nd * cnt;
 #define CK_E(LG) k_blk_modup<LG, true, true>
 #define CK_L(LG) k_blk_modup<LG, true, false>
-        if (b) CK_BLK13_E(blocks, dim3(ext, dg.nd, cnt), d, yr, src, dg, tb);
+        if (products) CK_BLK13_E(blocks, dim3(ext, dg.nd, cnt), d, yr, src, dg, tb);
 #undef CK_E
 #undef CK_L
 #define CK_E(LG) k_blk_modup<LG, false, true>
 #define CK_L(LG) k_blk_modup<LG, false, false>
-        if (!b) CK_BLK13_E(blocks, dim3(ext, dg.nd, cnt), d, yr, src, dg, tb);
+        if (!products) CK_BLK13_E(blocks, dim3(ext, dg.nd, cnt), d, yr, src, dg, tb);
 #undef CK_E
 #undef CK_L
         prof_end(ctx, K_CONV);
@@ -796,16 +796,13 @@ ckks_status modup_of(ckks_ctx *ctx, const Source &from, bool b, uint32_t count, 
 
 }  // namespace
 
-ckks_status blk_modup(ckks_ctx *ctx, const PolySrc &c1, const uint64_t *b, uint32_t count, uint32_t level,
-                      uint64_t *digits, uint64_t *stage)
+ckks_status blk_modup(ckks_ctx *ctx, const PolySrc &c1, uint32_t count, uint32_t level, uint64_t *digits, uint64_t *stage)
 {
-    Source src{c1, {}, {}};
-    if (b) src.mul[0] = b + (size_t)(level + 1) * ctx->n;
-    src.mult[0] = 1;
-    return modup_of(ctx, src, b != nullptr, count, level, digits, stage);
+    return modup_of(ctx, Source{c1, {}, {}}, false, count, level, digits, stage);
 }
 ckks_status blk_modup(ckks_ctx *ctx, const PolyProd &c, uint32_t count, uint32_t level, uint64_t *digits, uint64_t *stage)
 {
+    CK_REQUIRE(count <= (uint32_t)kPolyList, CKKS_EINVAL, "a ModUp of %u products, at most %d", count, kPolyList);
     Source src{};
     for (uint32_t r = 0; r < count; r++) {
         src.c1.list[r] = c.list[r];

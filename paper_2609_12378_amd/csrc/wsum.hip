@@ -608,7 +608,7 @@ ckks_status modup_cts(ckks_ctx *ctx, uint32_t L, const Args &a, uint32_t n_rot, 
         static_assert(kWsumCts <= (uint32_t)kPolyList, "a batch's polynomials fit the list");
         PolySrc src{};
         for (uint32_t i = 0; i < n_rot; i++) src.list[i] = a.ct[i].c + (size_t)L * ctx->n;
-        return blk_switch(ctx, L - 1) ? blk_modup(ctx, src, nullptr, n_rot, L - 1, dig, stage)
+        return blk_switch(ctx, L - 1) ? blk_modup(ctx, src, n_rot, L - 1, dig, stage)
                                       : up_modup(ctx, src, n_rot, L - 1, dig, false);
     }
     CK_TRY(wsum_gather_c1(ctx, a, n_rot, L, stage));

@@ -122,3 +122,30 @@ int main()
 }
 """)
     assert out == "127 degrees"
+
+
+def test_more_products_than_a_list_holds(tmp_path):
+    """ModUps of products take their operands from lists of kPolyList: a longer batch is refused on the host.  Those of
+    polynomials alone take no second factor (one for every entry of a batch, it was used for the first)."""
+    hp.run(tmp_path, RING + r"""
+#include "ks_args.h"
+#include "ops.h"
+
+int main()
+{
+    ckks_ctx c;
+    ring(c);
+    PolyProd p[2] = {};
+    ckks_status (*const polys)(ckks_ctx *, const PolySrc &, uint32_t, uint32_t, uint64_t *, uint64_t *) = blk_modup;
+    CHECK(polys);
+    for (uint32_t count : {(uint32_t)kPolyList + 1, 70000u}) {
+        clear_error();
+        CHECK(blk_modup(&c, p[0], count, 3, nullptr, nullptr) == CKKS_EINVAL);
+        CHECK(std::strstr(ckks_last_error(), "products"));
+        clear_error();
+        CHECK(up_modup_cols(&c, p[0], count, 3, nullptr) == CKKS_EINVAL);
+        CHECK(std::strstr(ckks_last_error(), "products"));
+    }
+    return 0;
+}
+""")
