@@ -204,6 +204,17 @@ def test_norms_at_the_borders_of_a_batch(log_n, count, weights):
         same(got[r].data, want[r], "ciphertext %d" % r)
 
 
+@pytest.mark.parametrize("ring_args,limbs,degree", [((14, 9, 1, 9, 50), 9, 12), ((14, 9, 1, 9, 50), 7, 5),
+                                                    ((15, 6, 1, 6, 50), 6, 8), ((16, 6, 1, 6, 50), 5, 4)], ids=str)
+def test_many_digits_in_two_passes(ring_args, limbs, degree):
+    """A step's digits end their transforms four to a reduction, its own apart: five to nine of them, and odd counts left."""
+    ctx, ck = ring(*ring_args)
+    poly, rlk = some_poly(degree, 1220 + degree), rlk_of(ck, 1221)
+    xs = random_cts(ck, limbs, 2, 1222)
+    for g, x in zip(ctx.poly_eval(bufs(xs, SCALE), poly, to_dev(rlk)), xs):
+        same(g.data, nc.poly_eval(ck, x, SCALE, poly, rlk), "polynomial")
+
+
 # ---- the epilogue over lazily divided sums ------------------------------------------------------------------------
 
 # ring, limbs, tokens, layout, d_in and d_out in ciphertexts, n1, degree
