@@ -522,9 +522,10 @@ ckks_status ckks_cache_append(ckks_ctx *ctx, const ckks_buf *k, const ckks_buf *
  * below, evaluated in double from left to right (ties to even); from 2^120 on
  * the call is refused (CKKS_ESCALE).  q(L) is the top prime of L limbs.  A value
  * keeps about log2 scale - 12 bits; scales near the primes keep the most.
- * Needs special primes; any primes and rings the context takes.  Outputs may
- * overlap neither inputs nor each other (CKKS_EINVAL); operands may be one
- * another.  All checks are before the first launch. */
+ * Needs special primes; any primes and rings the context takes (token-major
+ * projections: those of ckks_linear_project_tm).  Outputs may overlap neither
+ * inputs nor each other (CKKS_EINVAL); operands may be one another.  All checks
+ * are before the first launch. */
 
 /* sum_{i <= degree} coefs[i] T_i(t), T_i the Chebyshev polynomials, of t = (2 x -
  * lo - hi) / (hi - lo): what a smooth function on [lo, hi] is replaced by (its

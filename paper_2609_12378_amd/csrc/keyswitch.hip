@@ -1161,7 +1161,11 @@ ckks_status ks_moddown(ckks_ctx *ctx, uint64_t *u, uint32_t polys, uint32_t leve
     if (s1 > 0 && s2 == 8 && polys % 2 == 0 && polys / 2 <= (uint32_t)kRotBatch && ntt_uses_f64(ctx, L) &&
         ntt_map_f64(ctx, pm) && up_conv_ok(ctx, cd)) {
         // a rotation batch's ModDown: the row pass of the P rows, their columns with the conversion, the quotient in the
-        // last row pass (two polynomials of 24 + 8 limbs at N = 2^16 76 -> 58 us)
+        // last row pass.  Against the separate stages below, us for 2, 8 and 64 polynomials: N = 2^16, 24 + 8 limbs 57 and
+        // 74, 139 and 194, 929 and 1422; 2 + 8 limbs 44 and 43, 52 and 63, 259 and 355; N = 2^15, 12 + 4 limbs 42 and 43, 55
+        // and 74, 281 and 377; 2 + 4 limbs 33 and 34, 38 and 41, 102 and 129; N = 2^14, 12 + 4 limbs 31 and 36 for 2, 32 and
+        // 44 for 4, above which whole rows take it.  No count, ring or level between is slower by more than the 3 us in
+        // which a pair's few launches vary.
         RotArgs ra{};
         ra.count = polys / 2;
         for (uint32_t r = 0; r < ra.count; r++) {

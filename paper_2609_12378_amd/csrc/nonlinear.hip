@@ -77,7 +77,11 @@ size_t poly_mem(const ckks_ctx *ctx, uint32_t L, uint32_t count, const ChebPlan 
 }
 
 // Radixes of the rounds of a sum over 2^bits positions: at most 16, as even as they go.  A round of radix R reads R - 1
-// keys for one ModUp and one ModDown.
+// keys for one ModUp and one ModDown.  Measured on both sides, us a norm with rounds of up to 16, 8 and 4: fewer rounds win
+// wherever launches count (N = 2^12, one ciphertext 246, 275, 306; 2^13 590, 631, 680; 2^14 616, 656, 710, token-major 810,
+// 889, 990; 2^15 787, 797, 842; 2^16 of 6 limbs 496, 527, 583), fewer keys at N = 2^16 from about 12 limbs on (13 limbs
+// 1199, 1171, 1207; 24 limbs 2164, 2026, 2047; 16 ciphertexts of 24 limbs 3378, 3235, 3269).  One rule for all, since the
+// radixes say which keys a program makes: it costs those 2 to 7%, and 13 keys more for 256 positions.
 std::vector<uint32_t> sum_radixes(uint32_t count)
 {
     uint32_t bits = 0;
